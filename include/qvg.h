@@ -354,6 +354,110 @@ int qvg_attn_merge(int64_t n_rows, int32_t head_dim, const void *out_a_bf16, con
                    void *stream);
 
 /*
+ * Paged caches.  A cache of several chunks per unit (chunk_len = page_len tokens each) also serves as a POOL of pages for
+ * many sequences: page i of a unit is its tokens i * page_len .. (i + 1) * page_len - 1 and its table(s) i, written by
+ * qvg_encode_chunk like chunk i of a cache.  A sequence is a list of pages, the same ones in every unit; the pages hold its
+ * oldest tokens, all of them full but perhaps the last, and a bf16 TAIL holds the newest ones until they fill a page.
+ */
+
+/* What a step of a batch of sequences attends with and to (a HOST structure; its pointers are device pointers). */
+typedef struct qvg_tree_step {
+    int32_t n_seqs;            /* sequences, 0 .. 65535                                                          */
+    int32_t group;             /* query heads per KV head, >= 1: query head h reads KV head h / group            */
+    int32_t n_nodes;           /* new tokens per sequence, >= 0 (rows of q, k_new and v_new); group * n_nodes <= 2^20 */
+    int32_t table_pages;       /* entries of page_table per sequence, >= 0                                       */
+    int64_t page_len;          /* tokens of a page, >= 1; table_pages * page_len below 2^31                      */
+    int64_t pool_pages;        /* pages of a unit in the pool, 1 .. 2^31 - 1                                     */
+    const int32_t *page_table; /* [n_seqs][table_pages]: the sequence's pages in order; entries behind its last page are not
+                                  read; one outside 0 .. pool_pages - 1 reads the nearest page of the pool       */
+    const int32_t *kv_len;     /* [n_seqs] compressed tokens, clamped to 0 .. table_pages * page_len; NULL with table_pages == 0 */
+    const void *q;             /* bf16 [n_seqs][n_heads * group][n_nodes][d]: strides in elements, multiples of 8 */
+    int64_t q_stride_seq, q_stride_head, q_stride_node;
+    const void *k_new, *v_new; /* bf16 [n_seqs][n_heads][n_nodes][d]: K (already rotated) and V of the new tokens */
+    int64_t new_stride_seq, new_stride_head, new_stride_node;
+    const void *k_tail, *v_tail;  /* bf16 [n_seqs][n_heads][tail_capacity][d] (K already rotated); NULL with tail_capacity == 0 */
+    int64_t tail_stride_seq, tail_stride_head, tail_stride_token;
+    const int32_t *tail_len;   /* [n_seqs], clamped to 0 .. tail_capacity; NULL with tail_capacity == 0           */
+    int32_t tail_capacity;
+    int32_t reserved;          /* 0 */
+    const int32_t *nodes;      /* [n_seqs] new tokens that are there, clamped to 0 .. n_nodes; NULL: n_nodes      */
+    const uint32_t *mask;      /* [n_seqs][n_nodes][ceil(n_nodes / 32)]: bit j of row i (bit j % 32 of word j / 32): new token i
+                                  sees new token j; NULL: it sees the new tokens 0 .. i                          */
+    const void *k_rope_f16;    /* NULL, or [rope_tokens][d/2][2] f16 (cos, sin), as in qvg_attn_decode_ex: compressed keys are
+                                  rotated by their place in the sequence (0 .. kv_len - 1; beyond the table: its last row) */
+    int64_t rope_tokens;
+    void *out;                 /* bf16 [n_seqs][n_heads * group][n_nodes][d], strides like q's                    */
+    int64_t out_stride_seq, out_stride_head, out_stride_node;
+    float *lse;                /* [n_seqs][n_heads * group][n_nodes] fp32 natural-log sum of exp, or NULL         */
+} qvg_tree_step;
+
+/*
+ * Attention of the few new tokens of a step (one per sequence, or a tree of drafted tokens) over everything their sequence
+ * holds: O = softmax(softmax_scale * Q K^T) V per query head, where the keys of new token i of sequence b are
+ *   - the kv_len[b] compressed tokens in the sequence's pages: K_hat and V_hat of Eq. 7, not rounded in between,
+ *   - the tail_len[b] tokens of its tail,
+ *   - the new tokens j < nodes[b] that the mask's row i names.
+ * Rows i >= nodes[b] and rows that see no token at all get a zero output row and lse = -infinity.
+ * A new token that no row sees may hold anything (also what is no number); every other value must be finite, keys, values
+ * and decoded values of magnitude up to 65504.
+ *   k_*, v_*  the K and the V pool, [n_heads] units each, layout of a cache of pool_pages * page_len tokens per unit
+ *   scratch   optional, 16-byte aligned: with qvg_attn_tree_scratch_bytes bytes the sequences' tokens are dealt to several
+ *             workgroups per KV head and one more launch joins their partial results.  NULL or less: one workgroup per
+ *             sequence, KV head and 64 query rows, whose result differs by the order of fp32 sums.  Equal calls give equal bits.
+ *             Contents are scratch: nothing has to be initialised and nothing survives the call.
+ * What is rounded: queries, keys, values and probabilities enter the two contractions as binary16 (queries scaled by a power
+ * of two per row, probabilities by one per row and workgroup); scores, normaliser and output are accumulated in fp32.
+ */
+int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t,
+                  const void *k_centroids, const uint8_t *k_ids, const uint8_t *k_codes, const void *k_scales,
+                  const void *v_centroids, const uint8_t *v_ids, const uint8_t *v_codes, const void *v_scales,
+                  float softmax_scale, void *scratch, size_t scratch_bytes, void *stream);
+
+/* Bytes of scratch that let qvg_attn_tree divide a call of these sizes (from n_seqs, group, n_nodes, table_pages, page_len and
+ * tail_capacity; the pointers are not looked at); 0 when it would not be divided. */
+int qvg_attn_tree_scratch_bytes(const qvg_params *p, const qvg_tree_step *t, size_t *out);
+
+/*
+ * Masks of draft trees from their parents, as qvg_attn_tree reads them, and the nodes' depths.
+ *   parents    [n_seqs][n_nodes] int32: the parent of node i, below i; -1: the node follows the sequence's last token.
+ *              Any other value, or i >= nodes[b], makes the node a hole: no node sees it, it sees no node, and neither does
+ *              any node below it.
+ *   nodes      [n_seqs] int32 or NULL
+ *   mask_out   [n_seqs][n_nodes][ceil(n_nodes / 32)]: node i sees itself and its ancestors
+ *   depth_out  [n_seqs][n_nodes] int32 or NULL: number of ancestors (the token's place is the sequence's length + depth);
+ *              -1 for a hole
+ * n_nodes in 0 .. 1024.
+ */
+int qvg_tree_mask(int64_t n_seqs, int64_t n_nodes, const int32_t *parents, const int32_t *nodes, uint32_t *mask_out,
+                  int32_t *depth_out, void *stream);
+
+/*
+ * Append the K and V of the new tokens that are kept (the accepted path of a draft tree) to the tails:
+ *   tail[b][.][tail_len[b] + i] = new[b][.][path[b][i]],  i < n_keep[b],   tail_len_out[b] = tail_len[b] + n_keep[b].
+ *   path [n_seqs][n_path] int32, n_keep [n_seqs] (clamped to 0 .. n_path) int32, device.  A path entry outside
+ *   0 .. n_nodes - 1 leaves its row of the tail as it was, and so does a row beyond tail_capacity; tail_len_out (may be
+ *   tail_len, or NULL) is clamped to tail_capacity.  Views as in qvg_tree_step; the tails must not overlap k_new or v_new.
+ */
+int qvg_keep_nodes(int32_t n_heads, int32_t head_dim, int64_t n_seqs, int64_t n_nodes, const void *k_new, const void *v_new,
+                   int64_t new_stride_seq, int64_t new_stride_head, int64_t new_stride_node,
+                   const int32_t *path, int64_t n_path, const int32_t *n_keep,
+                   void *k_tail, void *v_tail, int64_t tail_stride_seq, int64_t tail_stride_head, int64_t tail_stride_token,
+                   int64_t tail_capacity, const int32_t *tail_len, int32_t *tail_len_out, void *stream);
+
+/*
+ * Copy whole pages, all arrays of all n_heads units: page src[i] of one pool becomes page dst[i] of another of the same
+ * parameters and page_len, or of the same one (compaction of a pool; gathering a sequence's pages into consecutive ones,
+ * which qvg_decode and qvg_attn_decode read).  src and dst are HOST arrays, read before the call returns.  QVG_ERR_BAD_PARAM
+ * for a page outside its pool, a destination named twice, and, within one pool (the same codes pointer), a destination that
+ * is also a source: the pairs are copied in no particular order.  Different pools must not overlap.
+ */
+int qvg_copy_pages(const qvg_params *p, int64_t page_len, int64_t n_pairs, const int32_t *src, const int32_t *dst,
+                   int64_t src_pool_pages, const void *src_centroids, const uint8_t *src_ids, const uint8_t *src_codes,
+                   const void *src_scales,
+                   int64_t dst_pool_pages, void *dst_centroids, uint8_t *dst_ids, uint8_t *dst_codes, void *dst_scales,
+                   void *stream);
+
+/*
  * The two k-means steps on their own (Sec. 4.1), as the encoder runs them.
  * assign: ids_out[h][n] = index of the nearest centroid of unit h; workspace
  *         qvg_workspace_bytes(p, QVG_ENTRY_KMEANS_ASSIGN, N, 0) bytes.

@@ -24,6 +24,7 @@ SCALE_F16, SCALE_E4M3 = 0, 1
 EXPORTS = ["qvg_encode_chunk", "qvg_encode_chunk_static", "qvg_decode", "qvg_decode_ex", "qvg_attn_decode", "qvg_attn_decode_ex",
            "qvg_attn_decode_causal", "qvg_attn_decode_f32", "qvg_attn_decode_parts", "qvg_attn_scratch_bytes", "qvg_attn_scratch_bytes_causal",
            "qvg_attn_merge",
+           "qvg_attn_tree", "qvg_attn_tree_scratch_bytes", "qvg_tree_mask", "qvg_keep_nodes", "qvg_copy_pages",
            "qvg_kmeans_assign",
            "qvg_kmeans_update", "qvg_workspace_bytes", "qvg_compressed_bytes",
            "qvg_status_string", "qvg_version"]
@@ -33,6 +34,20 @@ class QvgParams(C.Structure):
     _fields_ = [("n_heads", C.c_int32), ("head_dim", C.c_int32), ("n_clusters", C.c_int32),
                 ("group_size", C.c_int32), ("n_stages", C.c_int32), ("bits", C.c_int32),
                 ("n_smooth_stages", C.c_int32), ("kmeans_iters", C.c_int32), ("scale_format", C.c_int32)]
+
+
+class QvgTreeStep(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("group", C.c_int32), ("n_nodes", C.c_int32), ("table_pages", C.c_int32),
+                ("page_len", C.c_int64), ("pool_pages", C.c_int64), ("page_table", C.c_void_p), ("kv_len", C.c_void_p),
+                ("q", C.c_void_p), ("q_stride_seq", C.c_int64), ("q_stride_head", C.c_int64), ("q_stride_node", C.c_int64),
+                ("k_new", C.c_void_p), ("v_new", C.c_void_p),
+                ("new_stride_seq", C.c_int64), ("new_stride_head", C.c_int64), ("new_stride_node", C.c_int64),
+                ("k_tail", C.c_void_p), ("v_tail", C.c_void_p),
+                ("tail_stride_seq", C.c_int64), ("tail_stride_head", C.c_int64), ("tail_stride_token", C.c_int64),
+                ("tail_len", C.c_void_p), ("tail_capacity", C.c_int32), ("reserved", C.c_int32),
+                ("nodes", C.c_void_p), ("mask", C.c_void_p), ("k_rope_f16", C.c_void_p), ("rope_tokens", C.c_int64),
+                ("out", C.c_void_p), ("out_stride_seq", C.c_int64), ("out_stride_head", C.c_int64), ("out_stride_node", C.c_int64),
+                ("lse", C.c_void_p)]
 
 
 class QvgError(RuntimeError):
@@ -82,6 +97,19 @@ def lib():
         L.qvg_attn_scratch_bytes_causal.argtypes = L.qvg_attn_scratch_bytes.argtypes
         L.qvg_attn_merge.restype = C.c_int
         L.qvg_attn_merge.argtypes = [i64, C.c_int32, vp, vp, vp, vp, vp, vp, vp]
+        pt = C.POINTER(QvgTreeStep)
+        L.qvg_attn_tree.restype = C.c_int
+        L.qvg_attn_tree.argtypes = [pp, pt, vp, u8p, u8p, vp, vp, u8p, u8p, vp, C.c_float, vp, C.c_size_t, vp]
+        L.qvg_attn_tree_scratch_bytes.restype = C.c_int
+        L.qvg_attn_tree_scratch_bytes.argtypes = [pp, pt, C.POINTER(C.c_size_t)]
+        L.qvg_tree_mask.restype = C.c_int
+        L.qvg_tree_mask.argtypes = [i64, i64, vp, vp, vp, vp, vp]
+        L.qvg_keep_nodes.restype = C.c_int
+        L.qvg_keep_nodes.argtypes = [C.c_int32, C.c_int32, i64, i64, vp, vp, i64, i64, i64, vp, i64, vp, vp, vp, i64, i64, i64,
+                                     i64, vp, vp, vp]
+        L.qvg_copy_pages.restype = C.c_int
+        L.qvg_copy_pages.argtypes = [pp, i64, i64, C.POINTER(C.c_int32), C.POINTER(C.c_int32), i64, vp, u8p, u8p, vp,
+                                     i64, vp, u8p, u8p, vp, vp]
         L.qvg_kmeans_assign.restype = C.c_int
         L.qvg_kmeans_assign.argtypes = [pp, i64, vp, i64, i64, vp, u8p, vp, C.c_size_t, vp]
         L.qvg_kmeans_update.restype = C.c_int
@@ -428,6 +456,206 @@ def attn_merge(out_a, lse_a, out_b, lse_b, out=None, want_lse=False):
     return (out, lse) if want_lse else out
 
 
+def _rows4(x, name, shape=None):
+    """[B, H, N, d] bf16 view with a contiguous last dim -> its three strides (those of one element are 0: they are not used,
+    and a view may hold anything there)."""
+    _check(x, torch.bfloat16, name)
+    if x.dim() != 4 or (x.stride(3) != 1 and x.shape[3] != 1) or (shape is not None and tuple(x.shape) != tuple(shape)):
+        raise ValueError(f"{name}: need bf16 {'[B, H, N, d]' if shape is None else list(shape)} with unit stride along d")
+    return tuple(0 if n == 1 else s for n, s in zip(x.shape[:3], x.stride()[:3]))
+
+
+def _ints(t, shape, name):
+    _check(t, torch.int32, name)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous int32 tensor of shape {list(shape)}")
+    return t.data_ptr()
+
+
+def _here(*tensors):
+    """All tensors of a call are on the current device: its stream is the one the call goes to."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _check_pool(e: Encoded, name):
+    """The arrays of a pool agree with each other: whole pages, a set of tables to each."""
+    units, tokens = e.ids.shape[:2]
+    S, L = e.n_smooth, e.chunk_len
+    if tokens % L or tokens < L:
+        raise ValueError(f"{name}: the pool must hold whole pages of {L} tokens")
+    if (e.codes.shape[:2] != (units, tokens) or e.scales.shape[:2] != (units, tokens) or e.scales.shape[2] != e.codes.shape[2] or
+            e.centroids.shape[:2] != (units, tokens // L) or e.centroids.dim() != (4 if S == 1 else 5) or
+            (S > 1 and (e.centroids.shape[2] != S or tuple(e.ids.shape[2:]) != (S,)))):
+        raise ValueError(f"{name}: the pool's arrays are of different sizes")
+    _check_stored(e.centroids, e.ids, e.codes, e.scales, e.centroids.shape[-2])
+
+
+@functools.lru_cache(maxsize=256)
+def _tree_scratch_bytes(H, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity) -> int:
+    """Bytes of scratch of an attn_tree of these sizes (a function of its arguments alone)."""
+    need = C.c_size_t()
+    t = QvgTreeStep(n_seqs=n_seqs, group=group, n_nodes=n_nodes, table_pages=table_pages, page_len=page_len, pool_pages=1,
+                    tail_capacity=tail_capacity)
+    st = lib().qvg_attn_tree_scratch_bytes(make_params(H, 2, 128, 1), C.byref(t), C.byref(need))
+    if st != 0:
+        raise QvgError(st, "qvg_attn_tree_scratch_bytes")
+    return need.value
+
+
+def tree_mask(parents, n_nodes=None, mask=None, depth=None):
+    """qvg_tree_mask.  parents [B, N] int32 (the parent of node i, below i; -1: none) -> (mask [B, N, ceil(N / 32)] int32,
+    depth [B, N] int32).  n_nodes [B] int32: a tree's nodes, all N without.  Nodes behind them, and those with another
+    parent than allowed, are holes: an empty row, depth -1."""
+    _check(parents, torch.int32, "parents")
+    if parents.dim() != 2 or not parents.is_contiguous():
+        raise ValueError("parents: need a contiguous [B, N] int32 tensor")
+    _here(parents, n_nodes, mask, depth)
+    n, m = parents.shape
+    words = -(-m // 32)
+    mask = torch.empty(n, m, words, dtype=torch.int32, device=parents.device) if mask is None else mask
+    depth = torch.empty(n, m, dtype=torch.int32, device=parents.device) if depth is None else depth
+    st = lib().qvg_tree_mask(n, m, parents.data_ptr(), None if n_nodes is None else _ints(n_nodes, (n,), "n_nodes"),
+                             _ints(mask, (n, m, words), "mask"), _ints(depth, (n, m), "depth"), _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_tree_mask")
+    return mask, depth
+
+
+def attn_tree(q, k: Encoded, v: Encoded, page_table, kv_len, k_new, v_new, tail_k=None, tail_v=None, tail_len=None, n_nodes=None,
+              mask=None, softmax_scale=None, k_rope=None, want_lse=False, out=None, scratch=None):
+    """qvg_attn_tree: attention of the new tokens of B sequences over their compressed pages, their bf16 tails and each other.
+    q [B, H * group, N, d] bf16 -> out [B, H * group, N, d] (and lse fp32 [B, H * group, N]); query head h reads KV head
+    h // group.
+    k, v: the pools, [H] units of pages of chunk_len tokens (alloc_cache, filled by encode_chunk: chunk_index is the page);
+    page_table [B, P] int32, kv_len [B] int32: the sequences' pages and how many tokens they hold (page_table None: none);
+    k_new, v_new [B, H, N, d] bf16: the new tokens' own K and V; n_nodes [B] int32: how many there are (None: N);
+    mask [B, N, ceil(N / 32)] int32 (tree_mask): which new tokens a new token sees (None: itself and those before it);
+    tail_k, tail_v [B, H, R, d] bf16, tail_len [B] int32: tokens that are in no page yet;
+    k_rope [n, d/2, 2] float16: rotary embedding of the compressed keys by their place in the sequence.
+    Views may be strided (multiples of 8 elements, unit stride along d); K and V views share their strides.  Rows behind
+    n_nodes, and those that see nothing, are zero with lse -inf.
+    scratch: uint8 tensor of attn_tree_scratch bytes for dividing the call over the chip; without one it is taken from torch's
+    allocator (where that has no memory left the call runs undivided, which differs by the order of fp32 sums)."""
+    if (v.ids.shape, v.codes.shape, v.scales.shape, v.scales.dtype, v.centroids.shape, v.chunk_len, v.n_smooth) != \
+            (k.ids.shape, k.codes.shape, k.scales.shape, k.scales.dtype, k.centroids.shape, k.chunk_len, k.n_smooth):
+        raise ValueError("K and V pools must share shapes and parameters")
+    _check_pool(k, "k")
+    _check_pool(v, "v")
+    return _attn_tree(q, k, (k.centroids.data_ptr(), k.ids.data_ptr(), k.codes.data_ptr(), k.scales.data_ptr()),
+                      (v.centroids.data_ptr(), v.ids.data_ptr(), v.codes.data_ptr(), v.scales.data_ptr()), k.ids.shape[0], page_table,
+                      kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
+
+
+def attn_tree_scratch(heads, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity, device) -> torch.Tensor:
+    """Scratch for an attn_tree of these sizes."""
+    return torch.empty(_tree_scratch_bytes(heads, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity),
+                       dtype=torch.uint8, device=device)
+
+
+def _attn_tree(q, k: Encoded, kp, vp, H, page_table, kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask,
+               softmax_scale, k_rope, want_lse, out, scratch):
+    """attn_tree on the pointers kp and vp (centroids, ids, codes, scales of the two pools) of H units each; sizes and formats
+    are those of k."""
+    qs = _rows4(q, "q")
+    n, hq, m, d = q.shape
+    if hq < H or hq % H:
+        raise ValueError("q: the number of query heads must be a multiple of the KV heads'")
+    K = k.centroids.shape[-2]
+    T, code_bytes = k.codes.shape[2:]
+    L, pool_tokens = k.chunk_len, k.ids.shape[1]
+    ns = _rows4(k_new, "k_new", (n, H, m, d))
+    if _rows4(v_new, "v_new", (n, H, m, d)) != ns:
+        raise ValueError("k_new and v_new must share their strides")
+    t = QvgTreeStep(n_seqs=n, group=hq // H, n_nodes=m, page_len=L, pool_pages=max(1, pool_tokens // L))
+    _here(q, k.ids, k_new, v_new, page_table, kv_len, tail_k, tail_v, tail_len, n_nodes, mask, k_rope, out, scratch)
+    if page_table is not None and page_table.shape[-1] > 0:
+        t.table_pages = page_table.shape[-1]
+        t.page_table = _ints(page_table, (n, t.table_pages), "page_table")
+        t.kv_len = _ints(kv_len, (n,), "kv_len")
+        if k_rope is not None:
+            _check(k_rope, torch.float16, "k_rope")
+            if k_rope.dim() != 3 or tuple(k_rope.shape[1:]) != (d // 2, 2) or not k_rope.is_contiguous() or k_rope.shape[0] < 1:
+                raise ValueError("k_rope: need a contiguous [n, d/2, 2] float16 tensor")
+            t.k_rope_f16, t.rope_tokens = k_rope.data_ptr(), k_rope.shape[0]
+    t.q, (t.q_stride_seq, t.q_stride_head, t.q_stride_node) = q.data_ptr(), qs
+    t.k_new, t.v_new, (t.new_stride_seq, t.new_stride_head, t.new_stride_node) = k_new.data_ptr(), v_new.data_ptr(), ns
+    if tail_k is not None and tail_k.shape[2] > 0:
+        if tail_v is None or tail_len is None:
+            raise ValueError("tail_k needs tail_v and tail_len")
+        R = tail_k.shape[2]
+        ts = _rows4(tail_k, "tail_k", (n, H, R, d))
+        if _rows4(tail_v, "tail_v", (n, H, R, d)) != ts:
+            raise ValueError("tail_k and tail_v must share their strides")
+        t.k_tail, t.v_tail, (t.tail_stride_seq, t.tail_stride_head, t.tail_stride_token) = tail_k.data_ptr(), tail_v.data_ptr(), ts
+        t.tail_len, t.tail_capacity = _ints(tail_len, (n,), "tail_len"), R
+    if n_nodes is not None:
+        t.nodes = _ints(n_nodes, (n,), "n_nodes")
+    if mask is not None:
+        t.mask = _ints(mask, (n, m, -(-m // 32)), "mask")
+    if out is None:
+        out = torch.empty(n, hq, m, d, dtype=torch.bfloat16, device=q.device)
+    t.out, (t.out_stride_seq, t.out_stride_head, t.out_stride_node) = out.data_ptr(), _rows4(out, "out", (n, hq, m, d))
+    lse = torch.empty(n, hq, m, dtype=torch.float32, device=q.device) if want_lse else None
+    t.lse = _ptr(lse)
+    if scratch is None:
+        scratch = _scratch(_tree_scratch_bytes(H, n, hq // H, m, t.table_pages, L, t.tail_capacity), q.device)
+    p = QvgParams(H, d, K, d // k.scales.shape[3], T, code_bytes * 8 // d, k.n_smooth, 0, k.scale_format)
+    st = lib().qvg_attn_tree(p, C.byref(t), *kp, *vp, 1.0 / (d ** 0.5) if softmax_scale is None else softmax_scale,
+                             _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_attn_tree")
+    return (out, lse) if want_lse else out
+
+
+def keep_nodes(k_new, v_new, path, n_keep, tail_k, tail_v, tail_len, out_len=None) -> torch.Tensor:
+    """qvg_keep_nodes: the K and V of the kept new tokens go behind the tails.  k_new, v_new [B, H, N, d] bf16; path [B, M] int32:
+    the kept tokens' indices in order, n_keep [B] int32 how many; tail_k, tail_v [B, H, R, d] bf16 (written in place),
+    tail_len [B] int32.  Returns the new lengths [B] int32 (out_len, which may be tail_len itself, or a new tensor)."""
+    ns = _rows4(k_new, "k_new")
+    n, H, m, d = k_new.shape
+    ts = _rows4(tail_k, "tail_k", (n, H, tail_k.shape[2], d)) if tail_k.dim() == 4 else _rows4(tail_k, "tail_k")
+    if _rows4(v_new, "v_new", k_new.shape) != ns or _rows4(tail_v, "tail_v", tail_k.shape) != ts:
+        raise ValueError("K and V views must share their strides")
+    if path.dim() != 2:
+        raise ValueError("path: need [B, M]")
+    _here(k_new, v_new, path, n_keep, tail_k, tail_v, tail_len, out_len)
+    out_len = torch.empty_like(tail_len) if out_len is None else out_len
+    st = lib().qvg_keep_nodes(H, d, n, m, k_new.data_ptr(), v_new.data_ptr(), *ns, _ints(path, (n, path.shape[1]), "path"), path.shape[1],
+                              _ints(n_keep, (n,), "n_keep"), tail_k.data_ptr(), tail_v.data_ptr(), *ts, tail_k.shape[2],
+                              _ints(tail_len, (n,), "tail_len"), _ints(out_len, (n,), "out_len"), _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_keep_nodes")
+    return out_len
+
+
+def copy_pages(cache: Encoded, src, dst, into: Encoded | None = None) -> Encoded:
+    """qvg_copy_pages: page src[i] of every unit of the pool `cache` becomes page dst[i] of the pool `into` (the same one
+    without).  src, dst: sequences of Python integers; no destination twice, and none that is a source in the same pool."""
+    into = cache if into is None else into
+    K, d = cache.centroids.shape[-2:]
+    if (into.chunk_len, into.n_smooth, into.ids.shape[0], into.codes.shape[2:], into.scales.shape[2:], into.scales.dtype,
+            into.centroids.shape[2:]) != (cache.chunk_len, cache.n_smooth, cache.ids.shape[0], cache.codes.shape[2:],
+                                          cache.scales.shape[2:], cache.scales.dtype, cache.centroids.shape[2:]):
+        raise ValueError("the pools were allocated for different parameters")
+    if len(src) != len(dst):
+        raise ValueError("src and dst must have the same length")
+    L = cache.chunk_len
+    _check_pool(cache, "cache")
+    _check_pool(into, "into")
+    _here(cache.ids, into.ids)
+    T, code_bytes = cache.codes.shape[2:]
+    p = QvgParams(cache.ids.shape[0], d, K, d // cache.scales.shape[3], T, code_bytes * 8 // d, cache.n_smooth, 0, cache.scale_format)
+    ints = C.c_int32 * len(src)
+    ptrs = [(c.ids.shape[1] // L, c.centroids.data_ptr(), c.ids.data_ptr(), c.codes.data_ptr(), c.scales.data_ptr()) for c in (cache, into)]
+    st = lib().qvg_copy_pages(p, L, len(src), ints(*src), ints(*dst), *ptrs[0], *ptrs[1], _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_copy_pages")
+    return into
+
+
 def kmeans_assign(x, centroids) -> torch.Tensor:
     """qvg_kmeans_assign -> ids [H, N], uint8 (int16 with more than 256 centroids)."""
     sh, st_ = _view3(x, "x")
@@ -554,3 +782,182 @@ class StreamingCache:
         chunks = -(-self.n_tokens // self.chunk_len)
         table = c.n_smooth * c.centroids.shape[-2] * c.centroids.shape[-1] * 2
         return 2 * self.heads * (self.n_tokens * per_tok + chunks * table)
+
+
+class PagedCache:
+    """The compressed K and V caches of one layer of up to `max_seqs` sequences over one pool of `n_pages` pages of page_len
+    tokens (K heads, then V heads, as 2 * heads units).  A sequence's tokens go into a bf16 tail first and, whenever page_len
+    of them are there, through the encoder into a page of their own (k-means started from the sequence's page before, Sec. 4.3;
+    from `init` [2 * heads, K, d] or [2 * heads, S, K, d] for its first).  Pages never change once they are written, so `fork`
+    shares them and copies the tail only; `close` gives back those that no other sequence holds; `compact` moves the used ones
+    to the pool's front.  A step attends with a row of new tokens for every place 0 .. max_seqs - 1 (places that are not open
+    have none) and then keeps those that were accepted.
+    Argument marshalling and page numbers only: every step runs in the library's kernels."""
+
+    def __init__(self, heads, max_seqs, n_pages, page_len, max_pages, max_new, n_clusters, group_size, n_stages, init, head_dim=128,
+                 device="cuda", n_smooth=1, bits=2, scale_format=SCALE_F16, warm_iters=3, cold_iters=10):
+        self.heads, self.page_len, self.max_new = heads, page_len, max_new
+        self.group_size, self.n_stages = group_size, n_stages
+        self.init, self.warm_iters, self.cold_iters = init, warm_iters, cold_iters
+        self.pool = alloc_cache(2 * heads, n_pages * page_len, page_len, n_clusters, group_size, n_stages, head_dim, device,
+                                n_smooth=n_smooth, bits=bits, scale_format=scale_format)
+        self.tail = torch.empty(max_seqs, 2 * heads, page_len + max_new, head_dim, dtype=torch.bfloat16, device=device)
+        self.table = torch.zeros(max_seqs, max_pages, dtype=torch.int32, device=device)
+        self.kv_len = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+        self.tail_len = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+        self.pages = [None] * max_seqs                 # a sequence's pages in order; None: the place is not open
+        self.tails = [0] * max_seqs                    # tokens in the tail, as on the device
+        self.holders = [0] * n_pages                   # sequences that hold a page
+        p = make_params(2 * heads, n_clusters, group_size, n_stages, max(warm_iters, cold_iters), head_dim=head_dim, bits=bits,
+                        n_smooth_stages=n_smooth, scale_format=scale_format)
+        self._ws = torch.empty(max(workspace_bytes(p, ENTRY_ENCODE, page_len), 16), dtype=torch.uint8, device=device)
+
+    def free_pages(self) -> int:
+        return self.holders.count(0)
+
+    def length(self, seq) -> int:
+        return len(self._open(seq)) * self.page_len + self.tails[seq]
+
+    def _open(self, seq):
+        if not 0 <= seq < len(self.pages) or self.pages[seq] is None:
+            raise ValueError(f"sequence {seq} is not open")
+        return self.pages[seq]
+
+    def _place(self):
+        if None not in self.pages:
+            raise ValueError("all places are taken")
+        return self.pages.index(None)
+
+    def _tell(self, seq):
+        """The device's copy of a sequence's pages and lengths."""
+        pages = self.pages[seq] or []
+        if pages:
+            self.table[seq, :len(pages)] = torch.tensor(pages, dtype=torch.int32)
+        self.kv_len[seq], self.tail_len[seq] = len(pages) * self.page_len, self.tails[seq]
+
+    def open(self) -> int:
+        """A new, empty sequence; returns its place."""
+        seq = self._place()
+        self.pages[seq], self.tails[seq] = [], 0
+        self._tell(seq)
+        return seq
+
+    def fork(self, seq) -> int:
+        """A copy of a sequence: its pages are shared, its tail is copied."""
+        pages, to = self._open(seq), self._place()
+        for page in pages:
+            self.holders[page] += 1
+        self.pages[to], self.tails[to] = list(pages), self.tails[seq]
+        self.tail[to, :, :self.tails[seq]].copy_(self.tail[seq, :, :self.tails[seq]])
+        self._tell(to)
+        return to
+
+    def close(self, seq):
+        """End a sequence; pages that no other one holds are free again."""
+        for page in self._open(seq):
+            self.holders[page] -= 1
+        self.pages[seq], self.tails[seq] = None, 0
+        self._tell(seq)
+
+    def _need(self, tokens_of):
+        """Refuses what the pool or a table has no room for, before anything is changed: {sequence: tokens to come}."""
+        more = 0
+        for seq, n in tokens_of.items():
+            new = (self.tails[seq] + n) // self.page_len
+            if len(self._open(seq)) + new > self.table.shape[1]:
+                raise ValueError(f"sequence {seq} would have more than {self.table.shape[1]} pages")
+            more += new
+        if more > self.free_pages():
+            raise ValueError(f"{more} pages are needed, {self.free_pages()} are free")
+
+    def _encode(self, seq, x):
+        """One full page of a sequence, x [2 * heads, page_len, d]."""
+        pages, page = self.pages[seq], self.holders.index(0)
+        init = self.pool.centroids[:, pages[-1]] if pages else self.init
+        encode_chunk(x, init, self.group_size, self.n_stages, self.warm_iters if pages else self.cold_iters, cache=self.pool,
+                     chunk_index=page, workspace=self._ws)
+        self.holders[page] = 1
+        pages.append(page)
+
+    def _seal(self, seq):
+        """Full pages leave the tail."""
+        L, n = self.page_len, self.tails[seq]
+        full = n // L * L
+        for at in range(0, full, L):
+            self._encode(seq, self.tail[seq, :, at:at + L])
+        if full and n > full:
+            self.tail[seq, :, :n - full].copy_(self.tail[seq, :, full:n].clone())
+        self.tails[seq] = n - full
+        if full:
+            self._tell(seq)
+
+    def append(self, seq, kv):
+        """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence."""
+        n, L = kv.shape[1], self.page_len
+        self._need({seq: n})
+        at = 0
+        if self.tails[seq] == 0:                       # whole pages need no way through the tail
+            while n - at >= L:
+                self._encode(seq, kv[:, at:at + L])
+                at += L
+        while at < n:
+            m = min(n - at, L - self.tails[seq])
+            self.tail[seq, :, self.tails[seq]:self.tails[seq] + m].copy_(kv[:, at:at + m])
+            self.tails[seq] += m
+            at += m
+            self._seal(seq)
+        self._tell(seq)
+
+    def attend(self, q, k_new, v_new, n_nodes=None, mask=None, k_rope=None, softmax_scale=None, want_lse=False, out=None,
+               scratch=None):
+        """attn_tree of q [max_seqs, heads * group, N, d] over the sequences and the new tokens k_new, v_new
+        [max_seqs, heads, N, d].  n_nodes [max_seqs] int32: a place's new tokens (None: all N; pass 0 for places that are not
+        open, or ignore their rows)."""
+        c, h = self.pool, self.heads
+        kp = (c.centroids.data_ptr(), c.ids.data_ptr(), c.codes.data_ptr(), c.scales.data_ptr())
+        vp = (kp[0] + h * c.centroids.stride(0) * 2, kp[1] + h * c.ids.stride(0) * c.ids.element_size(),
+              kp[2] + h * c.codes.stride(0), kp[3] + h * c.scales.stride(0) * c.scales.element_size())
+        return _attn_tree(q, c, kp, vp, h, self.table, self.kv_len, k_new, v_new, self.tail[:, :h], self.tail[:, h:], self.tail_len,
+                          n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
+
+    def keep(self, k_new, v_new, path, n_keep):
+        """Accepted new tokens become part of the sequences: path [max_seqs, M] int32 on the device (M <= max_new), the indices of
+        the kept ones in order; n_keep: how many of each, max_seqs Python integers."""
+        n_keep = [int(n) for n in n_keep]
+        if len(n_keep) != len(self.pages) or path.shape[1] > self.max_new or any(not 0 <= n <= path.shape[1] for n in n_keep):
+            raise ValueError(f"n_keep: need {len(self.pages)} counts of at most {min(path.shape[1], self.max_new)} tokens")
+        kept = {s: n for s, n in enumerate(n_keep) if n}
+        self._need(kept)
+        h = self.heads
+        keep_nodes(k_new, v_new, path, torch.tensor(n_keep, dtype=torch.int32, device=path.device), self.tail[:, :h],
+                   self.tail[:, h:], self.tail_len, out_len=self.tail_len)
+        for seq, n in kept.items():
+            self.tails[seq] += n
+            self._seal(seq)
+
+    def compact(self) -> int:
+        """Moves the used pages to the pool's front and returns how many there are."""
+        used = [i for i, n in enumerate(self.holders) if n]
+        holes = [i for i in range(len(used)) if not self.holders[i]]
+        moved = dict(zip([i for i in used if i >= len(used)], holes))
+        if moved:
+            copy_pages(self.pool, list(moved), list(moved.values()))
+            for a, b in moved.items():
+                self.holders[a], self.holders[b] = 0, self.holders[a]
+            for seq, pages in enumerate(self.pages):
+                if pages and any(p in moved for p in pages):
+                    self.pages[seq] = [moved.get(p, p) for p in pages]
+                    self._tell(seq)
+        return len(used)
+
+    def gather(self, seq, into: Encoded | None = None) -> Encoded:
+        """A sequence's pages one behind the other in a cache of their own (`into`, or a new one), as decode and attn_decode
+        read it.  Units: K heads, then V heads."""
+        pages, c = self._open(seq), self.pool
+        if not pages:
+            raise ValueError("the sequence has no full page yet")
+        if into is None:
+            d = c.centroids.shape[-1]
+            into = alloc_cache(2 * self.heads, len(pages) * self.page_len, self.page_len, c.centroids.shape[-2], self.group_size,
+                               self.n_stages, d, c.ids.device, n_smooth=c.n_smooth, bits=c.bits, scale_format=c.scale_format)
+        return copy_pages(c, pages, list(range(len(pages))), into=into)

@@ -4,9 +4,11 @@
 #include <stdint.h>
 
 #include <mutex>
+#include <new>
 
 #include "qvg.h"
 #include "qvg_internal.hpp"
+#include "qvg_tree.hpp"
 
 using namespace qvg;
 
@@ -631,6 +633,170 @@ int qvg_attn_decode_f32(const qvg_params *p, int64_t n_q, const void *q, int64_t
     return attn_call(p, n_q, q, n_kv_tokens, chunk_len, kv_capacity_tokens, k_centroids, k_ids, k_codes, k_scales,
                      v_centroids, v_ids, v_codes, v_scales, k_rope, q_kv_len, softmax_scale, nullptr, out_f32, lse_out,
                      nullptr, 0, nullptr, 0, stream);
+}
+
+}  // extern "C"
+
+// ---- paged caches -----------------------------------------------------------------------------
+namespace {
+
+// a bf16 view of rows of 128 elements whose strides (in elements) keep every row 16-byte aligned
+bool rows_aligned(const void *base, int64_t seq, int64_t head, int64_t row) {
+    return aligned16(base) && ((seq | head | row) & 7) == 0;
+}
+constexpr int64_t kMaxInt = 0x7fffffff;
+
+// the sizes of a step (not its pointers)
+int check_step_sizes(const qvg_params *p, const qvg_tree_step *t) {
+    if (!t) return QVG_ERR_NULL;
+    if (t->n_seqs < 0 || t->n_seqs > 65535 || t->group < 1 || t->n_nodes < 0 || t->table_pages < 0 || t->tail_capacity < 0 || t->reserved != 0)
+        return QVG_ERR_BAD_PARAM;
+    if ((int64_t)t->group * t->n_nodes > (1 << 20)) return QVG_ERR_BAD_PARAM;
+    if (t->page_len < 1 || t->page_len > kMaxInt || t->pool_pages < 1 || t->pool_pages > kMaxInt) return QVG_ERR_BAD_PARAM;
+    if (t->table_pages > 0 && t->page_len > kMaxInt / t->table_pages) return QVG_ERR_BAD_PARAM;
+    // (tiles of 32 tokens, and blocks of query rows, are counted in 32 bits)
+    if (t->table_pages * ((t->page_len + 31) / 32) + (t->tail_capacity + 31) / 32 + (t->n_nodes + 31) / 32 > kMaxInt - 1024) return QVG_ERR_BAD_PARAM;
+    const int64_t rows = (int64_t)t->group * t->n_nodes, br = tree_block_rows(rows);
+    if ((int64_t)t->n_seqs * p->n_heads * ((rows + br - 1) / br) > (1 << 30)) return QVG_ERR_BAD_PARAM;
+    return QVG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qvg_attn_tree_scratch_bytes(const qvg_params *p, const qvg_tree_step *t, size_t *out) {
+    int st = check_params(p);
+    if (st != QVG_OK) return st;
+    if (!out) return QVG_ERR_NULL;
+    if ((st = check_step_sizes(p, t)) != QVG_OK) return st;
+    *out = tree_plan(p->n_heads, *t).state_bytes;
+    return QVG_OK;
+}
+
+int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t, const void *k_centroids, const uint8_t *k_ids,
+                  const uint8_t *k_codes, const void *k_scales, const void *v_centroids, const uint8_t *v_ids,
+                  const uint8_t *v_codes, const void *v_scales, float softmax_scale, void *scratch, size_t scratch_bytes,
+                  void *stream) {
+    int st = check_params(p);
+    if (st != QVG_OK) return st;
+    if ((st = check_step_sizes(p, t)) != QVG_OK) return st;
+    if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return QVG_ERR_BAD_PARAM;   // positive, finite
+    if (t->k_rope_f16 && t->table_pages > 0 && t->rope_tokens < 1) return QVG_ERR_BAD_PARAM;
+    if (t->n_seqs == 0 || t->n_nodes == 0) return QVG_OK;
+    if (!t->q || !t->out || !t->k_new || !t->v_new) return QVG_ERR_NULL;
+    if (t->table_pages > 0 && (!t->page_table || !t->kv_len || !k_centroids || !k_ids || !k_codes || !k_scales || !v_centroids ||
+                               !v_ids || !v_codes || !v_scales))
+        return QVG_ERR_NULL;
+    if (t->tail_capacity > 0 && (!t->k_tail || !t->v_tail || !t->tail_len)) return QVG_ERR_NULL;
+    if (!rows_aligned(t->q, t->q_stride_seq, t->q_stride_head, t->q_stride_node) ||
+        !rows_aligned(t->out, t->out_stride_seq, t->out_stride_head, t->out_stride_node) ||
+        !rows_aligned(t->k_new, t->new_stride_seq, t->new_stride_head, t->new_stride_node) || !aligned16(t->v_new))
+        return QVG_ERR_ALIGN;
+    if (t->tail_capacity > 0 && (!rows_aligned(t->k_tail, t->tail_stride_seq, t->tail_stride_head, t->tail_stride_token) || !aligned16(t->v_tail)))
+        return QVG_ERR_ALIGN;
+    if (t->table_pages > 0 && (!aligned16(k_centroids) || !aligned16(v_centroids) || !aligned16(k_codes) || !aligned16(v_codes) ||
+                               !scales_aligned(p, k_scales) || !scales_aligned(p, v_scales) || !ids_aligned(p, k_ids) || !ids_aligned(p, v_ids)))
+        return QVG_ERR_ALIGN;
+    if (!aligned16(t->k_rope_f16) || !aligned16(scratch)) return QVG_ERR_ALIGN;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(t->page_table) | reinterpret_cast<uintptr_t>(t->kv_len) | reinterpret_cast<uintptr_t>(t->tail_len) |
+                            reinterpret_cast<uintptr_t>(t->nodes) | reinterpret_cast<uintptr_t>(t->mask) | reinterpret_cast<uintptr_t>(t->lse);
+    if (words & 3u) return QVG_ERR_ALIGN;
+    TreeArgs a{};
+    a.k = PoolSide{static_cast<const bf16_t *>(k_centroids), k_ids, k_codes, static_cast<const uint8_t *>(k_scales)};
+    a.v = PoolSide{static_cast<const bf16_t *>(v_centroids), v_ids, v_codes, static_cast<const uint8_t *>(v_scales)};
+    a.H = p->n_heads; a.K = p->n_clusters; a.B = p->group_size; a.T = p->n_stages; a.S = p->n_smooth_stages;
+    a.fmt = format_of(p); a.id_wide = id_wide(p); a.t = *t; a.scale = softmax_scale;
+    const TreePlan plan = tree_plan(p->n_heads, *t);
+    a.row_blocks = plan.row_blocks;
+    a.parts = scratch && scratch_bytes >= plan.state_bytes ? plan.parts : 1;
+    a.state = static_cast<float *>(scratch);
+    return launch_attn_tree(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+int qvg_tree_mask(int64_t n_seqs, int64_t n_nodes, const int32_t *parents, const int32_t *nodes, uint32_t *mask_out,
+                  int32_t *depth_out, void *stream) {
+    if (n_seqs < 0 || n_seqs > kMaxInt || n_nodes < 0 || n_nodes > 1024) return QVG_ERR_BAD_PARAM;
+    if (n_seqs == 0 || n_nodes == 0) return QVG_OK;
+    if (!parents || !mask_out) return QVG_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(nodes) | reinterpret_cast<uintptr_t>(mask_out) |
+         reinterpret_cast<uintptr_t>(depth_out)) & 3u)
+        return QVG_ERR_ALIGN;
+    return launch_tree_mask((int)n_seqs, (int)n_nodes, parents, nodes, mask_out, depth_out, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+int qvg_keep_nodes(int32_t n_heads, int32_t head_dim, int64_t n_seqs, int64_t n_nodes, const void *k_new, const void *v_new,
+                   int64_t new_stride_seq, int64_t new_stride_head, int64_t new_stride_node, const int32_t *path, int64_t n_path,
+                   const int32_t *n_keep, void *k_tail, void *v_tail, int64_t tail_stride_seq, int64_t tail_stride_head,
+                   int64_t tail_stride_token, int64_t tail_capacity, const int32_t *tail_len, int32_t *tail_len_out, void *stream) {
+    if (n_heads < 1 || n_heads > 65535 || n_seqs < 0 || n_seqs > 65535 || n_nodes < 0 || n_nodes > (1 << 20) || n_path < 0 ||
+        n_path > (1 << 20) || tail_capacity < 0 || tail_capacity > kMaxInt)
+        return QVG_ERR_BAD_PARAM;
+    if (head_dim != kHeadDim) return QVG_ERR_UNSUPPORTED;
+    const int64_t blocks = (n_path + 15) / 16;
+    if (n_seqs * 2 * n_heads * blocks > kMaxInt) return QVG_ERR_BAD_PARAM;
+    if (n_seqs == 0) return QVG_OK;
+    if (!n_keep || !tail_len) return QVG_ERR_NULL;
+    const bool rows = n_path > 0 && n_nodes > 0 && tail_capacity > 0;
+    if (rows && (!k_new || !v_new || !path || !k_tail || !v_tail)) return QVG_ERR_NULL;
+    if (rows && (!rows_aligned(k_new, new_stride_seq, new_stride_head, new_stride_node) || !aligned16(v_new) ||
+                 !rows_aligned(k_tail, tail_stride_seq, tail_stride_head, tail_stride_token) || !aligned16(v_tail)))
+        return QVG_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(path) | reinterpret_cast<uintptr_t>(n_keep) | reinterpret_cast<uintptr_t>(tail_len) |
+         reinterpret_cast<uintptr_t>(tail_len_out)) & 3u)
+        return QVG_ERR_ALIGN;
+    KeepArgs a{};
+    a.k_new = static_cast<const bf16_t *>(k_new); a.v_new = static_cast<const bf16_t *>(v_new);
+    a.new_seq = new_stride_seq; a.new_head = new_stride_head; a.new_node = new_stride_node;
+    a.k_tail = static_cast<bf16_t *>(k_tail); a.v_tail = static_cast<bf16_t *>(v_tail);
+    a.tail_seq = tail_stride_seq; a.tail_head = tail_stride_head; a.tail_token = tail_stride_token;
+    a.path = path; a.keep = n_keep; a.tail_len = tail_len; a.tail_len_out = tail_len_out;
+    a.H = n_heads; a.n_seqs = (int)n_seqs; a.n_nodes = (int)n_nodes; a.n_path = (int)n_path; a.capacity = (int)tail_capacity;
+    a.blocks = rows ? (int)blocks : 0;
+    return launch_keep_nodes(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+int qvg_copy_pages(const qvg_params *p, int64_t page_len, int64_t n_pairs, const int32_t *src, const int32_t *dst,
+                   int64_t src_pool_pages, const void *src_centroids, const uint8_t *src_ids, const uint8_t *src_codes,
+                   const void *src_scales, int64_t dst_pool_pages, void *dst_centroids, uint8_t *dst_ids, uint8_t *dst_codes,
+                   void *dst_scales, void *stream) {
+    int st = check_params(p);
+    if (st != QVG_OK) return st;
+    if (page_len < 1 || page_len > kMaxInt || n_pairs < 0 || src_pool_pages < 0 || src_pool_pages > kMaxInt || dst_pool_pages < 0 ||
+        dst_pool_pages > kMaxInt)
+        return QVG_ERR_BAD_PARAM;
+    if (n_pairs == 0) return QVG_OK;
+    if (n_pairs > dst_pool_pages) return QVG_ERR_BAD_PARAM;              // some destination is named twice
+    if (!src || !dst || !src_centroids || !src_ids || !src_codes || !src_scales || !dst_centroids || !dst_ids || !dst_codes || !dst_scales)
+        return QVG_ERR_NULL;
+    if (!aligned16(src_centroids) || !aligned16(dst_centroids) || !aligned16(src_codes) || !aligned16(dst_codes) ||
+        !scales_aligned(p, src_scales) || !scales_aligned(p, dst_scales) || !ids_aligned(p, src_ids) || !ids_aligned(p, dst_ids))
+        return QVG_ERR_ALIGN;
+    {
+        const bool same = src_codes == dst_codes;
+        uint8_t *named = new (std::nothrow) uint8_t[(size_t)dst_pool_pages]();      // pages that are written
+        if (!named) return QVG_ERR_WORKSPACE;
+        bool ok = true;
+        for (int64_t i = 0; i < n_pairs && ok; ++i) {
+            ok = src[i] >= 0 && src[i] < src_pool_pages && dst[i] >= 0 && dst[i] < dst_pool_pages && !named[dst[i]];
+            if (ok) named[dst[i]] = 1;
+        }
+        for (int64_t i = 0; i < n_pairs && ok && same; ++i) ok = src[i] >= dst_pool_pages || !named[src[i]];
+        delete[] named;
+        if (!ok) return QVG_ERR_BAD_PARAM;
+    }
+    const int64_t table = (int64_t)p->n_smooth_stages * p->n_clusters * kHeadDim * (int64_t)sizeof(bf16_t);
+    const int64_t per_token[3] = {(int64_t)p->n_smooth_stages * (id_wide(p) ? 2 : 1), (int64_t)p->n_stages * (kHeadDim * p->bits / 8),
+                                  (int64_t)p->n_stages * (kHeadDim / p->group_size) * (p->scale_format == QVG_SCALE_E4M3 ? 1 : 2)};
+    const uint8_t *from[4] = {static_cast<const uint8_t *>(src_centroids), src_ids, src_codes, static_cast<const uint8_t *>(src_scales)};
+    uint8_t *to[4] = {static_cast<uint8_t *>(dst_centroids), dst_ids, dst_codes, static_cast<uint8_t *>(dst_scales)};
+    PageArray arrays[4];
+    for (int k = 0; k < 4; ++k) {
+        const int64_t bytes = k == 0 ? table : per_token[k - 1] * page_len;
+        arrays[k] = PageArray{from[k], to[k], bytes, bytes * src_pool_pages, bytes * dst_pool_pages};
+    }
+    return launch_copy_pages(arrays, p->n_heads, n_pairs, src, dst, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
 }
 
 }  // extern "C"

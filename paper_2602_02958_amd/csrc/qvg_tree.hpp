@@ -1,0 +1,45 @@
+// Arguments of the operators over paged caches (qvg_tree.hip: attention of a step's new tokens; qvg_pages.hip: tree
+// masks, kept tokens, page copies) and their launchers.
+#pragma once
+#include "qvg_internal.hpp"
+
+namespace qvg {
+
+struct PoolSide {                  // K or V pool: [H] units of pool_tokens tokens, pool_pages tables
+    const bf16_t *cent; const uint8_t *ids; const uint8_t *codes; const uint8_t *scales;
+};
+struct TreeArgs {
+    PoolSide k, v;
+    int H, K, B, T, S, fmt, id_wide;
+    qvg_tree_step t;
+    float scale;
+    int row_blocks, parts;         // 16 * RB query rows of a KV head to a block; workgroups that share a block's tokens
+    float *state;                  // partial results, parts > 1
+};
+// Rows of a KV head (group * n_nodes) are taken in blocks of 16, 32 or 64.
+inline int tree_block_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+struct TreePlan { int row_blocks, parts; size_t state_bytes; };
+TreePlan tree_plan(int H, const qvg_tree_step &t);
+hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s);
+
+hipError_t launch_tree_mask(int n_seqs, int n_nodes, const int32_t *parents, const int32_t *nodes, uint32_t *mask, int32_t *depth,
+                            hipStream_t s);
+
+struct KeepArgs {
+    const bf16_t *k_new, *v_new; int64_t new_seq, new_head, new_node;
+    bf16_t *k_tail, *v_tail; int64_t tail_seq, tail_head, tail_token;
+    const int32_t *path, *keep, *tail_len; int32_t *tail_len_out;
+    int H, n_seqs, n_nodes, n_path, capacity;
+    int blocks;                    // of 16 rows of a path
+};
+hipError_t launch_keep_nodes(const KeepArgs &a, hipStream_t s);
+
+struct PageArray {                 // one of a pool's four arrays
+    const uint8_t *src; uint8_t *dst;
+    int64_t bytes;                 // of a page
+    int64_t src_unit, dst_unit;    // bytes of a unit
+};
+hipError_t launch_copy_pages(const PageArray (&arrays)[4], int units, int64_t n_pairs, const int32_t *src, const int32_t *dst,
+                             hipStream_t s);
+
+}  // namespace qvg
