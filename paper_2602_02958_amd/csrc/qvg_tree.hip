@@ -123,6 +123,58 @@ __device__ __forceinline__ void store_row8(const TreeArgs &a, int b, int h, int6
 // A block's partial result: [rows][128] sums, then the rows' references, then their sums of weights.
 __host__ __device__ inline int64_t tree_state_floats(int rows) { return (int64_t)rows * (kHeadDim + 2); }
 
+// The wavefronts' results meet: O, m and l of each (m the same in a row's four lanes, l a lane's share), the block's result
+// to `state` or, undivided, to the output.  meet: [kTrWaves][16][kTrPitch] floats.
+template <int RB>
+__device__ __forceinline__ void finish_block(const TreeArgs &a, int b, int h, int bh, int rblk, int part, int nodes, float (*meet)[16][kTrPitch],
+                                             float (*ms)[16 * RB], float (*ls)[16 * RB], const floatx4_t (&O)[RB][8], const float (&m)[RB], float (&l)[RB]) {
+    constexpr int kRows = 16 * RB;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, kb = lane >> 4;
+    const int64_t rows = (int64_t)a.t.group * a.t.n_nodes;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        l[rb] += __shfl_xor(l[rb], 16, 64);
+        l[rb] += __shfl_xor(l[rb], 32, 64);
+        if (kb == 0) { ms[wave][rb * 16 + c] = m[rb]; ls[wave][rb * 16 + c] = l[rb]; }
+    }
+    __syncthreads();
+    const int row = tid >> 4, c8 = tid & 15;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        float mm = ms[0][rb * 16 + c];
+#pragma unroll
+        for (int v = 1; v < kTrWaves; ++v) mm = fmaxf(mm, ms[v][rb * 16 + c]);
+        const float f = __builtin_amdgcn_exp2f(m[rb] - mm);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; j += 4)
+                *reinterpret_cast<float4 *>(&meet[wave][c][32 * kb + 8 * r + j]) =
+                    make_float4(O[rb][j][r] * f, O[rb][j + 1][r] * f, O[rb][j + 2][r] * f, O[rb][j + 3][r] * f);
+        __syncthreads();
+        const int64_t r = (int64_t)rblk * kRows + rb * 16 + row;
+        float o[8], mt = ms[0][rb * 16 + row], lt = 0.0f;
+#pragma unroll
+        for (int v = 1; v < kTrWaves; ++v) mt = fmaxf(mt, ms[v][rb * 16 + row]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < kTrWaves; ++v) {
+            lt += ls[v][rb * 16 + row] * __builtin_amdgcn_exp2f(ms[v][rb * 16 + row] - mt);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += meet[v][row][c8 * 8 + e];
+        }
+        if (a.parts > 1) {
+            float *st = a.state + (((int64_t)bh * a.row_blocks + rblk) * a.parts + part) * tree_state_floats(kRows);
+            float *op = st + (rb * 16 + row) * kHeadDim + c8 * 8;
+            *reinterpret_cast<float4 *>(op) = make_float4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<float4 *>(op + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            if (c8 == 0) { st[kRows * kHeadDim + rb * 16 + row] = mt; st[kRows * (kHeadDim + 1) + rb * 16 + row] = lt; }
+        } else if (r < rows) store_row8(a, b, h, r, nodes, c8, o, mt, lt);
+        if (rb + 1 < RB) __syncthreads();
+    }
+}
+
 template <int FMT, int RB>
 __global__ __launch_bounds__(kTrThreads, 2)
 void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
@@ -329,49 +381,552 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
         }
     }
 
-    // ---- the wavefronts' results meet ---------------------------------------------------------
+    finish_block<RB>(a, b, h, bh, rblk, part, sq.nodes, meet, ms, ls, O, m, l);
+}
+
+// ---- the packed form ------------------------------------------------------------------------------
+// Up to four rounds of 2-bit levels, or one of 4-bit levels (any scale format, id width and number of smoothing stages).
+// The sum over Eq. 7's parts is left to the contractions where that saves vector instructions, of which the decoding is
+// made: the centroid rows go to the matrix cores as they are stored, as bf16, and only the residual of the rounds,
+// sum_t s_t q_t, is formed, two elements at a time in packed binary16 arithmetic (one round: exact).  So S^T = C Q^T + R Q^T
+// with Q as bf16 and as binary16, and O^T = C^T P + R^T P with P as a sum of two bf16 numbers (16 significant bits; one would
+// cost 2^-9 of every weight) and as binary16.
+// A tile's codes and scales come in with a few wide loads a tile ahead and the centroid rows with one 16-byte gather per lane,
+// row and octet; the V side's codes, all scales and ids pass through a few KB of LDS that are the wavefront's own, where they are
+// transposed: tokens become contiguous, so that a lane reads four tokens' levels or scales, already paired, at once.
+template <bool V> struct Flag { static constexpr bool value = V; };
+constexpr int kTrRowPitch = 36;                     // 16-bit words per row of 32 tokens (72 bytes: 8-byte aligned, spread over the banks)
+
+__device__ __forceinline__ halfx2_t as_half2(uint32_t w) { return __builtin_bit_cast(halfx2_t, w); }
+__device__ __forceinline__ uint32_t as_bits(halfx2_t h) { return __builtin_bit_cast(uint32_t, h); }
+// packed a * b + c, one rounding per element
+__device__ __forceinline__ halfx2_t fma_half2(halfx2_t a, halfx2_t b, halfx2_t c) { return __builtin_elementwise_fma(a, b, c); }
+
+// Two-bit levels of w's halves, field j from the top: (q, q') as (2q, 2q')
+__device__ __forceinline__ halfx2_t level2(uint32_t w, int j) { return as_half2((w << (2 * j)) & 0xC000C000u); }
+// Four-bit levels: x holds q + 8 in its nibbles; nibble k of both halves as (q, q').  With the exponent of 1024 in front a
+// nibble is 1024 + u, or 1024 + 16 u from the second place of a byte.
+__device__ __forceinline__ halfx2_t level4(uint32_t x, int k) {
+    const uint32_t w = k < 2 ? x : x >> 8;
+    const halfx2_t big = {(_Float16)1032.0f, (_Float16)1032.0f}, sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f},
+                   off = {(_Float16)-72.0f, (_Float16)-72.0f};
+    if (k & 1) return fma_half2(as_half2((w & 0x00F000F0u) | 0x64006400u), sixteenth, off);
+    return as_half2((w & 0x000F000Fu) | 0x64006400u) - big;
+}
+
+// Bytes of a wavefront's LDS: V codes [T][16 octets][32 tokens], scales [2][T * G][32], row offsets [2][S][32]
+template <int T, bool I4>
+__host__ __device__ inline int tree_wave_bytes(int G, int S) {
+    return T * 16 * kTrRowPitch * (I4 ? 4 : 2) + 2 * T * G * kTrRowPitch * 2 + 2 * S * kTrTile * 4;
+}
+constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
+template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB == 1 ? 0 : RB * 8 * 1024; }
+
+template <int T, bool I4, bool ROPE, int RB>
+__global__ __launch_bounds__(kTrThreads, RB > 2 ? 1 : 2)
+void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
+    constexpr int kRows = 16 * RB, kCode = I4 ? 64 : 32;                 // code bytes per token and round
+    constexpr int kVPieces = T * kCode / 32;                             // 16-byte pieces of the V codes to a lane
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float ms[kTrWaves][kRows], ls[kTrWaves][kRows];
+    const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
+    if (w >= blocks) return;                                             // uniform, before any barrier
+    const int part = w % a.parts, rblk = w / a.parts % a.row_blocks, bh = w / a.parts / a.row_blocks;
+    const int b = bh / a.H, h = bh - b * a.H;
+    const qvg_tree_step &t = a.t;
+    const SeqTiles sq = tiles_of_sequence(t, b);
+    const int lo = (int)((int64_t)sq.total * part / a.parts), hi = (int)((int64_t)sq.total * (part + 1) / a.parts);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, kb = lane >> 4;
+    const int64_t rows = (int64_t)t.group * t.n_nodes;
+    uint4 *qlds = reinterpret_cast<uint4 *>(smem);                       // RB > 1: [RB][8][64] fragments
+    unsigned char *own = smem + tree_query_bytes<RB>() + wave * wave_bytes;
+    uint16_t *vcodes = reinterpret_cast<uint16_t *>(own);
+    uint16_t *scales = vcodes + T * 16 * kTrRowPitch * (I4 ? 2 : 1);
+    const int S = a.S, G = kHeadDim / a.B, TG = T * G;
+    uint32_t *offs = reinterpret_cast<uint32_t *>(scales + 2 * TG * kTrRowPitch);
+
+    // ---- Q: fragments 0..3 as bf16, 4..7 as binary16 in the order of the residual's fragments ----
+    uint4 qreg[8];
+    float qs[RB];
+    int node[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        l[rb] += __shfl_xor(l[rb], 16, 64);
-        l[rb] += __shfl_xor(l[rb], 32, 64);
-        if (kb == 0) { ms[wave][rb * 16 + c] = m[rb]; ls[wave][rb * 16 + c] = l[rb]; }
-    }
-    __syncthreads();
-    const int row = tid >> 4, c8 = tid & 15;
+        const int64_t r = (int64_t)rblk * kRows + rb * 16 + c;
+        node[rb] = -1;
+        float v[32];
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        float mm = ms[0][rb * 16 + c];
+        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+        if (r < rows) {
+            const RowPlace p = place_row(a, h, r);
+            if (p.node < sq.nodes) {
+                node[rb] = p.node;
+                const bf16_t *qp = static_cast<const bf16_t *>(t.q) + b * t.q_stride_seq + p.head * t.q_stride_head + p.node * t.q_stride_node + 32 * kb;
 #pragma unroll
-        for (int v = 1; v < kTrWaves; ++v) mm = fmaxf(mm, ms[v][rb * 16 + c]);
-        const float f = __builtin_amdgcn_exp2f(m[rb] - mm);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < 8; j += 4)
-                *reinterpret_cast<float4 *>(&meet[wave][c][32 * kb + 8 * r + j]) =
-                    make_float4(O[rb][j][r] * f, O[rb][j + 1][r] * f, O[rb][j + 2][r] * f, O[rb][j + 3][r] * f);
-        __syncthreads();
-        const int64_t r = (int64_t)rblk * kRows + rb * 16 + row;
-        float o[8], mt = ms[0][rb * 16 + row], lt = 0.0f;
-#pragma unroll
-        for (int v = 1; v < kTrWaves; ++v) mt = fmaxf(mt, ms[v][rb * 16 + row]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-#pragma unroll
-        for (int v = 0; v < kTrWaves; ++v) {
-            lt += ls[v][rb * 16 + row] * __builtin_amdgcn_exp2f(ms[v][rb * 16 + row] - mt);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] += meet[v][row][c8 * 8 + e];
+                for (int i = 0; i < 4; ++i) unpack_bf16x8(*reinterpret_cast<const uint4 *>(qp + 8 * i), v + 8 * i);
+            }
         }
-        if (a.parts > 1) {
-            float *st = a.state + (((int64_t)bh * a.row_blocks + rblk) * a.parts + part) * tree_state_floats(kRows);
-            float *op = st + (rb * 16 + row) * kHeadDim + c8 * 8;
-            *reinterpret_cast<float4 *>(op) = make_float4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<float4 *>(op + 4) = make_float4(o[4], o[5], o[6], o[7]);
-            if (c8 == 0) { st[kRows * kHeadDim + rb * 16 + row] = mt; st[kRows * (kHeadDim + 1) + rb * 16 + row] = lt; }
-        } else if (r < rows) store_row8(a, b, h, r, sq.nodes, c8, o, mt, lt);
-        if (rb + 1 < RB) __syncthreads();
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, __builtin_fabsf(v[i]));
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
+        qs[rb] = __builtin_amdgcn_ldexpf(a.scale * 1.4426950408889634f, ex - 9);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], 9 - ex);
+        uint4 f[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = pack_bf16x8(v + 8 * i);
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = I4 ? pack_f16x2_rne(v[8 * i + e], v[8 * i + 4 + e])
+                          : pack_f16x2_rne(v[16 * (i >> 1) + 7 - 4 * (i & 1) - e], v[16 * (i >> 1) + 15 - 4 * (i & 1) - e]);
+            f[4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        if (RB == 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qreg[i] = f[i];
+        } else if (wave == rb % kTrWaves) {                              // one wavefront leaves them for all
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qlds[(rb * 8 + i) * 64 + lane] = f[i];
+        }
     }
+    if (RB > 1) __syncthreads();
+    auto qfrag = [&](int rb, int i) { return RB == 1 ? qreg[i] : qlds[(rb * 8 + i) * 64 + lane]; };
+
+    PoolSide ks = a.k, vs = a.v;
+    const int sb = (a.fmt & kFmtE4M3) ? 1 : 2, idb = a.id_wide ? 2 : 1;
+    {
+        const int64_t tok = (int64_t)h * t.pool_pages * t.page_len, tables = (int64_t)h * t.pool_pages * S * a.K * kHeadDim;
+        ks.cent += tables;              vs.cent += tables;
+        ks.ids += tok * S * idb;        vs.ids += tok * S * idb;
+        ks.codes += tok * T * kCode;    vs.codes += tok * T * kCode;
+        ks.scales += tok * TG * sb;     vs.scales += tok * TG * sb;
+    }
+
+    floatx4_t O[RB][8];
+    float m[RB], l[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = kTrNoScore; l[rb] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) O[rb][j] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    floatx4_t Sc[RB][2];
+    auto clear_scores = [&]() {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) Sc[rb][hf] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    // bf16 rows: fragment i of both halves of the tile's tokens
+    auto scores_of_rows = [&](const uint4 (&row)[2][4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const bf16x8_t q = __builtin_bit_cast(bf16x8_t, qfrag(rb, i));
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    Sc[rb][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, row[hf][i]), q, Sc[rb][hf], 0, 0, 0);
+            }
+    };
+    uint4 Phi[RB], Plo[RB], Ph[RB];
+    // soft-max of the tile's scores; MASK: the lane's row sees token i of the tile where bit i of see[rb] is set
+    auto weights = [&](auto masked, const uint32_t (&see)[RB]) {
+        constexpr bool MASK = decltype(masked)::value;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = Sc[rb][e >> 2][e & 3];
+                if (MASK) x[e] = (see[rb] >> (16 * (e >> 2) + 4 * kb + (e & 3))) & 1u ? x[e] : -INFINITY;
+            }
+            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * qs[rb];
+            if (__ballot(top > m[rb] + (kTrBelow + kTrLag))) {           // uniform: some row's reference moves
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float m_new = fmaxf(m[rb], top - kTrBelow), alpha = __builtin_amdgcn_exp2f(m[rb] - m_new);
+                l[rb] *= alpha; m[rb] = m_new;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) O[rb][j] *= alpha;
+            }
+            uint32_t ph[4], pl[4], pf[4];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], qs[rb], -m[rb])); l[rb] += x[e]; }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                ph[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+                pl[e] = pack_bf16x2(x[2 * e] - bf16_lo(ph[e]), x[2 * e + 1] - bf16_hi(ph[e]));
+                pf[e] = pack_f16x2_rne(x[2 * e], x[2 * e + 1]);
+            }
+            Phi[rb] = make_uint4(ph[0], ph[1], ph[2], ph[3]);
+            Plo[rb] = make_uint4(pl[0], pl[1], pl[2], pl[3]);
+            Ph[rb] = make_uint4(pf[0], pf[1], pf[2], pf[3]);
+        }
+    };
+    // O^T += (bf16 rows of the lane's eight tokens)^T P
+    auto add_rows = [&](const uint4 (&row)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t x[4];
+#pragma unroll
+            for (int pr = 0; pr < 4; ++pr) {
+                const uint4 &ra = row[2 * pr], &rc = row[2 * pr + 1];
+                const uint32_t p0 = j < 2 ? ra.x : j < 4 ? ra.y : j < 6 ? ra.z : ra.w, p1 = j < 2 ? rc.x : j < 4 ? rc.y : j < 6 ? rc.z : rc.w;
+                x[pr] = __builtin_amdgcn_perm(p1, p0, j & 1 ? 0x07060302u : 0x05040100u);
+            }
+            const bf16x8_t v = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, Phi[rb]), O[rb][j], 0, 0, 0);
+                O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, Plo[rb]), O[rb][j], 0, 0, 0);
+            }
+        }
+    };
+    auto order_lds = []() { asm volatile("" ::: "memory"); };             // the wavefront's LDS operations stay in this order
+
+    // ---- compressed tiles ----------------------------------------------------------------------
+    struct Where { int page_index, first, count; int64_t page, tok; };    // of a tile; tok: its first token in the pool
+    const int L = sq.kv ? (int)t.page_len : 1;
+    auto place = [&](int pi, int in_page) {
+        Where x;
+        x.page_index = pi; x.first = in_page * kTrTile;
+        x.count = min(kTrTile, min(L, sq.kv - pi * L) - x.first);
+        const int64_t pg = t.page_table[(int64_t)b * t.table_pages + pi];
+        x.page = pg < 0 ? 0 : (pg >= t.pool_pages ? t.pool_pages - 1 : pg);
+        x.tok = x.page * L + x.first;
+        return x;
+    };
+    // What a lane fetches of a tile: of tokens c and 16 + c the K codes of its 32 channels; 16-byte pieces of the V codes; a scale
+    // record and the ids of one token (lanes 0..31: K, 32..63: V).  Tokens that are not there read the last one.
+    struct Raw { uint4 kc4[I4 ? 2 : 1][I4 ? T : 1]; uint2 kc[2][I4 ? 1 : T]; uint4 vc[kVPieces]; };
+    const bool vside = lane >= 32;
+    const uint8_t *side_scales = vside ? vs.scales : ks.scales, *side_ids = vside ? vs.ids : ks.ids;
+    auto fetch = [&](const Where &x, Raw &f) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint8_t *kp = ks.codes + (x.tok + min(16 * hf + c, x.count - 1)) * (T * kCode);
+#pragma unroll
+            for (int r = 0; r < T; ++r) {
+                if (I4) f.kc4[hf][r] = *reinterpret_cast<const uint4 *>(kp + r * 64 + kb * 16);
+                else f.kc[hf][r] = *reinterpret_cast<const uint2 *>(kp + r * 32 + kb * 8);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kVPieces; ++i) {
+            const int piece = i * 64 + lane, n = piece / (T * kCode / 16), rest = piece - n * (T * kCode / 16);
+            f.vc[i] = *reinterpret_cast<const uint4 *>(vs.codes + (x.tok + min(n, x.count - 1)) * (T * kCode) + rest * 16);
+        }
+    };
+    uint32_t id_of[kMaxSmooth];
+    auto fetch_ids = [&](const Where &x) {
+        const int64_t n = x.tok + min(lane & 31, x.count - 1);
+#pragma unroll
+        for (int st = 0; st < kMaxSmooth; ++st)
+            if (st < S) id_of[st] = load_id(side_ids, n * S + st, a.id_wide);
+    };
+    // scales and ids of the tile into LDS, transposed; scales as binary16 (halved with 2-bit levels, which come as 2q)
+    auto park = [&](const Where &x, const Raw &f) {
+        const int n = lane & 31;
+        const int64_t rec = (x.tok + min(n, x.count - 1)) * TG;
+        uint16_t *sp = scales + (vside ? TG * kTrRowPitch : 0) + n;
+        for (int i = 0; i < TG; ++i) {
+            _Float16 v;
+            if (sb == 1) v = __builtin_bit_cast(_Float16, (uint16_t)((side_scales[rec + i] & 0x7f) << 7)) * (_Float16)(I4 ? 256.0f : 128.0f);
+            else v = __builtin_bit_cast(_Float16, reinterpret_cast<const uint16_t *>(side_scales)[rec + i]) * (_Float16)(I4 ? 1.0f : 0.5f);
+            sp[i * kTrRowPitch] = __builtin_bit_cast(uint16_t, v);
+        }
+#pragma unroll
+        for (int st = 0; st < kMaxSmooth; ++st)
+            if (st < S) offs[((vside ? S : 0) + st) * kTrTile + n] = (uint32_t)(st * a.K + min(id_of[st], (uint32_t)a.K - 1u)) * kHeadDim;
+#pragma unroll
+        for (int i = 0; i < kVPieces; ++i) {
+            const int piece = i * 64 + lane, tokn = piece / (T * kCode / 16), rest = piece - tokn * (T * kCode / 16);
+            const uint32_t wd[4] = {f.vc[i].x, f.vc[i].y, f.vc[i].z, f.vc[i].w};
+            if (I4) {                                                    // four octets of a token and round
+                const int r = rest / 4, oct = rest % 4 * 4;
+                uint32_t *vp = reinterpret_cast<uint32_t *>(vcodes) + (r * 16 + oct) * kTrRowPitch + tokn;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vp[e * kTrRowPitch] = wd[e];
+            } else {                                                     // eight octets
+                const int r = rest / 2, oct = rest % 2 * 8;
+                uint16_t *vp = vcodes + (r * 16 + oct) * kTrRowPitch + tokn;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) vp[e * kTrRowPitch] = (uint16_t)(wd[e >> 1] >> (16 * (e & 1)));
+            }
+        }
+    };
+    auto gather_k = [&](const Where &x, int st, uint4 (&row)[2][4]) {
+        const bf16_t *cent = ks.cent + x.page * S * a.K * kHeadDim + 32 * kb;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint4 *rp = reinterpret_cast<const uint4 *>(cent + offs[st * kTrTile + 16 * hf + c]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row[hf][i] = rp[i];
+        }
+    };
+    auto gather_v = [&](const Where &x, int st, uint4 (&row)[8]) {
+        const bf16_t *cent = vs.cent + x.page * S * a.K * kHeadDim + 8 * c;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(offs + (S + st) * kTrTile + 16 * hf + 4 * kb);
+            row[4 * hf + 0] = *reinterpret_cast<const uint4 *>(cent + o.x);
+            row[4 * hf + 1] = *reinterpret_cast<const uint4 *>(cent + o.y);
+            row[4 * hf + 2] = *reinterpret_cast<const uint4 *>(cent + o.z);
+            row[4 * hf + 3] = *reinterpret_cast<const uint4 *>(cent + o.w);
+        }
+    };
+    // the residual of tokens c and 16 + c as fragments 0..3 (in the order of Q's fragments 4..7)
+    auto residual_k = [&](const Raw &f, int hf, int i, uint4 &out) {       // i: fragment
+        const int d = i >> 1;                                            // 16 channels, which share a scale
+        const uint16_t *sp = scales + ((32 * kb + 16 * d) / a.B) * kTrRowPitch + 16 * hf + c;
+        halfx2_t r[4];
+#pragma unroll
+        for (int rd = 0; rd < T; ++rd) {
+            const _Float16 s1 = __builtin_bit_cast(_Float16, sp[rd * G * kTrRowPitch]);
+            const halfx2_t s2 = {s1, s1};
+            uint32_t wd;
+            if (I4) { const uint4 &q4 = f.kc4[I4 ? hf : 0][I4 ? rd : 0]; wd = (i == 0 ? q4.x : i == 1 ? q4.y : i == 2 ? q4.z : q4.w) ^ 0x88888888u; }
+            else { const uint2 &q2 = f.kc[hf][I4 ? 0 : rd]; wd = d ? q2.y : q2.x; }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const halfx2_t lv = I4 ? level4(wd, e) : level2(wd, 4 * (i & 1) + e);
+                r[e] = rd ? fma_half2(lv, s2, r[e]) : lv * s2;
+            }
+        }
+        out = make_uint4(as_bits(r[0]), as_bits(r[1]), as_bits(r[2]), as_bits(r[3]));
+    };
+    // K_hat rotated, as fragments of the residual's order: the values meet in binary16 (rows of all stages in fp32 first)
+    auto rotated_k = [&](const Where &x, int hf, const uint4 (&res)[4], const float (&cen)[32], uint4 (&out)[4]) {
+        const int64_t at = min((int64_t)x.page_index * L + x.first + min(16 * hf + c, x.count - 1), t.rope_tokens - 1);
+        const uint4 *rp = reinterpret_cast<const uint4 *>(static_cast<const f16_t *>(t.k_rope_f16) + at * kHeadDim + 32 * kb);
+        float v[32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t rw[4] = {res[i].x, res[i].y, res[i].z, res[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int ca = I4 ? 8 * i + e : 16 * (i >> 1) + 7 - 4 * (i & 1) - e, cb = ca + (I4 ? 4 : 8);
+                const halfx2_t r2 = as_half2(rw[e]);
+                v[ca] = cen[ca] + (float)r2[0];
+                v[cb] = cen[cb] + (float)r2[1];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rotate_octet(v + 8 * i, rp[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t x4[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int ca = I4 ? 8 * i + e : 16 * (i >> 1) + 7 - 4 * (i & 1) - e, cb = ca + (I4 ? 4 : 8);
+                x4[e] = pack_f16x2_rne(v[ca], v[cb]);
+            }
+            out[i] = make_uint4(x4[0], x4[1], x4[2], x4[3]);
+        }
+    };
+    auto scores_of_residual = [&](int i, const uint4 &r0, const uint4 &r1) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const halfx8_t q = __builtin_bit_cast(halfx8_t, qfrag(rb, 4 + i));
+            Sc[rb][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8_t, r0), q, Sc[rb][0], 0, 0, 0);
+            Sc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8_t, r1), q, Sc[rb][1], 0, 0, 0);
+        }
+    };
+    // O^T += R^T P
+    auto add_residual = [&]() {
+        const uint16_t *sp = scales + (TG + 8 * c / a.B) * kTrRowPitch + 4 * kb;
+        uint32_t r[8][4];                                                // [channel][pair of tokens]
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+            for (int rd = 0; rd < T; ++rd) {
+                const uint2 s4 = *reinterpret_cast<const uint2 *>(sp + rd * G * kTrRowPitch + 16 * hf);
+                if (I4) {
+                    const uint4 w4 = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(vcodes) + (rd * 16 + c) * kTrRowPitch + 16 * hf + 4 * kb);
+#pragma unroll
+                    for (int pp = 0; pp < 2; ++pp) {
+                        const uint32_t wa = pp ? w4.z : w4.x, wb = pp ? w4.w : w4.y;
+                        const halfx2_t s2 = as_half2(pp ? s4.y : s4.x);
+#pragma unroll
+                        for (int hh = 0; hh < 2; ++hh) {
+                            const uint32_t x = __builtin_amdgcn_perm(wb, wa, hh ? 0x07060302u : 0x05040100u) ^ 0x88888888u;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const halfx2_t lv = level4(x, e);
+                                r[4 * hh + e][2 * hf + pp] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[4 * hh + e][2 * hf + pp])) : lv * s2);
+                            }
+                        }
+                    }
+                } else {
+                    const uint2 w2 = *reinterpret_cast<const uint2 *>(vcodes + (rd * 16 + c) * kTrRowPitch + 16 * hf + 4 * kb);
+#pragma unroll
+                    for (int pp = 0; pp < 2; ++pp) {
+                        const uint32_t wd = pp ? w2.y : w2.x;
+                        const halfx2_t s2 = as_half2(pp ? s4.y : s4.x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const halfx2_t lv = level2(wd, e);
+                            r[7 - e][2 * hf + pp] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[7 - e][2 * hf + pp])) : lv * s2);
+                        }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const halfx8_t v = __builtin_bit_cast(halfx8_t, make_uint4(r[j][0], r[j][1], r[j][2], r[j][3]));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(halfx8_t, Ph[rb]), O[rb][j], 0, 0, 0);
+        }
+    };
+
+    int ti = lo + wave;
+    if (ti < hi && ti < sq.kv_tiles) {
+        int pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
+        Where cur = place(pi, in_page);
+        Raw f;
+        fetch_ids(cur);
+        fetch(cur, f);
+        const int stop = min(hi, sq.kv_tiles);
+        while (true) {
+            park(cur, f);
+            order_lds();
+            uint4 krow[2][4], vrow[8];
+            gather_k(cur, 0, krow);
+            const bool more = ti + kTrWaves < stop;                      // uniform
+            Where nxt = cur;
+            Raw g;
+            if (more) {
+                in_page += kTrWaves;
+                while (in_page >= sq.per_page) { in_page -= sq.per_page; ++pi; }
+                nxt = place(pi, in_page);
+                fetch_ids(nxt);
+                fetch(nxt, g);
+            }
+            clear_scores();
+            if (ROPE) {
+                uint4 res[2][4];
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) residual_k(f, hf, i, res[hf][i]);
+                float cen[2][32];
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) unpack_bf16x8(krow[hf][i], cen[hf] + 8 * i);
+                for (int st = 1; st < S; ++st) {
+                    gather_k(cur, st, krow);
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float x[8];
+                            unpack_bf16x8(krow[hf][i], x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) cen[hf][8 * i + e] += x[e];
+                        }
+                }
+                uint4 rot[2][4];
+                rotated_k(cur, 0, res[0], cen[0], rot[0]);
+                rotated_k(cur, 1, res[1], cen[1], rot[1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) scores_of_residual(i, rot[0][i], rot[1][i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint4 r0, r1;
+                    residual_k(f, 0, i, r0);
+                    residual_k(f, 1, i, r1);
+                    scores_of_residual(i, r0, r1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                scores_of_rows(krow);
+                for (int st = 1; st < S; ++st) {
+                    gather_k(cur, st, krow);
+                    scores_of_rows(krow);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            gather_v(cur, 0, vrow);
+            uint32_t see[RB];
+            const uint32_t there = cur.count >= 32 ? 0xffffffffu : (1u << cur.count) - 1u;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) see[rb] = there;
+            if (cur.count < kTrTile) weights(Flag<true>{}, see);                  // uniform
+            else weights(Flag<false>{}, see);
+            __builtin_amdgcn_sched_barrier(0);
+            add_residual();
+            __builtin_amdgcn_sched_barrier(0);
+            add_rows(vrow);
+            for (int st = 1; st < S; ++st) {
+                gather_v(cur, st, vrow);
+                add_rows(vrow);
+            }
+            order_lds();
+            ti += kTrWaves;
+            if (!more) break;
+            cur = nxt; f = g;
+        }
+    }
+
+    // ---- the tail's and the new tokens' tiles ---------------------------------------------------
+    for (; ti < hi; ti += kTrWaves) {
+        const bool fresh = ti >= sq.kv_tiles + sq.tail_tiles;
+        const int first = (ti - sq.kv_tiles - (fresh ? sq.tail_tiles : 0)) * kTrTile;
+        const int count = min(kTrTile, (fresh ? sq.nodes : sq.tail) - first);
+        const uint32_t there = count >= 32 ? 0xffffffffu : (1u << count) - 1u;
+        uint32_t see[RB], any = there;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) see[rb] = node[rb] >= 0 ? there : 0u;
+        if (fresh) {
+            any = 0u;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                if (node[rb] >= 0) {
+                    if (t.mask) see[rb] &= t.mask[((int64_t)b * t.n_nodes + node[rb]) * ((t.n_nodes + 31) / 32) + first / 32];
+                    else {
+                        const int left = node[rb] - first;                 // sees tokens first .. first + left
+                        see[rb] &= left < 0 ? 0u : (left >= 31 ? 0xffffffffu : (2u << left) - 1u);
+                    }
+                }
+                any |= see[rb];
+            }
+#pragma unroll
+            for (int off = 1; off < 16; off *= 2) any |= __shfl_xor(any, off, 64);
+        }
+        const int64_t stride = fresh ? t.new_stride_node : t.tail_stride_token;
+        const int64_t off = fresh ? b * t.new_stride_seq + h * t.new_stride_head + first * stride
+                                  : b * t.tail_stride_seq + h * t.tail_stride_head + first * stride;
+        const bf16_t *kr = static_cast<const bf16_t *>(fresh ? t.k_new : t.k_tail) + off + 32 * kb;
+        const bf16_t *vr = static_cast<const bf16_t *>(fresh ? t.v_new : t.v_tail) + off + 8 * c;
+        uint4 krow[2][4], vrow[8];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                krow[hf][i] = *reinterpret_cast<const uint4 *>(kr + min(16 * hf + c, count - 1) * stride + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            vrow[e] = *reinterpret_cast<const uint4 *>(vr + min(16 * (e >> 2) + 4 * kb + (e & 3), count - 1) * stride);
+        clear_scores();
+        scores_of_rows(krow);
+        weights(Flag<true>{}, see);
+        // (a new token that no row sees may be no number)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!((any >> (16 * (e >> 2) + 4 * kb + (e & 3))) & 1u)) vrow[e] = make_uint4(0u, 0u, 0u, 0u);
+        add_rows(vrow);
+    }
+    __syncthreads();                                                     // (the meeting place lies over the wavefronts' own LDS)
+    finish_block<RB>(a, b, h, bh, rblk, part, sq.nodes, reinterpret_cast<float (*)[16][kTrPitch]>(smem), ms, ls, O, m, l);
 }
 
 // Joins the parts of a block: 16 lanes to a row, 8 channels each.
@@ -438,16 +993,47 @@ static void launch_fmt(const TreeArgs &a, int blocks, int block_rows, hipStream_
     else if (block_rows == 32) launch_rb<FMT, 2>(a, blocks, s);
     else launch_rb<FMT, 4>(a, blocks, s);
 }
+template <int T, bool I4, bool ROPE, int RB>
+static hipError_t launch_packed_rb(const TreeArgs &a, int blocks, hipStream_t s) {
+    const int per_xcd = (blocks + 7) / 8, wave_bytes = tree_wave_bytes<T, I4>(kHeadDim / a.B, a.S);
+    int lds = tree_query_bytes<RB>() + kTrWaves * wave_bytes;
+    if (lds < kTrMeetBytes) lds = kTrMeetBytes;
+    const auto kernel = tree_attn_packed<T, I4, ROPE, RB>;
+    if (lds > 64 * 1024) {
+        static LdsHighWater mark;
+        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), (size_t)lds, mark);
+        if (e != hipSuccess) return e;
+    }
+    kernel<<<dim3((unsigned)(per_xcd * 8)), dim3(kTrThreads), (size_t)lds, s>>>(a, blocks, per_xcd, wave_bytes);
+    return hipSuccess;
+}
+template <int T, bool I4, bool ROPE>
+static hipError_t launch_packed_rope(const TreeArgs &a, int blocks, int br, hipStream_t s) {
+    return br == 16 ? launch_packed_rb<T, I4, ROPE, 1>(a, blocks, s) : br == 32 ? launch_packed_rb<T, I4, ROPE, 2>(a, blocks, s)
+                                                                                : launch_packed_rb<T, I4, ROPE, 4>(a, blocks, s);
+}
+template <int T, bool I4>
+static hipError_t launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s) {
+    return a.t.k_rope_f16 ? launch_packed_rope<T, I4, true>(a, blocks, br, s) : launch_packed_rope<T, I4, false>(a, blocks, br, s);
+}
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     const int br = tree_block_rows((int64_t)a.t.group * a.t.n_nodes);
     const int64_t units = (int64_t)a.t.n_seqs * a.H * a.row_blocks;
     const int blocks = (int)(units * a.parts);
-    switch (a.fmt) {
+    const bool i4 = (a.fmt & kFmtInt4) != 0;
+    hipError_t e = hipSuccess;
+    if (i4 && a.T == 1) e = launch_packed<1, true>(a, blocks, br, s);
+    else if (!i4 && a.T == 1) e = launch_packed<1, false>(a, blocks, br, s);
+    else if (!i4 && a.T == 2) e = launch_packed<2, false>(a, blocks, br, s);
+    else if (!i4 && a.T == 3) e = launch_packed<3, false>(a, blocks, br, s);
+    else if (!i4 && a.T == 4) e = launch_packed<4, false>(a, blocks, br, s);
+    else switch (a.fmt) {
         case 0: launch_fmt<0>(a, blocks, br, s); break;
         case kFmtE4M3: launch_fmt<kFmtE4M3>(a, blocks, br, s); break;
         case kFmtInt4: launch_fmt<kFmtInt4>(a, blocks, br, s); break;
         default: launch_fmt<kFmtE4M3 | kFmtInt4>(a, blocks, br, s); break;
     }
+    if (e != hipSuccess) return e;
     if (a.parts > 1) {
         const int64_t n = units * br;
         tree_join_kernel<<<dim3((unsigned)((n + 15) / 16)), dim3(256), 0, s>>>(a, br);
