@@ -593,57 +593,104 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     // ---- compressed tiles ----------------------------------------------------------------------
     struct Where { int page_index, first, count; int64_t page, tok; };    // of a tile; tok: its first token in the pool
     const int L = sq.kv ? (int)t.page_len : 1;
-    auto place = [&](int pi, int in_page) {
+    auto place = [&](int pi, int in_page, const Where &last) {            // (a tile of the page before needs no table)
         Where x;
         x.page_index = pi; x.first = in_page * kTrTile;
         x.count = min(kTrTile, min(L, sq.kv - pi * L) - x.first);
-        const int64_t pg = t.page_table[(int64_t)b * t.table_pages + pi];
-        x.page = pg < 0 ? 0 : (pg >= t.pool_pages ? t.pool_pages - 1 : pg);
+        x.page = last.page;
+        if (pi != last.page_index) {
+            const int64_t pg = __builtin_amdgcn_readfirstlane(t.page_table[(int64_t)b * t.table_pages + pi]);
+            x.page = pg < 0 ? 0 : (pg >= t.pool_pages ? t.pool_pages - 1 : pg);
+        }
         x.tok = x.page * L + x.first;
         return x;
     };
     // What a lane fetches of a tile: of tokens c and 16 + c the K codes of its 32 channels; 16-byte pieces of the V codes; a scale
     // record and the ids of one token (lanes 0..31: K, 32..63: V).  Tokens that are not there read the last one.
-    struct Raw { uint4 kc4[I4 ? 2 : 1][I4 ? T : 1]; uint2 kc[2][I4 ? 1 : T]; uint4 vc[kVPieces]; };
+    // (the record's first kScWords words; longer ones, of groups of 16 channels and three rounds or more, are completed in `park`)
+    constexpr int kScWords = T < 2 ? 4 : 8;
+    struct Raw { uint4 kc4[I4 ? 2 : 1][I4 ? T : 1]; uint2 kc[2][I4 ? 1 : T]; uint4 vc[kVPieces]; uint32_t sc[kScWords]; };
+    const int rec_bytes = TG * sb;
     const bool vside = lane >= 32;
     const uint8_t *side_scales = vside ? vs.scales : ks.scales, *side_ids = vside ? vs.ids : ks.ids;
+    // (addresses: a uniform base and 32-bit offsets, which are the lane's own constants in a full tile)
+    auto load16 = [](const void *base, uint32_t off) { return *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(base) + off); };
     auto fetch = [&](const Where &x, Raw &f) {
+        const uint8_t *kbase = ks.codes + x.tok * (T * kCode), *vbase = vs.codes + x.tok * (T * kCode);
+        const bool full = x.count == kTrTile;                            // uniform
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            const uint8_t *kp = ks.codes + (x.tok + min(16 * hf + c, x.count - 1)) * (T * kCode);
+            const uint32_t n = full ? 16 * hf + c : min(16 * hf + c, x.count - 1);
+            const uint32_t off = n * (T * kCode) + kb * (kCode / 4);
 #pragma unroll
             for (int r = 0; r < T; ++r) {
-                if (I4) f.kc4[hf][r] = *reinterpret_cast<const uint4 *>(kp + r * 64 + kb * 16);
-                else f.kc[hf][r] = *reinterpret_cast<const uint2 *>(kp + r * 32 + kb * 8);
+                if (I4) f.kc4[hf][r] = load16(kbase, off + r * 64);
+                else f.kc[hf][r] = *reinterpret_cast<const uint2 *>(kbase + (off + r * 32));
             }
         }
 #pragma unroll
         for (int i = 0; i < kVPieces; ++i) {
-            const int piece = i * 64 + lane, n = piece / (T * kCode / 16), rest = piece - n * (T * kCode / 16);
-            f.vc[i] = *reinterpret_cast<const uint4 *>(vs.codes + (x.tok + min(n, x.count - 1)) * (T * kCode) + rest * 16);
+            const uint32_t piece = i * 64 + lane;
+            if (full) f.vc[i] = load16(vbase, piece * 16);
+            else {
+                const uint32_t n = piece / (T * kCode / 16), rest = piece - n * (T * kCode / 16);
+                f.vc[i] = load16(vbase, min(n, (uint32_t)x.count - 1) * (T * kCode) + rest * 16);
+            }
+        }
+        // (a record is a multiple of its round's bytes, a power of two; E4M3 arrays may start anywhere: memcpy, which is one load)
+        const uint8_t *sp = side_scales + x.tok * rec_bytes + (uint32_t)(min(lane & 31, x.count - 1) * rec_bytes);
+        const int piece = G * sb * (T == 2 ? 2 : T == 4 ? 4 : 1);
+        if (piece >= 16) {
+            uint4 v;
+#pragma unroll
+            for (int i = 0; i < kScWords / 4; ++i)
+                if (16 * i < rec_bytes) { __builtin_memcpy(&v, sp + 16 * i, 16); f.sc[4 * i] = v.x; f.sc[4 * i + 1] = v.y; f.sc[4 * i + 2] = v.z; f.sc[4 * i + 3] = v.w; }
+        } else if (piece == 8) {
+            uint2 v;
+#pragma unroll
+            for (int i = 0; i < (T == 3 ? 3 : 1); ++i) { __builtin_memcpy(&v, sp + 8 * i, 8); f.sc[2 * i] = v.x; f.sc[2 * i + 1] = v.y; }
+        } else if (piece == 4) {
+#pragma unroll
+            for (int i = 0; i < (T == 3 ? 3 : 1); ++i) __builtin_memcpy(&f.sc[i], sp + 4 * i, 4);
+        } else if (piece == 2) {
+            uint16_t v[T == 3 ? 3 : 1];
+#pragma unroll
+            for (int i = 0; i < (T == 3 ? 3 : 1); ++i) __builtin_memcpy(&v[i], sp + 2 * i, 2);
+            f.sc[0] = v[0];
+            if (T == 3) { f.sc[0] |= (uint32_t)v[T == 3 ? 1 : 0] << 16; f.sc[1] = v[T == 3 ? 2 : 0]; }
+        } else {
+            f.sc[0] = sp[0];
+            if (T == 3) f.sc[0] |= (uint32_t)sp[1] << 8 | (uint32_t)sp[2] << 16;
         }
     };
     uint32_t id_of[kMaxSmooth];
     auto fetch_ids = [&](const Where &x) {
-        const int64_t n = x.tok + min(lane & 31, x.count - 1);
+        const uint8_t *ip = side_ids + x.tok * (S * idb) + (uint32_t)(min(lane & 31, x.count - 1) * S * idb);
 #pragma unroll
         for (int st = 0; st < kMaxSmooth; ++st)
-            if (st < S) id_of[st] = load_id(side_ids, n * S + st, a.id_wide);
+            if (st < S) id_of[st] = load_id(ip, st, a.id_wide);
     };
     // scales and ids of the tile into LDS, transposed; scales as binary16 (halved with 2-bit levels, which come as 2q)
     auto park = [&](const Where &x, const Raw &f) {
         const int n = lane & 31;
-        const int64_t rec = (x.tok + min(n, x.count - 1)) * TG;
         uint16_t *sp = scales + (vside ? TG * kTrRowPitch : 0) + n;
-        for (int i = 0; i < TG; ++i) {
-            _Float16 v;
-            if (sb == 1) v = __builtin_bit_cast(_Float16, (uint16_t)((side_scales[rec + i] & 0x7f) << 7)) * (_Float16)(I4 ? 256.0f : 128.0f);
-            else v = __builtin_bit_cast(_Float16, reinterpret_cast<const uint16_t *>(side_scales)[rec + i]) * (_Float16)(I4 ? 1.0f : 0.5f);
+        auto leave = [&](int i, uint32_t bits) {
+            const _Float16 v = sb == 1 ? __builtin_bit_cast(_Float16, (uint16_t)((bits & 0x7f) << 7)) * (_Float16)(I4 ? 256.0f : 128.0f)
+                                       : __builtin_bit_cast(_Float16, (uint16_t)bits) * (_Float16)(I4 ? 1.0f : 0.5f);
             sp[i * kTrRowPitch] = __builtin_bit_cast(uint16_t, v);
+        };
+        if (sb == 1) {
+#pragma unroll
+            for (int i = 0; i < T * 8; ++i) if (i < TG) leave(i, f.sc[i / 4] >> (8 * (i & 3)) & 0xffu);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * kScWords; ++i) if (i < TG) leave(i, f.sc[i / 2] >> (16 * (i & 1)) & 0xffffu);
+            const int64_t rec = (x.tok + min(n, x.count - 1)) * TG;
+            for (int i = 2 * kScWords; i < TG; ++i) leave(i, reinterpret_cast<const uint16_t *>(side_scales)[rec + i]);
         }
 #pragma unroll
         for (int st = 0; st < kMaxSmooth; ++st)
-            if (st < S) offs[((vside ? S : 0) + st) * kTrTile + n] = (uint32_t)(st * a.K + min(id_of[st], (uint32_t)a.K - 1u)) * kHeadDim;
+            if (st < S) offs[((vside ? S : 0) + st) * kTrTile + n] = (uint32_t)(st * a.K + min(id_of[st], (uint32_t)a.K - 1u)) * (kHeadDim * 2);
 #pragma unroll
         for (int i = 0; i < kVPieces; ++i) {
             const int piece = i * 64 + lane, tokn = piece / (T * kCode / 16), rest = piece - tokn * (T * kCode / 16);
@@ -662,23 +709,23 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
         }
     };
     auto gather_k = [&](const Where &x, int st, uint4 (&row)[2][4]) {
-        const bf16_t *cent = ks.cent + x.page * S * a.K * kHeadDim + 32 * kb;
+        const bf16_t *cent = ks.cent + x.page * S * a.K * kHeadDim;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            const uint4 *rp = reinterpret_cast<const uint4 *>(cent + offs[st * kTrTile + 16 * hf + c]);
+            const uint32_t off = offs[st * kTrTile + 16 * hf + c] + 64 * kb;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) row[hf][i] = rp[i];
+            for (int i = 0; i < 4; ++i) row[hf][i] = load16(cent, off + 16 * i);
         }
     };
     auto gather_v = [&](const Where &x, int st, uint4 (&row)[8]) {
-        const bf16_t *cent = vs.cent + x.page * S * a.K * kHeadDim + 8 * c;
+        const bf16_t *cent = vs.cent + x.page * S * a.K * kHeadDim;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             const uint4 o = *reinterpret_cast<const uint4 *>(offs + (S + st) * kTrTile + 16 * hf + 4 * kb);
-            row[4 * hf + 0] = *reinterpret_cast<const uint4 *>(cent + o.x);
-            row[4 * hf + 1] = *reinterpret_cast<const uint4 *>(cent + o.y);
-            row[4 * hf + 2] = *reinterpret_cast<const uint4 *>(cent + o.z);
-            row[4 * hf + 3] = *reinterpret_cast<const uint4 *>(cent + o.w);
+            row[4 * hf + 0] = load16(cent, o.x + 16 * c);
+            row[4 * hf + 1] = load16(cent, o.y + 16 * c);
+            row[4 * hf + 2] = load16(cent, o.z + 16 * c);
+            row[4 * hf + 3] = load16(cent, o.w + 16 * c);
         }
     };
     // the residual of tokens c and 16 + c as fragments 0..3 (in the order of Q's fragments 4..7)
@@ -790,7 +837,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     int ti = lo + wave;
     if (ti < hi && ti < sq.kv_tiles) {
         int pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
-        Where cur = place(pi, in_page);
+        Where cur = place(pi, in_page, Where{-1, 0, 0, 0, 0});
         Raw f;
         fetch_ids(cur);
         fetch(cur, f);
@@ -806,7 +853,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
             if (more) {
                 in_page += kTrWaves;
                 while (in_page >= sq.per_page) { in_page -= sq.per_page; ++pi; }
-                nxt = place(pi, in_page);
+                nxt = place(pi, in_page, cur);
                 fetch_ids(nxt);
                 fetch(nxt, g);
             }
@@ -971,8 +1018,8 @@ TreePlan tree_plan(int H, const qvg_tree_step &t) {
     if (units < 1) return p;
     const int64_t tiles = t.table_pages * ((t.page_len + kTrTile - 1) / kTrTile) + (t.tail_capacity + kTrTile - 1) / kTrTile +
                           (t.n_nodes + kTrTile - 1) / kTrTile;
-    // about a thousand workgroups (four to a CU), two tiles to a wavefront at least
-    int64_t parts = (1024 + units - 1) / units;
+    // as many workgroups as the chip holds at once (two to a CU), two tiles to a wavefront at least
+    int64_t parts = 512 / units;
     const int64_t most = tiles / (2 * kTrWaves);
     if (parts > most) parts = most;
     if (parts > 1) {

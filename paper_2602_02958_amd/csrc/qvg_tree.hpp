@@ -16,8 +16,8 @@ struct TreeArgs {
     int row_blocks, parts;         // 16 * RB query rows of a KV head to a block; workgroups that share a block's tokens
     float *state;                  // partial results, parts > 1
 };
-// Rows of a KV head (group * n_nodes) are taken in blocks of 16, 32 or 64.
-inline int tree_block_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+// Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32.
+inline int tree_block_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
 struct TreePlan { int row_blocks, parts; size_t state_bytes; };
 TreePlan tree_plan(int H, const qvg_tree_step &t);
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s);
