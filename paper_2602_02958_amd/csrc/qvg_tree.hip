@@ -849,14 +849,17 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
             gather_k(cur, 0, krow);
             const bool more = ti + kTrWaves < stop;                      // uniform
             Where nxt = cur;
-            Raw g;
             if (more) {
                 in_page += kTrWaves;
                 while (in_page >= sq.per_page) { in_page -= sq.per_page; ++pi; }
                 nxt = place(pi, in_page, cur);
-                fetch_ids(nxt);
-                fetch(nxt, g);
             }
+            // The load counter is in order: the rows that this tile still needs are asked for before the next tile's data, which
+            // then has the rest of the tile to arrive
+            auto ahead = [&]() {
+                gather_v(cur, 0, vrow);
+                if (more) { fetch_ids(nxt); fetch(nxt, f); }
+            };
             clear_scores();
             if (ROPE) {
                 uint4 res[2][4];
@@ -864,6 +867,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
                 for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) residual_k(f, hf, i, res[hf][i]);
+                if (S == 1) ahead();
                 float cen[2][32];
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
@@ -882,6 +886,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
                         }
                 }
                 uint4 rot[2][4];
+                if (S > 1) ahead();
                 rotated_k(cur, 0, res[0], cen[0], rot[0]);
                 rotated_k(cur, 1, res[1], cen[1], rot[1]);
 #pragma unroll
@@ -895,14 +900,15 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
                     scores_of_residual(i, r0, r1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                if (S == 1) ahead();
                 scores_of_rows(krow);
                 for (int st = 1; st < S; ++st) {
                     gather_k(cur, st, krow);
                     scores_of_rows(krow);
                 }
+                if (S > 1) ahead();
             }
             __builtin_amdgcn_sched_barrier(0);
-            gather_v(cur, 0, vrow);
             uint32_t see[RB];
             const uint32_t there = cur.count >= 32 ? 0xffffffffu : (1u << cur.count) - 1u;
 #pragma unroll
@@ -920,7 +926,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
             order_lds();
             ti += kTrWaves;
             if (!more) break;
-            cur = nxt; f = g;
+            cur = nxt;
         }
     }
 
