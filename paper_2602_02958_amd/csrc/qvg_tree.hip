@@ -982,33 +982,46 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     finish_block<RB>(a, b, h, bh, rblk, part, sq.nodes, reinterpret_cast<float (*)[16][kTrPitch]>(smem), ms, ls, O, m, l);
 }
 
-// Joins the parts of a block: 16 lanes to a row, 8 channels each.
+// Joins a query row's parts: a workgroup to a row, 16 lanes (8 channels each) to a part, so that 16 parts are read at a time.
 __global__ __launch_bounds__(256)
 void tree_join_kernel(TreeArgs a, int block_rows) {
-    const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);      // block row
-    const int c8 = threadIdx.x & 15;
-    const int64_t total = (int64_t)a.t.n_seqs * a.H * a.row_blocks * block_rows;
-    if (i >= total) return;
-    const int64_t block = i / block_rows;
-    const int row = (int)(i - block * block_rows);
-    const int64_t bh = block / a.row_blocks;
+    __shared__ float sums[16][kTrPitch], weights[16];
+    const int64_t rows = (int64_t)a.t.group * a.t.n_nodes;
+    const int64_t bh = (int64_t)(blockIdx.x / (unsigned)rows), r = (int64_t)blockIdx.x - bh * rows;
     const int b = (int)(bh / a.H), h = (int)(bh - (int64_t)b * a.H);
-    const int64_t r = (block - bh * a.row_blocks) * block_rows + row;
-    if (r >= (int64_t)a.t.group * a.t.n_nodes) return;
-    const float *st = a.state + block * a.parts * tree_state_floats(block_rows);
-    const float *mp = st + block_rows * kHeadDim + row, *lp = mp + block_rows;
-    const int64_t step = tree_state_floats(block_rows);
+    const int64_t block = bh * a.row_blocks + r / block_rows;
+    const int row = (int)(r % block_rows), grp = threadIdx.x >> 4, c8 = threadIdx.x & 15;
+    const int step = (int)tree_state_floats(block_rows);
+    const float *st = a.state + block * a.parts * step;
+    const float *mp = st + block_rows * kHeadDim + row, *lp = mp + block_rows, *op = st + row * kHeadDim + c8 * 8;
     float m = kTrNoScore, l = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-    for (int p = 0; p < a.parts; ++p) m = fmaxf(m, mp[p * step]);
-    for (int p = 0; p < a.parts; ++p) {
-        const float f = __builtin_amdgcn_exp2f(mp[p * step] - m);
-        const float *op = st + p * step + row * kHeadDim + c8 * 8;
-        const float4 x = *reinterpret_cast<const float4 *>(op), y = *reinterpret_cast<const float4 *>(op + 4);
-        l += lp[p * step] * f;
+    // every lane finds the maximum over all parts: lane i of 64 looks at parts i, i + 64, ..
+    for (int p = threadIdx.x & 63; p < a.parts; p += 64) m = fmaxf(m, mp[(int64_t)p * step]);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+#pragma unroll 4
+    for (int p = grp; p < a.parts; p += 16) {
+        const float f = __builtin_amdgcn_exp2f(mp[(int64_t)p * step] - m);
+        const float4 x = *reinterpret_cast<const float4 *>(op + (int64_t)p * step), y = *reinterpret_cast<const float4 *>(op + (int64_t)p * step + 4);
+        l += lp[(int64_t)p * step] * f;
         o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
         o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
+    }
+    *reinterpret_cast<float4 *>(&sums[grp][c8 * 8]) = make_float4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<float4 *>(&sums[grp][c8 * 8 + 4]) = make_float4(o[4], o[5], o[6], o[7]);
+    if (c8 == 0) weights[grp] = l;
+    __syncthreads();
+    if (grp) return;
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll
+    for (int g = 0; g < 16; ++g) {
+        l += weights[g];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] += sums[g][c8 * 8 + e];
     }
     int nodes = a.t.n_nodes;
     if (a.t.nodes) { nodes = a.t.nodes[b]; nodes = nodes < 0 ? 0 : (nodes > a.t.n_nodes ? a.t.n_nodes : nodes); }
@@ -1088,8 +1101,8 @@ hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     }
     if (e != hipSuccess) return e;
     if (a.parts > 1) {
-        const int64_t n = units * br;
-        tree_join_kernel<<<dim3((unsigned)((n + 15) / 16)), dim3(256), 0, s>>>(a, br);
+        const int64_t n = (int64_t)a.t.n_seqs * a.H * a.t.group * a.t.n_nodes;
+        tree_join_kernel<<<dim3((unsigned)n), dim3(256), 0, s>>>(a, br);
     }
     return hipGetLastError();
 }
