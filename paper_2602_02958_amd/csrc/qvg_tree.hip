@@ -420,10 +420,10 @@ __host__ __device__ inline int tree_wave_bytes(int G, int S) {
     return T * 16 * kTrRowPitch * (I4 ? 4 : 2) + 2 * T * G * kTrRowPitch * 2 + 2 * S * kTrTile * 4;
 }
 constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
-template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB == 1 ? 0 : RB * 8 * 1024; }
+template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB * 8 * 1024; }
 
 template <int T, bool I4, bool ROPE, int RB>
-__global__ __launch_bounds__(kTrThreads, RB > 2 ? 1 : 2)
+__global__ __launch_bounds__(kTrThreads, 2)
 void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     constexpr int kRows = 16 * RB, kCode = I4 ? 64 : 32;                 // code bytes per token and round
     constexpr int kVPieces = T * kCode / 32;                             // 16-byte pieces of the V codes to a lane
@@ -439,7 +439,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
     const int64_t rows = (int64_t)t.group * t.n_nodes;
-    uint4 *qlds = reinterpret_cast<uint4 *>(smem);                       // RB > 1: [RB][8][64] fragments
+    uint4 *qlds = reinterpret_cast<uint4 *>(smem);                       // [RB][8][64] fragments
     unsigned char *own = smem + tree_query_bytes<RB>() + wave * wave_bytes;
     uint16_t *vcodes = reinterpret_cast<uint16_t *>(own);
     uint16_t *scales = vcodes + T * 16 * kTrRowPitch * (I4 ? 2 : 1);
@@ -447,7 +447,6 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     uint32_t *offs = reinterpret_cast<uint32_t *>(scales + 2 * TG * kTrRowPitch);
 
     // ---- Q: fragments 0..3 as bf16, 4..7 as binary16 in the order of the residual's fragments ----
-    uint4 qreg[8];
     float qs[RB];
     int node[RB];
 #pragma unroll
@@ -486,16 +485,13 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
                           : pack_f16x2_rne(v[16 * (i >> 1) + 7 - 4 * (i & 1) - e], v[16 * (i >> 1) + 15 - 4 * (i & 1) - e]);
             f[4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
         }
-        if (RB == 1) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qreg[i] = f[i];
-        } else if (wave == rb % kTrWaves) {                              // one wavefront leaves them for all
+        if (wave == rb % kTrWaves) {                              // one wavefront leaves them for all
 #pragma unroll
             for (int i = 0; i < 8; ++i) qlds[(rb * 8 + i) * 64 + lane] = f[i];
         }
     }
-    if (RB > 1) __syncthreads();
-    auto qfrag = [&](int rb, int i) { return RB == 1 ? qreg[i] : qlds[(rb * 8 + i) * 64 + lane]; };
+    __syncthreads();
+    auto qfrag = [&](int rb, int i) { return qlds[(rb * 8 + i) * 64 + lane]; };
 
     PoolSide ks = a.k, vs = a.v;
     const int sb = (a.fmt & kFmtE4M3) ? 1 : 2, idb = a.id_wide ? 2 : 1;
@@ -900,13 +896,13 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
                     scores_of_residual(i, r0, r1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (S == 1) ahead();
                 scores_of_rows(krow);
                 for (int st = 1; st < S; ++st) {
                     gather_k(cur, st, krow);
                     scores_of_rows(krow);
                 }
-                if (S > 1) ahead();
+                __builtin_amdgcn_sched_barrier(0);
+                ahead();
             }
             __builtin_amdgcn_sched_barrier(0);
             uint32_t see[RB];
@@ -1037,7 +1033,7 @@ TreePlan tree_plan(int H, const qvg_tree_step &t) {
     if (units < 1) return p;
     const int64_t tiles = t.table_pages * ((t.page_len + kTrTile - 1) / kTrTile) + (t.tail_capacity + kTrTile - 1) / kTrTile +
                           (t.n_nodes + kTrTile - 1) / kTrTile;
-    // as many workgroups as the chip holds at once (two to a CU), two tiles to a wavefront at least
+    // as many workgroups as the chip holds at once (two to a CU, three with blocks of 16 rows), two tiles to a wavefront at least
     int64_t parts = 512 / units;
     const int64_t most = tiles / (2 * kTrWaves);
     if (parts > most) parts = most;
