@@ -446,48 +446,53 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     const int S = a.S, G = kHeadDim / a.B, TG = T * G;
     uint32_t *offs = reinterpret_cast<uint32_t *>(scales + 2 * TG * kTrRowPitch);
 
-    // ---- Q: fragments 0..3 as bf16, 4..7 as binary16 in the order of the residual's fragments ----
+    // ---- Q: fragments 0..3 as bf16 (channels 32 i + 8 kb + e: a row's gathers then read 64 consecutive bytes of a token with four
+    // lanes), 4..7 as binary16 in the order of the residual's fragments (channels 32 kb + ..) ----
     float qs[RB];
     int node[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const int64_t r = (int64_t)rblk * kRows + rb * 16 + c;
         node[rb] = -1;
-        float v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+        const bf16_t *qp = nullptr;
         if (r < rows) {
             const RowPlace p = place_row(a, h, r);
             if (p.node < sq.nodes) {
                 node[rb] = p.node;
-                const bf16_t *qp = static_cast<const bf16_t *>(t.q) + b * t.q_stride_seq + p.head * t.q_stride_head + p.node * t.q_stride_node + 32 * kb;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) unpack_bf16x8(*reinterpret_cast<const uint4 *>(qp + 8 * i), v + 8 * i);
+                qp = static_cast<const bf16_t *>(t.q) + b * t.q_stride_seq + p.head * t.q_stride_head + p.node * t.q_stride_node;
             }
         }
-        float top = 0.0f;
+        auto octet = [&](int oct, float *v) {
+            unpack_bf16x8(qp ? *reinterpret_cast<const uint4 *>(qp + 8 * oct) : make_uint4(0u, 0u, 0u, 0u), v);
+        };
+        float v[32], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) octet(4 * kb + i, v + 8 * i);
 #pragma unroll
         for (int i = 0; i < 32; ++i) top = fmaxf(top, __builtin_fabsf(v[i]));
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
         qs[rb] = __builtin_amdgcn_ldexpf(a.scale * 1.4426950408889634f, ex - 9);
+        if (wave == rb % kTrWaves) {                                     // one wavefront leaves them for all
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], 9 - ex);
-        uint4 f[8];
+            for (int i = 0; i < 32; ++i) v[i] = __builtin_amdgcn_ldexpf(v[i], 9 - ex);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[i] = pack_bf16x8(v + 8 * i);
-            uint32_t x[4];
+            for (int i = 0; i < 4; ++i) {
+                uint32_t x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x[e] = I4 ? pack_f16x2_rne(v[8 * i + e], v[8 * i + 4 + e])
-                          : pack_f16x2_rne(v[16 * (i >> 1) + 7 - 4 * (i & 1) - e], v[16 * (i >> 1) + 15 - 4 * (i & 1) - e]);
-            f[4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
-        }
-        if (wave == rb % kTrWaves) {                              // one wavefront leaves them for all
+                for (int e = 0; e < 4; ++e)
+                    x[e] = I4 ? pack_f16x2_rne(v[8 * i + e], v[8 * i + 4 + e])
+                              : pack_f16x2_rne(v[16 * (i >> 1) + 7 - 4 * (i & 1) - e], v[16 * (i >> 1) + 15 - 4 * (i & 1) - e]);
+                qlds[(rb * 8 + 4 + i) * 64 + lane] = make_uint4(x[0], x[1], x[2], x[3]);
+            }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) qlds[(rb * 8 + i) * 64 + lane] = f[i];
+            for (int i = 0; i < 4; ++i) {
+                octet(4 * i + kb, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_ldexpf(v[e], 9 - ex);
+                qlds[(rb * 8 + i) * 64 + lane] = pack_bf16x8(v);
+            }
         }
     }
     __syncthreads();
@@ -708,9 +713,10 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
         const bf16_t *cent = ks.cent + x.page * S * a.K * kHeadDim;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t off = offs[st * kTrTile + 16 * hf + c] + 64 * kb;
+            // (as Q's fragments take them; the rotation wants them as the residual is)
+            const uint32_t off = offs[st * kTrTile + 16 * hf + c] + (ROPE ? 64 : 16) * kb;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) row[hf][i] = load16(cent, off + 16 * i);
+            for (int i = 0; i < 4; ++i) row[hf][i] = load16(cent, off + (ROPE ? 16 : 64) * i);
         }
     };
     auto gather_v = [&](const Where &x, int st, uint4 (&row)[8]) {
@@ -781,52 +787,51 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
             Sc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8_t, r1), q, Sc[rb][1], 0, 0, 0);
         }
     };
-    // O^T += R^T P
+    // O^T += R^T P, four channels of the lane's octet at a time (which registers are what the loop is short of)
     auto add_residual = [&]() {
         const uint16_t *sp = scales + (TG + 8 * c / a.B) * kTrRowPitch + 4 * kb;
-        uint32_t r[8][4];                                                // [channel][pair of tokens]
+        uint2 s4[T][2], w2[I4 ? 1 : T][2];
+        uint4 w4[I4 ? T : 1][2];
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int rd = 0; rd < T; ++rd)
 #pragma unroll
-            for (int rd = 0; rd < T; ++rd) {
-                const uint2 s4 = *reinterpret_cast<const uint2 *>(sp + rd * G * kTrRowPitch + 16 * hf);
-                if (I4) {
-                    const uint4 w4 = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(vcodes) + (rd * 16 + c) * kTrRowPitch + 16 * hf + 4 * kb);
+            for (int hf = 0; hf < 2; ++hf) {
+                s4[rd][hf] = *reinterpret_cast<const uint2 *>(sp + rd * G * kTrRowPitch + 16 * hf);
+                const int at = (rd * 16 + c) * kTrRowPitch + 16 * hf + 4 * kb;
+                if (I4) w4[I4 ? rd : 0][hf] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(vcodes) + at);
+                else w2[I4 ? 0 : rd][hf] = *reinterpret_cast<const uint2 *>(vcodes + at);
+            }
 #pragma unroll
-                    for (int pp = 0; pp < 2; ++pp) {
-                        const uint32_t wa = pp ? w4.z : w4.x, wb = pp ? w4.w : w4.y;
-                        const halfx2_t s2 = as_half2(pp ? s4.y : s4.x);
+        for (int half = 0; half < 2; ++half) {                           // channels 4 half .. 4 half + 3
+            uint32_t r[4][4];                                            // [channel][pair of tokens]
 #pragma unroll
-                        for (int hh = 0; hh < 2; ++hh) {
-                            const uint32_t x = __builtin_amdgcn_perm(wb, wa, hh ? 0x07060302u : 0x05040100u) ^ 0x88888888u;
+            for (int rd = 0; rd < T; ++rd)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const halfx2_t lv = level4(x, e);
-                                r[4 * hh + e][2 * hf + pp] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[4 * hh + e][2 * hf + pp])) : lv * s2);
-                            }
-                        }
+                for (int pr = 0; pr < 4; ++pr) {
+                    const uint2 &sv = s4[rd][pr >> 1];
+                    const halfx2_t s2 = as_half2(pr & 1 ? sv.y : sv.x);
+                    uint32_t x;
+                    if (I4) {
+                        const uint4 &wv = w4[I4 ? rd : 0][pr >> 1];
+                        x = __builtin_amdgcn_perm(pr & 1 ? wv.w : wv.y, pr & 1 ? wv.z : wv.x, half ? 0x07060302u : 0x05040100u) ^ 0x88888888u;
+                    } else {
+                        const uint2 &wv = w2[I4 ? 0 : rd][pr >> 1];
+                        x = pr & 1 ? wv.y : wv.x;
                     }
-                } else {
-                    const uint2 w2 = *reinterpret_cast<const uint2 *>(vcodes + (rd * 16 + c) * kTrRowPitch + 16 * hf + 4 * kb);
 #pragma unroll
-                    for (int pp = 0; pp < 2; ++pp) {
-                        const uint32_t wd = pp ? w2.y : w2.x;
-                        const halfx2_t s2 = as_half2(pp ? s4.y : s4.x);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const halfx2_t lv = level2(wd, e);
-                            r[7 - e][2 * hf + pp] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[7 - e][2 * hf + pp])) : lv * s2);
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        const halfx2_t lv = I4 ? level4(x, e) : level2(x, 7 - (4 * half + e));
+                        r[e][pr] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[e][pr])) : lv * s2);
                     }
                 }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const halfx8_t v = __builtin_bit_cast(halfx8_t, make_uint4(r[e][0], r[e][1], r[e][2], r[e][3]));
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    O[rb][4 * half + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(halfx8_t, Ph[rb]), O[rb][4 * half + e], 0, 0, 0);
             }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const halfx8_t v = __builtin_bit_cast(halfx8_t, make_uint4(r[j][0], r[j][1], r[j][2], r[j][3]));
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-                O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(halfx8_t, Ph[rb]), O[rb][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -954,14 +959,14 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
         const int64_t stride = fresh ? t.new_stride_node : t.tail_stride_token;
         const int64_t off = fresh ? b * t.new_stride_seq + h * t.new_stride_head + first * stride
                                   : b * t.tail_stride_seq + h * t.tail_stride_head + first * stride;
-        const bf16_t *kr = static_cast<const bf16_t *>(fresh ? t.k_new : t.k_tail) + off + 32 * kb;
+        const bf16_t *kr = static_cast<const bf16_t *>(fresh ? t.k_new : t.k_tail) + off + 8 * kb;
         const bf16_t *vr = static_cast<const bf16_t *>(fresh ? t.v_new : t.v_tail) + off + 8 * c;
         uint4 krow[2][4], vrow[8];
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                krow[hf][i] = *reinterpret_cast<const uint4 *>(kr + min(16 * hf + c, count - 1) * stride + 8 * i);
+                krow[hf][i] = *reinterpret_cast<const uint4 *>(kr + min(16 * hf + c, count - 1) * stride + 32 * i);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             vrow[e] = *reinterpret_cast<const uint4 *>(vr + min(16 * (e >> 2) + 4 * kb + (e & 3), count - 1) * stride);
