@@ -414,19 +414,27 @@ __device__ __forceinline__ halfx2_t level4(uint32_t x, int k) {
     return as_half2((w & 0x000F000Fu) | 0x64006400u) - big;
 }
 
-// Bytes of a wavefront's LDS: V codes [T][16 octets][32 tokens], scales [2][T * G][32], row offsets [2][S][32]
-template <int T, bool I4>
-__host__ __device__ inline int tree_wave_bytes(int G, int S) {
-    return T * 16 * kTrRowPitch * (I4 ? 4 : 2) + 2 * T * G * kTrRowPitch * 2 + 2 * S * kTrTile * 4;
-}
-constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
+// A stored format at compile time: with sizes that are known every load of the loop has one form, and nothing waits for it
+// before it is used (as run-time branches between forms the loop took 1.0 instead of ... us).
 template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB * 8 * 1024; }
+template <int T_, int G_, bool FP8_, bool I4_, int S_>
+struct TreeFormat {
+    static constexpr int T = T_, G = G_, S = S_, TG = T * G;             // rounds, groups per token, smoothing stages
+    static constexpr bool FP8 = FP8_, I4 = I4_;
+    static constexpr int code = I4 ? 64 : 32;                            // code bytes per token and round
+    static constexpr int record = TG * (FP8 ? 1 : 2);                    // scale bytes per token
+    // bytes of a wavefront's LDS: V codes [T][16 octets][32 tokens], scales [2][T * G][32], row offsets [2][S][32]
+    static constexpr int wave_bytes = T * 16 * kTrRowPitch * (I4 ? 4 : 2) + 2 * TG * kTrRowPitch * 2 + 2 * S * kTrTile * 4;
+};
+constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
 
-template <int T, bool I4, bool ROPE, int RB>
+template <class F, bool ROPE, int RB>
 __global__ __launch_bounds__(kTrThreads, 2)
-void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
-    constexpr int kRows = 16 * RB, kCode = I4 ? 64 : 32;                 // code bytes per token and round
-    constexpr int kVPieces = T * kCode / 32;                             // 16-byte pieces of the V codes to a lane
+void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
+    constexpr int T = F::T, G = F::G, TG = F::TG, S = F::S, kCode = F::code, kRec = F::record;
+    constexpr bool I4 = F::I4, FP8 = F::FP8;
+    constexpr int kRows = 16 * RB;
+    constexpr int kVPieces = T * kCode / 32, kTokPieces = T * kCode / 16;   // 16-byte pieces of the V codes: to a lane, of a token
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float ms[kTrWaves][kRows], ls[kTrWaves][kRows];
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
@@ -440,10 +448,9 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     const int c = lane & 15, kb = lane >> 4;
     const int64_t rows = (int64_t)t.group * t.n_nodes;
     uint4 *qlds = reinterpret_cast<uint4 *>(smem);                       // [RB][8][64] fragments
-    unsigned char *own = smem + tree_query_bytes<RB>() + wave * wave_bytes;
+    unsigned char *own = smem + tree_query_bytes<RB>() + wave * F::wave_bytes;
     uint16_t *vcodes = reinterpret_cast<uint16_t *>(own);
     uint16_t *scales = vcodes + T * 16 * kTrRowPitch * (I4 ? 2 : 1);
-    const int S = a.S, G = kHeadDim / a.B, TG = T * G;
     uint32_t *offs = reinterpret_cast<uint32_t *>(scales + 2 * TG * kTrRowPitch);
 
     // ---- Q: fragments 0..3 as bf16 (channels 32 i + 8 kb + e: a row's gathers then read 64 consecutive bytes of a token with four
@@ -499,13 +506,13 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     auto qfrag = [&](int rb, int i) { return qlds[(rb * 8 + i) * 64 + lane]; };
 
     PoolSide ks = a.k, vs = a.v;
-    const int sb = (a.fmt & kFmtE4M3) ? 1 : 2, idb = a.id_wide ? 2 : 1;
+    const int idb = a.id_wide ? 2 : 1;
     {
         const int64_t tok = (int64_t)h * t.pool_pages * t.page_len, tables = (int64_t)h * t.pool_pages * S * a.K * kHeadDim;
         ks.cent += tables;              vs.cent += tables;
         ks.ids += tok * S * idb;        vs.ids += tok * S * idb;
         ks.codes += tok * T * kCode;    vs.codes += tok * T * kCode;
-        ks.scales += tok * TG * sb;     vs.scales += tok * TG * sb;
+        ks.scales += tok * kRec;        vs.scales += tok * kRec;
     }
 
     floatx4_t O[RB][8];
@@ -606,95 +613,52 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
         x.tok = x.page * L + x.first;
         return x;
     };
-    // What a lane fetches of a tile: of tokens c and 16 + c the K codes of its 32 channels; 16-byte pieces of the V codes; a scale
-    // record and the ids of one token (lanes 0..31: K, 32..63: V).  Tokens that are not there read the last one.
-    // (the record's first kScWords words; longer ones, of groups of 16 channels and three rounds or more, are completed in `park`)
-    constexpr int kScWords = T < 2 ? 4 : 8;
-    struct Raw { uint4 kc4[I4 ? 2 : 1][I4 ? T : 1]; uint2 kc[2][I4 ? 1 : T]; uint4 vc[kVPieces]; uint32_t sc[kScWords]; };
-    const int rec_bytes = TG * sb;
+    // What a lane fetches of a tile: of tokens c and 16 + c the K codes of its 32 channels; 16-byte pieces of the V codes; the
+    // scale record and the ids of one token (lanes 0..31: K, 32..63: V).  What belongs to tokens that are not there is read from
+    // the tile's last token instead, whatever piece of it that is: their weights are zero.  Addresses are a uniform base and
+    // 32-bit offsets.
+    struct Raw { uint4 kc4[2][I4 ? T : 1]; uint2 kc[2][I4 ? 1 : T]; uint4 vc[kVPieces]; uint32_t sc[(kRec + 3) / 4], id[S]; };
     const bool vside = lane >= 32;
     const uint8_t *side_scales = vside ? vs.scales : ks.scales, *side_ids = vside ? vs.ids : ks.ids;
-    // (addresses: a uniform base and 32-bit offsets, which are the lane's own constants in a full tile)
     auto load16 = [](const void *base, uint32_t off) { return *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(base) + off); };
     auto fetch = [&](const Where &x, Raw &f) {
         const uint8_t *kbase = ks.codes + x.tok * (T * kCode), *vbase = vs.codes + x.tok * (T * kCode);
-        const bool full = x.count == kTrTile;                            // uniform
+        const uint32_t n = min(lane & 31, x.count - 1);
+        const uint8_t *ip = side_ids + x.tok * (S * idb) + n * (S * idb);
+#pragma unroll
+        for (int st = 0; st < S; ++st) f.id[st] = load_id(ip, st, a.id_wide);
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t n = full ? 16 * hf + c : min(16 * hf + c, x.count - 1);
-            const uint32_t off = n * (T * kCode) + kb * (kCode / 4);
+            const uint32_t off = (uint32_t)min(16 * hf + c, x.count - 1) * (T * kCode) + kb * (kCode / 4);
 #pragma unroll
             for (int r = 0; r < T; ++r) {
-                if (I4) f.kc4[hf][r] = load16(kbase, off + r * 64);
-                else f.kc[hf][r] = *reinterpret_cast<const uint2 *>(kbase + (off + r * 32));
+                if (I4) f.kc4[hf][I4 ? r : 0] = load16(kbase, off + r * 64);
+                else f.kc[hf][I4 ? 0 : r] = *reinterpret_cast<const uint2 *>(kbase + (off + r * 32));
             }
         }
+        const uint32_t last = (uint32_t)x.count * (T * kCode) - 16;
 #pragma unroll
-        for (int i = 0; i < kVPieces; ++i) {
-            const uint32_t piece = i * 64 + lane;
-            if (full) f.vc[i] = load16(vbase, piece * 16);
-            else {
-                const uint32_t n = piece / (T * kCode / 16), rest = piece - n * (T * kCode / 16);
-                f.vc[i] = load16(vbase, min(n, (uint32_t)x.count - 1) * (T * kCode) + rest * 16);
-            }
-        }
-        // (a record is a multiple of its round's bytes, a power of two; E4M3 arrays may start anywhere: memcpy, which is one load)
-        const uint8_t *sp = side_scales + x.tok * rec_bytes + (uint32_t)(min(lane & 31, x.count - 1) * rec_bytes);
-        const int piece = G * sb * (T == 2 ? 2 : T == 4 ? 4 : 1);
-        if (piece >= 16) {
-            uint4 v;
-#pragma unroll
-            for (int i = 0; i < kScWords / 4; ++i)
-                if (16 * i < rec_bytes) { __builtin_memcpy(&v, sp + 16 * i, 16); f.sc[4 * i] = v.x; f.sc[4 * i + 1] = v.y; f.sc[4 * i + 2] = v.z; f.sc[4 * i + 3] = v.w; }
-        } else if (piece == 8) {
-            uint2 v;
-#pragma unroll
-            for (int i = 0; i < (T == 3 ? 3 : 1); ++i) { __builtin_memcpy(&v, sp + 8 * i, 8); f.sc[2 * i] = v.x; f.sc[2 * i + 1] = v.y; }
-        } else if (piece == 4) {
-#pragma unroll
-            for (int i = 0; i < (T == 3 ? 3 : 1); ++i) __builtin_memcpy(&f.sc[i], sp + 4 * i, 4);
-        } else if (piece == 2) {
-            uint16_t v[T == 3 ? 3 : 1];
-#pragma unroll
-            for (int i = 0; i < (T == 3 ? 3 : 1); ++i) __builtin_memcpy(&v[i], sp + 2 * i, 2);
-            f.sc[0] = v[0];
-            if (T == 3) { f.sc[0] |= (uint32_t)v[T == 3 ? 1 : 0] << 16; f.sc[1] = v[T == 3 ? 2 : 0]; }
-        } else {
-            f.sc[0] = sp[0];
-            if (T == 3) f.sc[0] |= (uint32_t)sp[1] << 8 | (uint32_t)sp[2] << 16;
-        }
+        for (int i = 0; i < kVPieces; ++i) f.vc[i] = load16(vbase, min((uint32_t)(i * 64 + lane) * 16, last));
+        __builtin_memcpy(f.sc, side_scales + x.tok * kRec + n * kRec, kRec);     // (E4M3 arrays may start anywhere)
     };
-    uint32_t id_of[kMaxSmooth];
-    auto fetch_ids = [&](const Where &x) {
-        const uint8_t *ip = side_ids + x.tok * (S * idb) + (uint32_t)(min(lane & 31, x.count - 1) * S * idb);
-#pragma unroll
-        for (int st = 0; st < kMaxSmooth; ++st)
-            if (st < S) id_of[st] = load_id(ip, st, a.id_wide);
-    };
-    // scales and ids of the tile into LDS, transposed; scales as binary16 (halved with 2-bit levels, which come as 2q)
-    auto park = [&](const Where &x, const Raw &f) {
+    // The tile's scales, row offsets and V codes into LDS, transposed; scales as binary16 (halved with 2-bit levels, which come as 2q)
+    auto park = [&](const Raw &f) {
         const int n = lane & 31;
+#pragma unroll
+        for (int st = 0; st < S; ++st)
+            offs[((vside ? S : 0) + st) * kTrTile + n] = (uint32_t)(st * a.K + min(f.id[st], (uint32_t)a.K - 1u)) * (kHeadDim * 2);
         uint16_t *sp = scales + (vside ? TG * kTrRowPitch : 0) + n;
-        auto leave = [&](int i, uint32_t bits) {
-            const _Float16 v = sb == 1 ? __builtin_bit_cast(_Float16, (uint16_t)((bits & 0x7f) << 7)) * (_Float16)(I4 ? 256.0f : 128.0f)
-                                       : __builtin_bit_cast(_Float16, (uint16_t)bits) * (_Float16)(I4 ? 1.0f : 0.5f);
+#pragma unroll
+        for (int i = 0; i < TG; ++i) {
+            const uint32_t bits = FP8 ? f.sc[i / 4] >> (8 * (i & 3)) & 0x7fu : f.sc[i / 2] >> (16 * (i & 1)) & 0xffffu;
+            // (E4M3 bits under binary16's exponent, seven places up, are the value times 2^-8)
+            const _Float16 v = FP8 ? __builtin_bit_cast(_Float16, (uint16_t)(bits << 7)) * (_Float16)(I4 ? 256.0f : 128.0f)
+                                   : __builtin_bit_cast(_Float16, (uint16_t)bits) * (_Float16)(I4 ? 1.0f : 0.5f);
             sp[i * kTrRowPitch] = __builtin_bit_cast(uint16_t, v);
-        };
-        if (sb == 1) {
-#pragma unroll
-            for (int i = 0; i < T * 8; ++i) if (i < TG) leave(i, f.sc[i / 4] >> (8 * (i & 3)) & 0xffu);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2 * kScWords; ++i) if (i < TG) leave(i, f.sc[i / 2] >> (16 * (i & 1)) & 0xffffu);
-            const int64_t rec = (x.tok + min(n, x.count - 1)) * TG;
-            for (int i = 2 * kScWords; i < TG; ++i) leave(i, reinterpret_cast<const uint16_t *>(side_scales)[rec + i]);
         }
 #pragma unroll
-        for (int st = 0; st < kMaxSmooth; ++st)
-            if (st < S) offs[((vside ? S : 0) + st) * kTrTile + n] = (uint32_t)(st * a.K + min(id_of[st], (uint32_t)a.K - 1u)) * (kHeadDim * 2);
-#pragma unroll
         for (int i = 0; i < kVPieces; ++i) {
-            const int piece = i * 64 + lane, tokn = piece / (T * kCode / 16), rest = piece - tokn * (T * kCode / 16);
+            const int piece = i * 64 + lane, tokn = piece / kTokPieces, rest = piece - tokn * kTokPieces;
             const uint32_t wd[4] = {f.vc[i].x, f.vc[i].y, f.vc[i].z, f.vc[i].w};
             if (I4) {                                                    // four octets of a token and round
                 const int r = rest / 4, oct = rest % 4 * 4;
@@ -733,14 +697,14 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     // the residual of tokens c and 16 + c as fragments 0..3 (in the order of Q's fragments 4..7)
     auto residual_k = [&](const Raw &f, int hf, int i, uint4 &out) {       // i: fragment
         const int d = i >> 1;                                            // 16 channels, which share a scale
-        const uint16_t *sp = scales + ((32 * kb + 16 * d) / a.B) * kTrRowPitch + 16 * hf + c;
+        const uint16_t *sp = scales + ((32 * kb + 16 * d) * G / kHeadDim) * kTrRowPitch + 16 * hf + c;
         halfx2_t r[4];
 #pragma unroll
         for (int rd = 0; rd < T; ++rd) {
             const _Float16 s1 = __builtin_bit_cast(_Float16, sp[rd * G * kTrRowPitch]);
             const halfx2_t s2 = {s1, s1};
             uint32_t wd;
-            if (I4) { const uint4 &q4 = f.kc4[I4 ? hf : 0][I4 ? rd : 0]; wd = (i == 0 ? q4.x : i == 1 ? q4.y : i == 2 ? q4.z : q4.w) ^ 0x88888888u; }
+            if (I4) { const uint4 &q4 = f.kc4[hf][I4 ? rd : 0]; wd = (i == 0 ? q4.x : i == 1 ? q4.y : i == 2 ? q4.z : q4.w) ^ 0x88888888u; }
             else { const uint2 &q2 = f.kc[hf][I4 ? 0 : rd]; wd = d ? q2.y : q2.x; }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -789,7 +753,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
     };
     // O^T += R^T P, four channels of the lane's octet at a time (which registers are what the loop is short of)
     auto add_residual = [&]() {
-        const uint16_t *sp = scales + (TG + 8 * c / a.B) * kTrRowPitch + 4 * kb;
+        const uint16_t *sp = scales + (TG + 8 * c * G / kHeadDim) * kTrRowPitch + 4 * kb;
         uint2 s4[T][2], w2[I4 ? 1 : T][2];
         uint4 w4[I4 ? T : 1][2];
 #pragma unroll
@@ -840,11 +804,10 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
         int pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
         Where cur = place(pi, in_page, Where{-1, 0, 0, 0, 0});
         Raw f;
-        fetch_ids(cur);
         fetch(cur, f);
         const int stop = min(hi, sq.kv_tiles);
         while (true) {
-            park(cur, f);
+            park(f);
             order_lds();
             uint4 krow[2][4], vrow[8];
             gather_k(cur, 0, krow);
@@ -859,7 +822,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
             // then has the rest of the tile to arrive
             auto ahead = [&]() {
                 gather_v(cur, 0, vrow);
-                if (more) { fetch_ids(nxt); fetch(nxt, f); }
+                if (more) fetch(nxt, f);
             };
             clear_scores();
             if (ROPE) {
@@ -899,7 +862,6 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd, int wave_bytes) {
                     residual_k(f, 0, i, r0);
                     residual_k(f, 1, i, r1);
                     scores_of_residual(i, r0, r1);
-                    __builtin_amdgcn_sched_barrier(0);
                 }
                 scores_of_rows(krow);
                 for (int st = 1; st < S; ++st) {
@@ -1057,50 +1019,42 @@ static void launch_rb(const TreeArgs &a, int blocks, hipStream_t s) {
 template <int FMT>
 static void launch_fmt(const TreeArgs &a, int blocks, int block_rows, hipStream_t s) {
     if (block_rows == 16) launch_rb<FMT, 1>(a, blocks, s);
-    else if (block_rows == 32) launch_rb<FMT, 2>(a, blocks, s);
-    else launch_rb<FMT, 4>(a, blocks, s);
+    else launch_rb<FMT, 2>(a, blocks, s);
 }
-template <int T, bool I4, bool ROPE, int RB>
-static hipError_t launch_packed_rb(const TreeArgs &a, int blocks, hipStream_t s) {
-    const int per_xcd = (blocks + 7) / 8, wave_bytes = tree_wave_bytes<T, I4>(kHeadDim / a.B, a.S);
-    int lds = tree_query_bytes<RB>() + kTrWaves * wave_bytes;
-    if (lds < kTrMeetBytes) lds = kTrMeetBytes;
-    const auto kernel = tree_attn_packed<T, I4, ROPE, RB>;
-    if (lds > 64 * 1024) {
-        static LdsHighWater mark;
-        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), (size_t)lds, mark);
-        if (e != hipSuccess) return e;
-    }
-    kernel<<<dim3((unsigned)(per_xcd * 8)), dim3(kTrThreads), (size_t)lds, s>>>(a, blocks, per_xcd, wave_bytes);
-    return hipSuccess;
+template <class F, bool ROPE, int RB>
+static void launch_packed_rb(const TreeArgs &a, int blocks, hipStream_t s) {
+    const int per_xcd = (blocks + 7) / 8;
+    constexpr int own = tree_query_bytes<RB>() + kTrWaves * F::wave_bytes, lds = own < kTrMeetBytes ? kTrMeetBytes : own;
+    static_assert(lds <= 64 * 1024, "more LDS needs the kernel's attribute raised");
+    tree_attn_packed<F, ROPE, RB><<<dim3((unsigned)(per_xcd * 8)), dim3(kTrThreads), (size_t)lds, s>>>(a, blocks, per_xcd);
 }
-template <int T, bool I4, bool ROPE>
-static hipError_t launch_packed_rope(const TreeArgs &a, int blocks, int br, hipStream_t s) {
-    return br == 16 ? launch_packed_rb<T, I4, ROPE, 1>(a, blocks, s) : br == 32 ? launch_packed_rb<T, I4, ROPE, 2>(a, blocks, s)
-                                                                                : launch_packed_rb<T, I4, ROPE, 4>(a, blocks, s);
-}
-template <int T, bool I4>
-static hipError_t launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s) {
-    return a.t.k_rope_f16 ? launch_packed_rope<T, I4, true>(a, blocks, br, s) : launch_packed_rope<T, I4, false>(a, blocks, br, s);
+template <int T, int G, bool FP8, bool I4, int S>
+static bool launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s) {
+    if (a.T != T || kHeadDim / a.B != G || a.S != S || a.fmt != ((FP8 ? kFmtE4M3 : 0) | (I4 ? kFmtInt4 : 0))) return false;
+    typedef TreeFormat<T, G, FP8, I4, S> F;
+    if (a.t.k_rope_f16) { if (br == 16) launch_packed_rb<F, true, 1>(a, blocks, s); else launch_packed_rb<F, true, 2>(a, blocks, s); }
+    else if (br == 16) launch_packed_rb<F, false, 1>(a, blocks, s);
+    else launch_packed_rb<F, false, 2>(a, blocks, s);
+    return true;
 }
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     const int br = tree_block_rows((int64_t)a.t.group * a.t.n_nodes);
     const int64_t units = (int64_t)a.t.n_seqs * a.H * a.row_blocks;
     const int blocks = (int)(units * a.parts);
-    const bool i4 = (a.fmt & kFmtInt4) != 0;
-    hipError_t e = hipSuccess;
-    if (i4 && a.T == 1) e = launch_packed<1, true>(a, blocks, br, s);
-    else if (!i4 && a.T == 1) e = launch_packed<1, false>(a, blocks, br, s);
-    else if (!i4 && a.T == 2) e = launch_packed<2, false>(a, blocks, br, s);
-    else if (!i4 && a.T == 3) e = launch_packed<3, false>(a, blocks, br, s);
-    else if (!i4 && a.T == 4) e = launch_packed<4, false>(a, blocks, br, s);
-    else switch (a.fmt) {
+    // The packed form is built for the formats of the package's configurations and of the paper's presets, and their
+    // neighbours in group size; any other one is decoded element by element.
+    const bool packed = launch_packed<1, 2, true, false, 1>(a, blocks, br, s) || launch_packed<1, 8, true, false, 1>(a, blocks, br, s) ||
+                        launch_packed<1, 8, true, false, 4>(a, blocks, br, s) || launch_packed<1, 2, true, true, 1>(a, blocks, br, s) ||
+                        launch_packed<1, 8, true, true, 4>(a, blocks, br, s) || launch_packed<1, 2, false, false, 1>(a, blocks, br, s) ||
+                        launch_packed<2, 2, false, false, 1>(a, blocks, br, s) || launch_packed<2, 4, false, false, 1>(a, blocks, br, s) ||
+                        launch_packed<3, 2, false, false, 1>(a, blocks, br, s) || launch_packed<3, 4, false, false, 1>(a, blocks, br, s) ||
+                        launch_packed<4, 2, false, false, 1>(a, blocks, br, s) || launch_packed<4, 4, false, false, 1>(a, blocks, br, s);
+    if (!packed) switch (a.fmt) {
         case 0: launch_fmt<0>(a, blocks, br, s); break;
         case kFmtE4M3: launch_fmt<kFmtE4M3>(a, blocks, br, s); break;
         case kFmtInt4: launch_fmt<kFmtInt4>(a, blocks, br, s); break;
         default: launch_fmt<kFmtE4M3 | kFmtInt4>(a, blocks, br, s); break;
     }
-    if (e != hipSuccess) return e;
     if (a.parts > 1) {
         const int64_t n = (int64_t)a.t.n_seqs * a.H * a.t.group * a.t.n_nodes;
         tree_join_kernel<<<dim3((unsigned)n), dim3(256), 0, s>>>(a, br);
