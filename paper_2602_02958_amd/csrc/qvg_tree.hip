@@ -391,8 +391,11 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
 // sum_t s_t q_t, is formed, two elements at a time in packed binary16 arithmetic (one round: exact).  So S^T = C Q^T + R Q^T
 // with Q as bf16 and as binary16, and O^T = C^T P + R^T P with P as a sum of two bf16 numbers (16 significant bits; one would
 // cost 2^-9 of every weight) and as binary16.
-// A tile's codes and scales come in with a few wide loads a tile ahead and the centroid rows with one 16-byte gather per lane,
-// row and octet; the V side's codes, all scales and ids pass through a few KB of LDS that are the wavefront's own, where they are
+// A token's part q.c of a score depends on its centroid alone: at the start of a page the workgroup contracts the page's tables
+// with its queries once and keeps the scores of all rows in LDS, where the tokens' accumulators start from what their ids name.
+// (Gathering K's rows as well, 256 bytes per token and side, the loop was bound by what the L2s give to gathers, about 10 TB/s:
+// one token over 12 heads x 187200 tokens of one round 125 us instead of ... .)  V's rows are gathered, 16 bytes per lane, row and octet.
+// A tile's codes and scales come in with a few wide loads a tile ahead; the V side's codes, all scales and ids pass through a few KB of LDS that are the wavefront's own, where they are
 // transposed: tokens become contiguous, so that a lane reads four tokens' levels or scales, already paired, at once.
 template <bool V> struct Flag { static constexpr bool value = V; };
 constexpr int kTrRowPitch = 36;                     // 16-bit words per row of 32 tokens (72 bytes: 8-byte aligned, spread over the banks)
@@ -435,6 +438,9 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     constexpr bool I4 = F::I4, FP8 = F::FP8;
     constexpr int kRows = 16 * RB;
     constexpr int kVPieces = T * kCode / 32, kTokPieces = T * kCode / 16;   // 16-byte pieces of the V codes: to a lane, of a token
+    // the scores of the centroids in LDS; not where keys are rotated, nor where four stages' tables and 32 rows would leave a
+    // CU one workgroup
+    constexpr bool kTable = !ROPE && (S == 1 || RB == 1);
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float ms[kTrWaves][kRows], ls[kTrWaves][kRows];
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
@@ -452,6 +458,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     uint16_t *vcodes = reinterpret_cast<uint16_t *>(own);
     uint16_t *scales = vcodes + T * 16 * kTrRowPitch * (I4 ? 2 : 1);
     uint32_t *offs = reinterpret_cast<uint32_t *>(scales + 2 * TG * kTrRowPitch);
+    float *table = reinterpret_cast<float *>(smem + tree_query_bytes<RB>() + kTrWaves * F::wave_bytes);   // [S * K][kRows], kTable
 
     // ---- Q: fragments 0..3 as bf16 (channels 32 i + 8 kb + e: a row's gathers then read 64 consecutive bytes of a token with four
     // lanes), 4..7 as binary16 in the order of the residual's fragments (channels 32 kb + ..) ----
@@ -646,7 +653,8 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
         const int n = lane & 31;
 #pragma unroll
         for (int st = 0; st < S; ++st)
-            offs[((vside ? S : 0) + st) * kTrTile + n] = (uint32_t)(st * a.K + min(f.id[st], (uint32_t)a.K - 1u)) * (kHeadDim * 2);
+            offs[((vside ? S : 0) + st) * kTrTile + n] =
+                (uint32_t)(st * a.K + min(f.id[st], (uint32_t)a.K - 1u)) * (uint32_t)(kTable && !vside ? kRows * 4 : kHeadDim * 2);
         uint16_t *sp = scales + (vside ? TG * kTrRowPitch : 0) + n;
 #pragma unroll
         for (int i = 0; i < TG; ++i) {
@@ -799,18 +807,67 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
         }
     };
 
-    int ti = lo + wave;
-    if (ti < hi && ti < sq.kv_tiles) {
-        int pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
-        Where cur = place(pi, in_page, Where{-1, 0, 0, 0, 0});
+    // the centroids' scores: q . c of every row of the page's tables, 16 rows to a contraction
+    auto build_table = [&](int64_t page) {
+        const bf16_t *cent = ks.cent + page * S * a.K * kHeadDim;
+        const int n = S * a.K;
+        for (int r0 = wave * 16; r0 < n; r0 += kTrWaves * 16) {
+            const uint32_t off = (uint32_t)min(r0 + c, n - 1) * (kHeadDim * 2) + 16 * kb;
+            uint4 row[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row[i] = load16(cent, off + 64 * i);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                floatx4_t x = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, row[i]), __builtin_bit_cast(bf16x8_t, qfrag(rb, i)), x, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) table[(r0 + 4 * kb + r) * kRows + rb * 16 + c] = x[r];
+            }
+        }
+    };
+    auto scores_of_ids = [&]() {
+#pragma unroll
+        for (int st = 0; st < S; ++st)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const uint4 o = *reinterpret_cast<const uint4 *>(offs + st * kTrTile + 16 * hf + 4 * kb);
+                const uint32_t at[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = *reinterpret_cast<const float *>(reinterpret_cast<const unsigned char *>(table) + at[r] + (rb * 16 + c) * 4);
+                        Sc[rb][hf][r] = st ? Sc[rb][hf][r] + x : x;
+                    }
+            }
+    };
+
+    const int stop = min(hi, sq.kv_tiles);
+    if (lo < stop) {                                                     // uniform over the workgroup
+        int ti = lo + wave, pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
+        Where cur{-1, 0, 0, 0, 0};
         Raw f;
-        fetch(cur, f);
-        const int stop = min(hi, sq.kv_tiles);
-        while (true) {
+        if (ti < stop) {
+            cur = place(pi, in_page, cur);
+            fetch(cur, f);
+        }
+        // page by page; a wavefront without tiles in a page still helps with its table
+        Where held{-1, 0, 0, 0, 0};
+        for (int pg = lo / sq.per_page; pg * sq.per_page < stop; ++pg) {
+            if (kTable) {
+                held = place(pg, 0, held);
+                __syncthreads();
+                build_table(held.page);
+                __syncthreads();
+            }
+            const int page_end = min(stop, (pg + 1) * sq.per_page);
+            while (ti < page_end) {
             park(f);
             order_lds();
             uint4 krow[2][4], vrow[8];
-            gather_k(cur, 0, krow);
+            if (!kTable) gather_k(cur, 0, krow);
             const bool more = ti + kTrWaves < stop;                      // uniform
             Where nxt = cur;
             if (more) {
@@ -824,7 +881,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                 gather_v(cur, 0, vrow);
                 if (more) fetch(nxt, f);
             };
-            clear_scores();
+            if (kTable) scores_of_ids(); else clear_scores();
             if (ROPE) {
                 uint4 res[2][4];
 #pragma unroll
@@ -863,10 +920,12 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                     residual_k(f, 1, i, r1);
                     scores_of_residual(i, r0, r1);
                 }
-                scores_of_rows(krow);
-                for (int st = 1; st < S; ++st) {
-                    gather_k(cur, st, krow);
+                if (!kTable) {
                     scores_of_rows(krow);
+                    for (int st = 1; st < S; ++st) {
+                        gather_k(cur, st, krow);
+                        scores_of_rows(krow);
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 ahead();
@@ -888,13 +947,13 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             }
             order_lds();
             ti += kTrWaves;
-            if (!more) break;
             cur = nxt;
+            }
         }
     }
 
     // ---- the tail's and the new tokens' tiles ---------------------------------------------------
-    for (; ti < hi; ti += kTrWaves) {
+    for (int ti = max(lo, sq.kv_tiles) + wave; ti < hi; ti += kTrWaves) {
         const bool fresh = ti >= sq.kv_tiles + sq.tail_tiles;
         const int first = (ti - sq.kv_tiles - (fresh ? sq.tail_tiles : 0)) * kTrTile;
         const int count = min(kTrTile, (fresh ? sq.nodes : sq.tail) - first);
@@ -1022,19 +1081,26 @@ static void launch_fmt(const TreeArgs &a, int blocks, int block_rows, hipStream_
     else launch_rb<FMT, 2>(a, blocks, s);
 }
 template <class F, bool ROPE, int RB>
-static void launch_packed_rb(const TreeArgs &a, int blocks, hipStream_t s) {
+static hipError_t launch_packed_rb(const TreeArgs &a, int blocks, hipStream_t s) {
     const int per_xcd = (blocks + 7) / 8;
-    constexpr int own = tree_query_bytes<RB>() + kTrWaves * F::wave_bytes, lds = own < kTrMeetBytes ? kTrMeetBytes : own;
-    static_assert(lds <= 64 * 1024, "more LDS needs the kernel's attribute raised");
+    constexpr bool table = !ROPE && (F::S == 1 || RB == 1);               // (as in the kernel)
+    constexpr int own = tree_query_bytes<RB>() + kTrWaves * F::wave_bytes;
+    int lds = own + (table ? (F::S * a.K + 15) / 16 * 16 * 16 * RB * 4 : 0);
+    if (lds < kTrMeetBytes) lds = kTrMeetBytes;
+    if (lds > 64 * 1024) {
+        static LdsHighWater mark;
+        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(tree_attn_packed<F, ROPE, RB>), (size_t)lds, mark);
+        if (e != hipSuccess) return e;
+    }
     tree_attn_packed<F, ROPE, RB><<<dim3((unsigned)(per_xcd * 8)), dim3(kTrThreads), (size_t)lds, s>>>(a, blocks, per_xcd);
+    return hipSuccess;
 }
 template <int T, int G, bool FP8, bool I4, int S>
-static bool launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s) {
+static bool launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s, hipError_t &e) {
     if (a.T != T || kHeadDim / a.B != G || a.S != S || a.fmt != ((FP8 ? kFmtE4M3 : 0) | (I4 ? kFmtInt4 : 0))) return false;
     typedef TreeFormat<T, G, FP8, I4, S> F;
-    if (a.t.k_rope_f16) { if (br == 16) launch_packed_rb<F, true, 1>(a, blocks, s); else launch_packed_rb<F, true, 2>(a, blocks, s); }
-    else if (br == 16) launch_packed_rb<F, false, 1>(a, blocks, s);
-    else launch_packed_rb<F, false, 2>(a, blocks, s);
+    if (a.t.k_rope_f16) e = br == 16 ? launch_packed_rb<F, true, 1>(a, blocks, s) : launch_packed_rb<F, true, 2>(a, blocks, s);
+    else e = br == 16 ? launch_packed_rb<F, false, 1>(a, blocks, s) : launch_packed_rb<F, false, 2>(a, blocks, s);
     return true;
 }
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
@@ -1043,12 +1109,14 @@ hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     const int blocks = (int)(units * a.parts);
     // The packed form is built for the formats of the package's configurations and of the paper's presets, and their
     // neighbours in group size; any other one is decoded element by element.
-    const bool packed = launch_packed<1, 2, true, false, 1>(a, blocks, br, s) || launch_packed<1, 8, true, false, 1>(a, blocks, br, s) ||
-                        launch_packed<1, 8, true, false, 4>(a, blocks, br, s) || launch_packed<1, 2, true, true, 1>(a, blocks, br, s) ||
-                        launch_packed<1, 8, true, true, 4>(a, blocks, br, s) || launch_packed<1, 2, false, false, 1>(a, blocks, br, s) ||
-                        launch_packed<2, 2, false, false, 1>(a, blocks, br, s) || launch_packed<2, 4, false, false, 1>(a, blocks, br, s) ||
-                        launch_packed<3, 2, false, false, 1>(a, blocks, br, s) || launch_packed<3, 4, false, false, 1>(a, blocks, br, s) ||
-                        launch_packed<4, 2, false, false, 1>(a, blocks, br, s) || launch_packed<4, 4, false, false, 1>(a, blocks, br, s);
+    hipError_t e = hipSuccess;
+    const bool packed = launch_packed<1, 2, true, false, 1>(a, blocks, br, s, e) || launch_packed<1, 8, true, false, 1>(a, blocks, br, s, e) ||
+                        launch_packed<1, 8, true, false, 4>(a, blocks, br, s, e) || launch_packed<1, 2, true, true, 1>(a, blocks, br, s, e) ||
+                        launch_packed<1, 8, true, true, 4>(a, blocks, br, s, e) || launch_packed<1, 2, false, false, 1>(a, blocks, br, s, e) ||
+                        launch_packed<2, 2, false, false, 1>(a, blocks, br, s, e) || launch_packed<2, 4, false, false, 1>(a, blocks, br, s, e) ||
+                        launch_packed<3, 2, false, false, 1>(a, blocks, br, s, e) || launch_packed<3, 4, false, false, 1>(a, blocks, br, s, e) ||
+                        launch_packed<4, 2, false, false, 1>(a, blocks, br, s, e) || launch_packed<4, 4, false, false, 1>(a, blocks, br, s, e);
+    if (e != hipSuccess) return e;
     if (!packed) switch (a.fmt) {
         case 0: launch_fmt<0>(a, blocks, br, s); break;
         case kFmtE4M3: launch_fmt<kFmtE4M3>(a, blocks, br, s); break;
