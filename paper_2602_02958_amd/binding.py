@@ -457,17 +457,30 @@ def attn_merge(out_a, lse_a, out_b, lse_b, out=None, want_lse=False):
 
 
 def _rows4(x, name, shape=None):
-    """[B, H, N, d] bf16 view with a contiguous last dim -> its three strides (those of one element are 0: they are not used,
-    and a view may hold anything there)."""
-    _check(x, torch.bfloat16, name)
-    if x.dim() != 4 or (x.stride(3) != 1 and x.shape[3] != 1) or (shape is not None and tuple(x.shape) != tuple(shape)):
+    """[B, H, N, d] bf16 view with a contiguous last dim -> its three strides (of a dimension of one element 0: it is not
+    used, and a view may hold anything there)."""
+    if x.dtype is not torch.bfloat16 or not x.is_cuda:
+        _check(x, torch.bfloat16, name)
+    if x.dim() != 4 or x.stride(3) != 1 or (shape is not None and x.shape != shape):
         raise ValueError(f"{name}: need bf16 {'[B, H, N, d]' if shape is None else list(shape)} with unit stride along d")
-    return tuple(0 if n == 1 else s for n, s in zip(x.shape[:3], x.stride()[:3]))
+    a, b, c, _ = x.stride()
+    if (a | b | c) & 7:
+        return tuple(0 if n == 1 else s for n, s in zip(x.shape[:3], (a, b, c)))
+    return a, b, c
+
+
+def _same_rows(x, y, names, shape=None):
+    """The strides that two views share."""
+    sx, sy = _rows4(x, names[0], shape), _rows4(y, names[1], x.shape)
+    if sx != sy and any(a != b and n != 1 for a, b, n in zip(sx, sy, x.shape)):
+        raise ValueError(f"{names[0]} and {names[1]} must share their strides")
+    return sx
 
 
 def _ints(t, shape, name):
-    _check(t, torch.int32, name)
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not torch.int32 or not t.is_cuda:
+        _check(t, torch.int32, name)
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: need a contiguous int32 tensor of shape {list(shape)}")
     return t.data_ptr()
 
@@ -482,15 +495,14 @@ def _here(*tensors):
 
 def _check_pool(e: Encoded, name):
     """The arrays of a pool agree with each other: whole pages, a set of tables to each."""
-    units, tokens = e.ids.shape[:2]
-    S, L = e.n_smooth, e.chunk_len
+    ids, codes, scales, cent, S, L = e.ids.shape, e.codes.shape, e.scales.shape, e.centroids.shape, e.n_smooth, e.chunk_len
+    units, tokens = ids[0], ids[1]
     if tokens % L or tokens < L:
         raise ValueError(f"{name}: the pool must hold whole pages of {L} tokens")
-    if (e.codes.shape[:2] != (units, tokens) or e.scales.shape[:2] != (units, tokens) or e.scales.shape[2] != e.codes.shape[2] or
-            e.centroids.shape[:2] != (units, tokens // L) or e.centroids.dim() != (4 if S == 1 else 5) or
-            (S > 1 and (e.centroids.shape[2] != S or tuple(e.ids.shape[2:]) != (S,)))):
+    if (codes[:3] != scales[:3] or codes[:2] != ids[:2] or cent[0] != units or cent[1] != tokens // L or
+            (len(cent) != 4 or len(ids) != 2 if S == 1 else len(cent) != 5 or cent[2] != S or ids[2:] != (S,))):
         raise ValueError(f"{name}: the pool's arrays are of different sizes")
-    _check_stored(e.centroids, e.ids, e.codes, e.scales, e.centroids.shape[-2])
+    _check_stored(e.centroids, e.ids, e.codes, e.scales, cent[-2])
 
 
 @functools.lru_cache(maxsize=256)
@@ -564,44 +576,39 @@ def _attn_tree(q, k: Encoded, kp, vp, H, page_table, kv_len, k_new, v_new, tail_
     if hq < H or hq % H:
         raise ValueError("q: the number of query heads must be a multiple of the KV heads'")
     K = k.centroids.shape[-2]
-    T, code_bytes = k.codes.shape[2:]
-    L, pool_tokens = k.chunk_len, k.ids.shape[1]
-    ns = _rows4(k_new, "k_new", (n, H, m, d))
-    if _rows4(v_new, "v_new", (n, H, m, d)) != ns:
-        raise ValueError("k_new and v_new must share their strides")
-    t = QvgTreeStep(n_seqs=n, group=hq // H, n_nodes=m, page_len=L, pool_pages=max(1, pool_tokens // L))
+    _, _, T, code_bytes = k.codes.shape
+    L = k.chunk_len
+    ns = _same_rows(k_new, v_new, ("k_new", "v_new"), (n, H, m, d))
     _here(q, k.ids, k_new, v_new, page_table, kv_len, tail_k, tail_v, tail_len, n_nodes, mask, k_rope, out, scratch)
+    pages, table, lens, rope, rope_tokens = 0, None, None, None, 0
     if page_table is not None and page_table.shape[-1] > 0:
-        t.table_pages = page_table.shape[-1]
-        t.page_table = _ints(page_table, (n, t.table_pages), "page_table")
-        t.kv_len = _ints(kv_len, (n,), "kv_len")
+        pages = page_table.shape[-1]
+        table, lens = _ints(page_table, (n, pages), "page_table"), _ints(kv_len, (n,), "kv_len")
         if k_rope is not None:
             _check(k_rope, torch.float16, "k_rope")
-            if k_rope.dim() != 3 or tuple(k_rope.shape[1:]) != (d // 2, 2) or not k_rope.is_contiguous() or k_rope.shape[0] < 1:
+            if k_rope.dim() != 3 or k_rope.shape[1:] != (d // 2, 2) or not k_rope.is_contiguous() or k_rope.shape[0] < 1:
                 raise ValueError("k_rope: need a contiguous [n, d/2, 2] float16 tensor")
-            t.k_rope_f16, t.rope_tokens = k_rope.data_ptr(), k_rope.shape[0]
-    t.q, (t.q_stride_seq, t.q_stride_head, t.q_stride_node) = q.data_ptr(), qs
-    t.k_new, t.v_new, (t.new_stride_seq, t.new_stride_head, t.new_stride_node) = k_new.data_ptr(), v_new.data_ptr(), ns
+            rope, rope_tokens = k_rope.data_ptr(), k_rope.shape[0]
+    R, tail, ts = 0, (None, None, None), (0, 0, 0)
     if tail_k is not None and tail_k.shape[2] > 0:
         if tail_v is None or tail_len is None:
             raise ValueError("tail_k needs tail_v and tail_len")
         R = tail_k.shape[2]
-        ts = _rows4(tail_k, "tail_k", (n, H, R, d))
-        if _rows4(tail_v, "tail_v", (n, H, R, d)) != ts:
-            raise ValueError("tail_k and tail_v must share their strides")
-        t.k_tail, t.v_tail, (t.tail_stride_seq, t.tail_stride_head, t.tail_stride_token) = tail_k.data_ptr(), tail_v.data_ptr(), ts
-        t.tail_len, t.tail_capacity = _ints(tail_len, (n,), "tail_len"), R
-    if n_nodes is not None:
-        t.nodes = _ints(n_nodes, (n,), "n_nodes")
-    if mask is not None:
-        t.mask = _ints(mask, (n, m, -(-m // 32)), "mask")
+        ts = _same_rows(tail_k, tail_v, ("tail_k", "tail_v"), (n, H, R, d))
+        tail = (tail_k.data_ptr(), tail_v.data_ptr(), _ints(tail_len, (n,), "tail_len"))
     if out is None:
         out = torch.empty(n, hq, m, d, dtype=torch.bfloat16, device=q.device)
-    t.out, (t.out_stride_seq, t.out_stride_head, t.out_stride_node) = out.data_ptr(), _rows4(out, "out", (n, hq, m, d))
+        os_ = (hq * m * d, m * d, d)
+    else:
+        os_ = _rows4(out, "out", q.shape)
     lse = torch.empty(n, hq, m, dtype=torch.float32, device=q.device) if want_lse else None
-    t.lse = _ptr(lse)
     if scratch is None:
-        scratch = _scratch(_tree_scratch_bytes(H, n, hq // H, m, t.table_pages, L, t.tail_capacity), q.device)
+        scratch = _scratch(_tree_scratch_bytes(H, n, hq // H, m, pages, L, R), q.device)
+    # (fields in the struct's order: naming them costs more than the smallest call's launches)
+    t = QvgTreeStep(n, hq // H, m, pages, L, max(1, k.ids.shape[1] // L), table, lens, q.data_ptr(), *qs,
+                    k_new.data_ptr(), v_new.data_ptr(), *ns, tail[0], tail[1], *ts, tail[2], R, 0,
+                    None if n_nodes is None else _ints(n_nodes, (n,), "n_nodes"),
+                    None if mask is None else _ints(mask, (n, m, -(-m // 32)), "mask"), rope, rope_tokens, out.data_ptr(), *os_, _ptr(lse))
     p = QvgParams(H, d, K, d // k.scales.shape[3], T, code_bytes * 8 // d, k.n_smooth, 0, k.scale_format)
     st = lib().qvg_attn_tree(p, C.byref(t), *kp, *vp, 1.0 / (d ** 0.5) if softmax_scale is None else softmax_scale,
                              _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
@@ -614,11 +621,9 @@ def keep_nodes(k_new, v_new, path, n_keep, tail_k, tail_v, tail_len, out_len=Non
     """qvg_keep_nodes: the K and V of the kept new tokens go behind the tails.  k_new, v_new [B, H, N, d] bf16; path [B, M] int32:
     the kept tokens' indices in order, n_keep [B] int32 how many; tail_k, tail_v [B, H, R, d] bf16 (written in place),
     tail_len [B] int32.  Returns the new lengths [B] int32 (out_len, which may be tail_len itself, or a new tensor)."""
-    ns = _rows4(k_new, "k_new")
+    ns = _same_rows(k_new, v_new, ("k_new", "v_new"))
     n, H, m, d = k_new.shape
-    ts = _rows4(tail_k, "tail_k", (n, H, tail_k.shape[2], d)) if tail_k.dim() == 4 else _rows4(tail_k, "tail_k")
-    if _rows4(v_new, "v_new", k_new.shape) != ns or _rows4(tail_v, "tail_v", tail_k.shape) != ts:
-        raise ValueError("K and V views must share their strides")
+    ts = _same_rows(tail_k, tail_v, ("tail_k", "tail_v"), (n, H, tail_k.shape[2], d) if tail_k.dim() == 4 else None)
     if path.dim() != 2:
         raise ValueError("path: need [B, M]")
     _here(k_new, v_new, path, n_keep, tail_k, tail_v, tail_len, out_len)

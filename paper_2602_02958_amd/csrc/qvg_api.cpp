@@ -754,6 +754,8 @@ int qvg_keep_nodes(int32_t n_heads, int32_t head_dim, int64_t n_seqs, int64_t n_
     a.path = path; a.keep = n_keep; a.tail_len = tail_len; a.tail_len_out = tail_len_out;
     a.H = n_heads; a.n_seqs = (int)n_seqs; a.n_nodes = (int)n_nodes; a.n_path = (int)n_path; a.capacity = (int)tail_capacity;
     a.blocks = rows ? (int)blocks : 0;
+    const uintptr_t was = reinterpret_cast<uintptr_t>(tail_len), now = reinterpret_cast<uintptr_t>(tail_len_out), size = (uintptr_t)n_seqs * sizeof(int32_t);
+    a.lengths_here = rows && tail_len_out && (now >= was + size || was >= now + size);
     return launch_keep_nodes(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
 }
 

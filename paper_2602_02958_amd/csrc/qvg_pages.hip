@@ -7,13 +7,15 @@ namespace qvg {
 // A node's row is its parent's row and its own bit.  One workgroup to a tree.  First every node finds, inside its block of 32
 // nodes, its ancestors and the parent of the topmost one (five pointer doublings by lane exchange, all blocks at once);
 // then the blocks take turns: the rows of a block are complete below its own word once the row of that outside ancestor is
-// copied, which lies in an earlier block.  So a tree of n nodes takes n / 32 steps however deep it is.
+// copied, which lies in an earlier block.  So a tree of n nodes takes n / 32 steps however deep it is.  The rows go out at the
+// end: a store in every step made its barrier wait for memory (64 trees of 1000 nodes 36 us instead of ...).
 __global__ __launch_bounds__(1024)
 void tree_mask_kernel(int n, int words, const int32_t *parents, const int32_t *nodes, uint32_t *mask, int32_t *depth) {
     extern __shared__ uint32_t lds[];
     uint32_t *rows = lds;                                   // [n][words]
     int *exit_of = reinterpret_cast<int *>(rows + n * words);          // [words * 32] outside ancestor, -1: none, -2: a hole
     uint32_t *inside = reinterpret_cast<uint32_t *>(exit_of + words * 32);   // [words * 32]
+    int *deep = reinterpret_cast<int *>(inside + words * 32);          // [words * 32] depths, -1: a hole
     const int b = blockIdx.x, tid = threadIdx.x;
     int live = n;
     if (nodes) { live = nodes[b]; live = live < 0 ? 0 : (live > n ? n : live); }
@@ -33,33 +35,31 @@ void tree_mask_kernel(int n, int words, const int32_t *parents, const int32_t *n
         exit_of[i] = up; inside[i] = bits;
     }
     __syncthreads();
+    // lanes of a wavefront have neighbouring words of a row; `shift`: words rounded up to a power of two
+    int shift = 0;
+    while ((1 << shift) < words) ++shift;
     for (int w = 0; w < words; ++w) {
-        // 32 rows of w + 1 words
-        for (int e = tid; e < 32 * words; e += blockDim.x) {
-            const int i = w * 32 + e / words, k = e - e / words * words;
-            if (i < n) {
+        for (int e = tid; e < 32 << shift; e += blockDim.x) {
+            const int i = w * 32 + (e >> shift), k = e & ((1 << shift) - 1);
+            if (i < n && k < words) {
                 const int up = exit_of[i];
-                // (a hole's row is empty: the outside ancestor's own word tells)
-                const bool hole = up == -2 || (up >= 0 && rows[up * words + (up >> 5)] == 0u);
-                const uint32_t v = hole || k > w ? 0u : k == w ? inside[i] : (up >= 0 ? rows[up * words + k] : 0u);
-                rows[i * words + k] = v;
-                mask[((int64_t)b * n + i) * words + k] = v;
+                const bool hole = up == -2 || (up >= 0 && deep[up] < 0);
+                rows[i * words + k] = hole || k > w ? 0u : k == w ? inside[i] : (up >= 0 ? rows[up * words + k] : 0u);
+                if (k == 0) deep[i] = hole ? -1 : __builtin_popcount(inside[i]) + (up >= 0 ? deep[up] : -1);
             }
         }
         __syncthreads();
     }
+    uint32_t *out = mask + (int64_t)b * n * words;
+    for (int e = tid; e < n * words; e += blockDim.x) out[e] = rows[e];
     if (depth)
-        for (int i = tid; i < n; i += blockDim.x) {
-            int d = -1;
-            for (int k = 0; k < words; ++k) d += __builtin_popcount(rows[i * words + k]);
-            depth[(int64_t)b * n + i] = d;
-        }
+        for (int i = tid; i < n; i += blockDim.x) depth[(int64_t)b * n + i] = deep[i];
 }
 
 hipError_t launch_tree_mask(int n_seqs, int n_nodes, const int32_t *parents, const int32_t *nodes, uint32_t *mask, int32_t *depth,
                             hipStream_t s) {
     const int words = (n_nodes + 31) / 32;
-    const size_t lds = ((size_t)n_nodes * words + 2 * (size_t)words * 32) * sizeof(uint32_t);
+    const size_t lds = ((size_t)n_nodes * words + 3 * (size_t)words * 32) * sizeof(uint32_t);
     static LdsHighWater mark;
     if (lds > 64 * 1024) {
         const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(tree_mask_kernel), lds, mark);
@@ -81,6 +81,8 @@ void keep_nodes_kernel(KeepArgs a) {
     int keep = a.keep[b], len = a.tail_len[b];
     keep = keep < 0 ? 0 : (keep > a.n_path ? a.n_path : keep);
     len = len < 0 ? 0 : (len > a.capacity ? a.capacity : len);
+    // (where the new lengths have a place of their own; else they wait for the rows to be done with the old ones)
+    if (a.lengths_here && u == 0 && i == 0 && c8 == 0) a.tail_len_out[b] = len + keep > a.capacity ? a.capacity : len + keep;
     if (i >= keep || len + i >= a.capacity) return;
     const int from = a.path[(int64_t)b * a.n_path + i];
     if (from < 0 || from >= a.n_nodes) return;
@@ -88,7 +90,7 @@ void keep_nodes_kernel(KeepArgs a) {
     bf16_t *dst = (side ? a.v_tail : a.k_tail) + b * a.tail_seq + h * a.tail_head + (int64_t)(len + i) * a.tail_token;
     reinterpret_cast<uint4 *>(dst)[c8] = reinterpret_cast<const uint4 *>(src)[c8];
 }
-// (in a launch of its own, behind the rows: tail_len_out may be tail_len)
+// (in a launch of its own, behind the rows, when tail_len_out may be tail_len)
 __global__ __launch_bounds__(256)
 void keep_lengths_kernel(KeepArgs a) {
     const int b = blockIdx.x * 256 + threadIdx.x;
@@ -99,9 +101,9 @@ void keep_lengths_kernel(KeepArgs a) {
     a.tail_len_out[b] = len + keep > a.capacity ? a.capacity : len + keep;
 }
 hipError_t launch_keep_nodes(const KeepArgs &a, hipStream_t s) {
-    if (a.n_path > 0)
+    if (a.blocks > 0)
         keep_nodes_kernel<<<dim3((unsigned)((int64_t)a.n_seqs * 2 * a.H * a.blocks)), dim3(256), 0, s>>>(a);
-    if (a.tail_len_out) keep_lengths_kernel<<<dim3((unsigned)((a.n_seqs + 255) / 256)), dim3(256), 0, s>>>(a);
+    if (a.tail_len_out && !a.lengths_here) keep_lengths_kernel<<<dim3((unsigned)((a.n_seqs + 255) / 256)), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -117,33 +119,40 @@ struct CopyArgs {
 };
 template <typename W>
 __device__ __forceinline__ void copy_pieces(const uint8_t *src, uint8_t *dst, int64_t from, int64_t bytes) {
-    const int64_t end = from + kCpBlock < bytes ? from + kCpBlock : bytes;
-    const W *s = reinterpret_cast<const W *>(src);
-    W *d = reinterpret_cast<W *>(dst);
-    for (int64_t i = from / (int64_t)sizeof(W) + threadIdx.x; i < end / (int64_t)sizeof(W); i += 4 * 256) {
-        W v[4];
-        const int64_t n = end / (int64_t)sizeof(W);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) if (i + k * 256 < n) v[k] = s[i + k * 256];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) if (i + k * 256 < n) d[i + k * 256] = v[k];
+    const int n = (int)((from + kCpBlock < bytes ? (int64_t)kCpBlock : bytes - from) / (int64_t)sizeof(W));
+    const W *s = reinterpret_cast<const W *>(src + from);
+    W *d = reinterpret_cast<W *>(dst + from);
+    const int i = (int)threadIdx.x;
+    if (i + 3 * 256 < n) {                                               // four pieces at a time (all there is of 16-byte ones)
+        for (int j = i; j + 3 * 256 < n; j += 4 * 256) {
+            const W x0 = s[j], x1 = s[j + 256], x2 = s[j + 512], x3 = s[j + 768];
+            d[j] = x0; d[j + 256] = x1; d[j + 512] = x2; d[j + 768] = x3;
+        }
     }
+    for (int j = i + (n - i > 0 ? (n - i + 255) / 256 / 4 * 4 * 256 : 0); j < n; j += 256) d[j] = s[j];
 }
+// Every field that a workgroup needs is asked for at once, the arrays' four descriptions among them: the arguments lie in memory
+// that is far away, and one after the other (or as a value, which indexed at run time every thread keeps in scratch memory)
+// they took 16 us of a copy of 1 MB.
 __global__ __launch_bounds__(256)
-void copy_pages_kernel(CopyArgs a) {
+void copy_pages_kernel(CopyArgs) {
+    const CopyArgs &a = *(const CopyArgs *)__builtin_amdgcn_kernarg_segment_ptr();
     const int pair = blockIdx.z, unit = blockIdx.y, blk = blockIdx.x;
-    int k = 0;
-    while (blk >= a.first_block[k + 1]) ++k;                             // (the last entry is the grid's width)
-    const PageArray p = a.array[k];
-    const uint8_t *src = p.src + unit * p.src_unit + a.src[pair] * p.bytes;
-    uint8_t *dst = p.dst + unit * p.dst_unit + a.dst[pair] * p.bytes;
-    const int64_t from = (int64_t)(blk - a.first_block[k]) * kCpBlock;
-    switch (a.width[k]) {
-        case 16: copy_pieces<uint4>(src, dst, from, p.bytes); break;
-        case 8: copy_pieces<uint2>(src, dst, from, p.bytes); break;
-        case 4: copy_pieces<uint32_t>(src, dst, from, p.bytes); break;
-        case 2: copy_pieces<uint16_t>(src, dst, from, p.bytes); break;
-        default: copy_pieces<uint8_t>(src, dst, from, p.bytes); break;
+    const int64_t from_page = a.src[pair], to_page = a.dst[pair];
+    const PageArray p0 = a.array[0], p1 = a.array[1], p2 = a.array[2], p3 = a.array[3];
+    const int f1 = a.first_block[1], f2 = a.first_block[2], f3 = a.first_block[3];
+    const int w0 = a.width[0], w1 = a.width[1], w2 = a.width[2], w3 = a.width[3];
+    auto pick = [&](auto x0, auto x1, auto x2, auto x3) { return blk < f1 ? x0 : blk < f2 ? x1 : blk < f3 ? x2 : x3; };
+    const int64_t bytes = pick(p0.bytes, p1.bytes, p2.bytes, p3.bytes);
+    const uint8_t *src = pick(p0.src, p1.src, p2.src, p3.src) + unit * pick(p0.src_unit, p1.src_unit, p2.src_unit, p3.src_unit) + from_page * bytes;
+    uint8_t *dst = pick(p0.dst, p1.dst, p2.dst, p3.dst) + unit * pick(p0.dst_unit, p1.dst_unit, p2.dst_unit, p3.dst_unit) + to_page * bytes;
+    const int64_t from = (int64_t)(blk - pick(0, f1, f2, f3)) * kCpBlock;
+    switch (pick(w0, w1, w2, w3)) {
+        case 16: copy_pieces<uint4>(src, dst, from, bytes); break;
+        case 8: copy_pieces<uint2>(src, dst, from, bytes); break;
+        case 4: copy_pieces<uint32_t>(src, dst, from, bytes); break;
+        case 2: copy_pieces<uint16_t>(src, dst, from, bytes); break;
+        default: copy_pieces<uint8_t>(src, dst, from, bytes); break;
     }
 }
 hipError_t launch_copy_pages(const PageArray (&arrays)[4], int units, int64_t n_pairs, const int32_t *src, const int32_t *dst,

@@ -397,7 +397,6 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
 // one token over 12 heads x 187200 tokens of one round 125 us instead of ... .)  V's rows are gathered, 16 bytes per lane, row and octet.
 // A tile's codes and scales come in with a few wide loads a tile ahead; the V side's codes, all scales and ids pass through a few KB of LDS that are the wavefront's own, where they are
 // transposed: tokens become contiguous, so that a lane reads four tokens' levels or scales, already paired, at once.
-template <bool V> struct Flag { static constexpr bool value = V; };
 constexpr int kTrRowPitch = 36;                     // 16-bit words per row of 32 tokens (72 bytes: 8-byte aligned, spread over the banks)
 
 __device__ __forceinline__ halfx2_t as_half2(uint32_t w) { return __builtin_bit_cast(halfx2_t, w); }
@@ -437,6 +436,9 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     constexpr int T = F::T, G = F::G, TG = F::TG, S = F::S, kCode = F::code, kRec = F::record;
     constexpr bool I4 = F::I4, FP8 = F::FP8;
     constexpr int kRows = 16 * RB;
+    // One block of 16 rows takes V's rows as they are and P twice; for more rows the values are put together in binary16, 96
+    // instructions a tile, and P is taken once, which saves 24 instructions, eight registers and 16 contractions a block
+    constexpr bool kSplitV = RB == 1;
     constexpr int kVPieces = T * kCode / 32, kTokPieces = T * kCode / 16;   // 16-byte pieces of the V codes: to a lane, of a token
     // the scores of the centroids in LDS; not where keys are rotated, nor where four stages' tables and 32 rows would leave a
     // CU one workgroup
@@ -549,57 +551,83 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                     Sc[rb][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, row[hf][i]), q, Sc[rb][hf], 0, 0, 0);
             }
     };
-    uint4 Phi[RB], Plo[RB], Ph[RB];
-    // soft-max of the tile's scores; MASK: the lane's row sees token i of the tile where bit i of see[rb] is set
-    auto weights = [&](auto masked, const uint32_t (&see)[RB]) {
-        constexpr bool MASK = decltype(masked)::value;
+    uint4 Phi[1], Plo[1], Ph[RB];
+    // the lane's row sees token i of the tile where bit i of see[rb] is set
+    auto hide = [&](const uint32_t (&see)[RB]) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                Sc[rb][e >> 2][e & 3] = (see[rb] >> (16 * (e >> 2) + 4 * kb + (e & 3))) & 1u ? Sc[rb][e >> 2][e & 3] : -INFINITY;
+    };
+    // soft-max of the tile's scores
+    auto weights = [&]() {
+        float top[RB];
+        bool move = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            float x[8];
+            const floatx4_t &x = Sc[rb][0], &y = Sc[rb][1];
+            top[rb] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))) * qs[rb];
+            move |= top[rb] > m[rb] + (kTrBelow + kTrLag);
+        }
+        if (__ballot(move)) {                                            // uniform: some row's reference moves
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = Sc[rb][e >> 2][e & 3];
-                if (MASK) x[e] = (see[rb] >> (16 * (e >> 2) + 4 * kb + (e & 3))) & 1u ? x[e] : -INFINITY;
-            }
-            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * qs[rb];
-            if (__ballot(top > m[rb] + (kTrBelow + kTrLag))) {           // uniform: some row's reference moves
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float m_new = fmaxf(m[rb], top - kTrBelow), alpha = __builtin_amdgcn_exp2f(m[rb] - m_new);
+            for (int rb = 0; rb < RB; ++rb) {
+                float x = fmaxf(top[rb], __shfl_xor(top[rb], 16, 64));
+                x = fmaxf(x, __shfl_xor(x, 32, 64));
+                const float m_new = fmaxf(m[rb], x - kTrBelow), alpha = __builtin_amdgcn_exp2f(m[rb] - m_new);
                 l[rb] *= alpha; m[rb] = m_new;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) O[rb][j] *= alpha;
             }
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float x[8];
             uint32_t ph[4], pl[4], pf[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], qs[rb], -m[rb])); l[rb] += x[e]; }
+            for (int e = 0; e < 8; ++e) { x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sc[rb][e >> 2][e & 3], qs[rb], -m[rb])); l[rb] += x[e]; }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
+                pf[e] = pack_f16x2_rne(x[2 * e], x[2 * e + 1]);
+                if (!kSplitV) continue;
                 ph[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
                 pl[e] = pack_bf16x2(x[2 * e] - bf16_lo(ph[e]), x[2 * e + 1] - bf16_hi(ph[e]));
-                pf[e] = pack_f16x2_rne(x[2 * e], x[2 * e + 1]);
             }
-            Phi[rb] = make_uint4(ph[0], ph[1], ph[2], ph[3]);
-            Plo[rb] = make_uint4(pl[0], pl[1], pl[2], pl[3]);
             Ph[rb] = make_uint4(pf[0], pf[1], pf[2], pf[3]);
+            if (kSplitV) {
+                Phi[0] = make_uint4(ph[0], ph[1], ph[2], ph[3]);
+                Plo[0] = make_uint4(pl[0], pl[1], pl[2], pl[3]);
+            }
         }
+    };
+    // the word of a row that holds channel j of the lane's octet; channel j of a pair of rows, as bf16 and as binary16
+    auto word_of = [](const uint4 &row, int j) { return j < 2 ? row.x : j < 4 ? row.y : j < 6 ? row.z : row.w; };
+    auto pair_f16 = [&](const uint4 &ra, const uint4 &rb_, int j) {
+        const uint32_t wa = word_of(ra, j), wb = word_of(rb_, j);
+        return as_half2(j & 1 ? pack_f16x2_rne(bf16_hi(wa), bf16_hi(wb)) : pack_f16x2_rne(bf16_lo(wa), bf16_lo(wb)));
+    };
+    auto add_pv = [&](int j, const uint32_t (&x)[4]) {
+        const halfx8_t v = __builtin_bit_cast(halfx8_t, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(halfx8_t, Ph[rb]), O[rb][j], 0, 0, 0);
     };
     // O^T += (bf16 rows of the lane's eight tokens)^T P
     auto add_rows = [&](const uint4 (&row)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint32_t x[4];
+            if (kSplitV) {
 #pragma unroll
-            for (int pr = 0; pr < 4; ++pr) {
-                const uint4 &ra = row[2 * pr], &rc = row[2 * pr + 1];
-                const uint32_t p0 = j < 2 ? ra.x : j < 4 ? ra.y : j < 6 ? ra.z : ra.w, p1 = j < 2 ? rc.x : j < 4 ? rc.y : j < 6 ? rc.z : rc.w;
-                x[pr] = __builtin_amdgcn_perm(p1, p0, j & 1 ? 0x07060302u : 0x05040100u);
-            }
-            const bf16x8_t v = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+                for (int pr = 0; pr < 4; ++pr)
+                    x[pr] = __builtin_amdgcn_perm(word_of(row[2 * pr + 1], j), word_of(row[2 * pr], j), j & 1 ? 0x07060302u : 0x05040100u);
+                const bf16x8_t v = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+                O[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, Phi[0]), O[0][j], 0, 0, 0);
+                O[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, Plo[0]), O[0][j], 0, 0, 0);
+            } else {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, Phi[rb]), O[rb][j], 0, 0, 0);
-                O[rb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, Plo[rb]), O[rb][j], 0, 0, 0);
+                for (int pr = 0; pr < 4; ++pr) x[pr] = as_bits(pair_f16(row[2 * pr], row[2 * pr + 1], j));
+                add_pv(j, x);
             }
         }
     };
@@ -759,8 +787,9 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             Sc[rb][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8_t, r1), q, Sc[rb][1], 0, 0, 0);
         }
     };
-    // O^T += R^T P, four channels of the lane's octet at a time (which registers are what the loop is short of)
-    auto add_residual = [&]() {
+    // O^T += R^T P (kSplitV), or (C + R)^T P with the sums of the rows in `start` ([channel][pair of tokens]), four channels of the
+    // lane's octet at a time (registers are what the loop is short of)
+    auto add_residual = [&](auto start) {
         const uint16_t *sp = scales + (TG + 8 * c * G / kHeadDim) * kTrRowPitch + 4 * kb;
         uint2 s4[T][2], w2[I4 ? 1 : T][2];
         uint4 w4[I4 ? T : 1][2];
@@ -793,16 +822,11 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const halfx2_t lv = I4 ? level4(x, e) : level2(x, 7 - (4 * half + e));
-                        r[e][pr] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[e][pr])) : lv * s2);
+                        r[e][pr] = as_bits(rd ? fma_half2(lv, s2, as_half2(r[e][pr])) : kSplitV ? lv * s2 : fma_half2(lv, s2, start(4 * half + e, pr)));
                     }
                 }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const halfx8_t v = __builtin_bit_cast(halfx8_t, make_uint4(r[e][0], r[e][1], r[e][2], r[e][3]));
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    O[rb][4 * half + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(halfx8_t, Ph[rb]), O[rb][4 * half + e], 0, 0, 0);
-            }
+            for (int e = 0; e < 4; ++e) add_pv(4 * half + e, r[e]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -931,19 +955,38 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                 ahead();
             }
             __builtin_amdgcn_sched_barrier(0);
-            uint32_t see[RB];
-            const uint32_t there = cur.count >= 32 ? 0xffffffffu : (1u << cur.count) - 1u;
+            if (cur.count < kTrTile) {                                   // uniform: the page's last tile
+                uint32_t see[RB];
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) see[rb] = there;
-            if (cur.count < kTrTile) weights(Flag<true>{}, see);                  // uniform
-            else weights(Flag<false>{}, see);
+                for (int rb = 0; rb < RB; ++rb) see[rb] = (1u << cur.count) - 1u;
+                hide(see);
+            }
+            weights();
             __builtin_amdgcn_sched_barrier(0);
-            add_residual();
-            __builtin_amdgcn_sched_barrier(0);
-            add_rows(vrow);
-            for (int st = 1; st < S; ++st) {
-                gather_v(cur, st, vrow);
+            if (kSplitV) {
+                add_residual([&](int, int) { return halfx2_t{}; });
+                __builtin_amdgcn_sched_barrier(0);
                 add_rows(vrow);
+                for (int st = 1; st < S; ++st) {
+                    gather_v(cur, st, vrow);
+                    add_rows(vrow);
+                }
+            } else if (S == 1) {
+                add_residual([&](int j, int pr) { return pair_f16(vrow[2 * pr], vrow[2 * pr + 1], j); });
+            } else {
+                halfx2_t sum[8][4];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int pr = 0; pr < 4; ++pr) sum[j][pr] = pair_f16(vrow[2 * pr], vrow[2 * pr + 1], j);
+                for (int st = 1; st < S; ++st) {
+                    gather_v(cur, st, vrow);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int pr = 0; pr < 4; ++pr) sum[j][pr] += pair_f16(vrow[2 * pr], vrow[2 * pr + 1], j);
+                }
+                add_residual([&](int j, int pr) { return sum[j][pr]; });
             }
             order_lds();
             ti += kTrWaves;
@@ -993,7 +1036,8 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             vrow[e] = *reinterpret_cast<const uint4 *>(vr + min(16 * (e >> 2) + 4 * kb + (e & 3), count - 1) * stride);
         clear_scores();
         scores_of_rows(krow);
-        weights(Flag<true>{}, see);
+        hide(see);
+        weights();
         // (a new token that no row sees may be no number)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -1099,8 +1143,10 @@ template <int T, int G, bool FP8, bool I4, int S>
 static bool launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s, hipError_t &e) {
     if (a.T != T || kHeadDim / a.B != G || a.S != S || a.fmt != ((FP8 ? kFmtE4M3 : 0) | (I4 ? kFmtInt4 : 0))) return false;
     typedef TreeFormat<T, G, FP8, I4, S> F;
-    if (a.t.k_rope_f16) e = br == 16 ? launch_packed_rb<F, true, 1>(a, blocks, s) : launch_packed_rb<F, true, 2>(a, blocks, s);
-    else e = br == 16 ? launch_packed_rb<F, false, 1>(a, blocks, s) : launch_packed_rb<F, false, 2>(a, blocks, s);
+    if (a.t.k_rope_f16)
+        e = br == 16 ? launch_packed_rb<F, true, 1>(a, blocks, s) : launch_packed_rb<F, true, 2>(a, blocks, s);
+    else
+        e = br == 16 ? launch_packed_rb<F, false, 1>(a, blocks, s) : launch_packed_rb<F, false, 2>(a, blocks, s);
     return true;
 }
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {

@@ -31,6 +31,7 @@ struct KeepArgs {
     const int32_t *path, *keep, *tail_len; int32_t *tail_len_out;
     int H, n_seqs, n_nodes, n_path, capacity;
     int blocks;                    // of 16 rows of a path
+    int lengths_here;              // the rows' launch writes tail_len_out too
 };
 hipError_t launch_keep_nodes(const KeepArgs &a, hipStream_t s);
 
