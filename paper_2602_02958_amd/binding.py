@@ -506,12 +506,12 @@ def _check_pool(e: Encoded, name):
 
 
 @functools.lru_cache(maxsize=256)
-def _tree_scratch_bytes(H, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity) -> int:
+def _tree_scratch_bytes(H, group_size, T, bits, n_smooth, scale_format, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity) -> int:
     """Bytes of scratch of an attn_tree of these sizes (a function of its arguments alone)."""
     need = C.c_size_t()
     t = QvgTreeStep(n_seqs=n_seqs, group=group, n_nodes=n_nodes, table_pages=table_pages, page_len=page_len, pool_pages=1,
                     tail_capacity=tail_capacity)
-    st = lib().qvg_attn_tree_scratch_bytes(make_params(H, 2, 128, 1), C.byref(t), C.byref(need))
+    st = lib().qvg_attn_tree_scratch_bytes(QvgParams(H, 128, 2, group_size, T, bits, n_smooth, 0, scale_format), C.byref(t), C.byref(need))
     if st != 0:
         raise QvgError(st, "qvg_attn_tree_scratch_bytes")
     return need.value
@@ -561,10 +561,13 @@ def attn_tree(q, k: Encoded, v: Encoded, page_table, kv_len, k_new, v_new, tail_
                       kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
 
 
-def attn_tree_scratch(heads, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity, device) -> torch.Tensor:
-    """Scratch for an attn_tree of these sizes."""
-    return torch.empty(_tree_scratch_bytes(heads, n_seqs, group, n_nodes, table_pages, page_len, tail_capacity),
-                       dtype=torch.uint8, device=device)
+def attn_tree_scratch(k: Encoded, n_seqs, group, n_nodes, table_pages, tail_capacity) -> torch.Tensor:
+    """Scratch for an attn_tree of these sizes over the pool k."""
+    _, _, T, code_bytes = k.codes.shape
+    d = k.centroids.shape[-1]
+    return torch.empty(_tree_scratch_bytes(k.ids.shape[0], d // k.scales.shape[3], T, code_bytes * 8 // d, k.n_smooth, k.scale_format,
+                                           n_seqs, group, n_nodes, table_pages, k.chunk_len, tail_capacity),
+                       dtype=torch.uint8, device=k.ids.device)
 
 
 def _attn_tree(q, k: Encoded, kp, vp, H, page_table, kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask,
@@ -602,14 +605,15 @@ def _attn_tree(q, k: Encoded, kp, vp, H, page_table, kv_len, k_new, v_new, tail_
     else:
         os_ = _rows4(out, "out", q.shape)
     lse = torch.empty(n, hq, m, dtype=torch.float32, device=q.device) if want_lse else None
+    B, bits, fp8 = d // k.scales.shape[3], code_bytes * 8 // d, k.scale_format
     if scratch is None:
-        scratch = _scratch(_tree_scratch_bytes(H, n, hq // H, m, pages, L, R), q.device)
+        scratch = _scratch(_tree_scratch_bytes(H, B, T, bits, k.n_smooth, fp8, n, hq // H, m, pages, L, R), q.device)
     # (fields in the struct's order: naming them costs more than the smallest call's launches)
     t = QvgTreeStep(n, hq // H, m, pages, L, max(1, k.ids.shape[1] // L), table, lens, q.data_ptr(), *qs,
                     k_new.data_ptr(), v_new.data_ptr(), *ns, tail[0], tail[1], *ts, tail[2], R, 0,
                     None if n_nodes is None else _ints(n_nodes, (n,), "n_nodes"),
                     None if mask is None else _ints(mask, (n, m, -(-m // 32)), "mask"), rope, rope_tokens, out.data_ptr(), *os_, _ptr(lse))
-    p = QvgParams(H, d, K, d // k.scales.shape[3], T, code_bytes * 8 // d, k.n_smooth, 0, k.scale_format)
+    p = QvgParams(H, d, K, B, T, bits, k.n_smooth, 0, fp8)
     st = lib().qvg_attn_tree(p, C.byref(t), *kp, *vp, 1.0 / (d ** 0.5) if softmax_scale is None else softmax_scale,
                              _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
     if st != 0:

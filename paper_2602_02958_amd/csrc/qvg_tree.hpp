@@ -13,13 +13,29 @@ struct TreeArgs {
     int H, K, B, T, S, fmt, id_wide;
     qvg_tree_step t;
     float scale;
-    int row_blocks, parts;         // 16 * RB query rows of a KV head to a block; workgroups that share a block's tokens
+    int row_blocks, parts;         // blocks of a KV head's query rows; workgroups that share a block's tokens
     float *state;                  // partial results, parts > 1
 };
-// Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32.
-inline int tree_block_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
+// The stored formats of the package's configurations and of the paper's presets, and their neighbours in group size: X(rounds,
+// groups per token, E4M3 scales, 4-bit levels, smoothing stages).  They have kernels of their own; any other one is decoded
+// element by element (one token over 12 heads x 187200 tokens: 125 us in the packed form of two rounds, 1.2 ms so).
+#define QVG_TREE_FORMATS(X)                                                                                              \
+    X(1, 2, true, false, 1) X(1, 8, true, false, 1) X(1, 8, true, false, 4) X(1, 2, true, true, 1) X(1, 8, true, true, 4) \
+    X(1, 2, false, false, 1) X(2, 2, false, false, 1) X(2, 4, false, false, 1) X(3, 2, false, false, 1)                   \
+    X(3, 4, false, false, 1) X(4, 2, false, false, 1) X(4, 4, false, false, 1)
+inline bool tree_packed(int T, int G, int fmt, int S) {
+#define QVG_TREE_IS(t, g, fp8, i4, s) if (T == t && G == g && S == s && fmt == ((fp8 ? kFmtE4M3 : 0) | (i4 ? kFmtInt4 : 0))) return true;
+    QVG_TREE_FORMATS(QVG_TREE_IS)
+#undef QVG_TREE_IS
+    return false;
+}
+// Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32, in the packed formats up to 128: a wavefront holds 32 rows
+// at most, and several of them share what they decode.
+inline int tree_block_rows(int64_t rows, bool packed) { return rows <= 16 ? 16 : rows <= 32 || !packed ? 32 : rows <= 64 ? 64 : 128; }
 struct TreePlan { int row_blocks, parts; size_t state_bytes; };
-TreePlan tree_plan(int H, const qvg_tree_step &t);
+TreePlan tree_plan(const qvg_params &p, const qvg_tree_step &t);
+hipError_t launch_tree_packed(const TreeArgs &a, int blocks, int block_rows, hipStream_t s);
+hipError_t launch_tree_wide(const TreeArgs &a, int blocks, int block_rows, hipStream_t s);
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s);
 
 hipError_t launch_tree_mask(int n_seqs, int n_nodes, const int32_t *parents, const int32_t *nodes, uint32_t *mask, int32_t *depth,
