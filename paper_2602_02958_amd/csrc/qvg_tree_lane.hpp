@@ -245,6 +245,34 @@ struct TreeLane {
             for (int i = 0; i < 4; ++i) row[hf][i] = load16(cent, off + (AS_RESIDUAL ? 16 : 64) * i);
         }
     }
+    // All stages' rows of token 16 hf + c, its 32 channels 32 kb + .., and their sum in fp32
+    __device__ __forceinline__ void gather_half(const Where &x, int hf, uint4 (&row)[S][4]) const {
+        const bf16_t *cent = ks.cent + x.page * S * a.K * kHeadDim;
+#pragma unroll
+        for (int st = 0; st < S; ++st) {
+            const uint32_t off = offs[st * kTrTile + 16 * hf + c] + 64 * kb;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row[st][i] = load16(cent, off + 16 * i);
+        }
+    }
+    __device__ __forceinline__ void sum_rows(const uint4 (&row)[S][4], float (&v)[32]) const {
+#pragma unroll
+        for (int st = 0; st < S; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float x[8];
+                unpack_bf16x8(row[st][i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[8 * i + e] = st ? v[8 * i + e] + x[e] : x[e];
+            }
+    }
+    // the (cos, sin) pairs of that token and these channels
+    __device__ __forceinline__ void gather_rope(const Where &x, int hf, uint4 (&rp)[4]) const {
+        const int64_t at = min((int64_t)x.page_index * L + x.first + min(16 * hf + c, x.count - 1), a.t.rope_tokens - 1);
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const f16_t *>(a.t.k_rope_f16) + at * kHeadDim + 32 * kb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rp[i] = p[i];
+    }
     // Octet c of the rows of tokens 4 kb + r and 16 + 4 kb + r
     __device__ __forceinline__ void gather_v(const Where &x, int st, uint4 (&row)[8]) const {
         const bf16_t *cent = vs.cent + x.page * S * a.K * kHeadDim;
@@ -282,32 +310,31 @@ struct TreeLane {
         }
         out = make_uint4(as_bits(r[0]), as_bits(r[1]), as_bits(r[2]), as_bits(r[3]));
     }
-    // K_hat rotated, as fragments of the residual's order: rows and residual meet in fp32 (v: the rows' sums of the 32 channels)
-    __device__ __forceinline__ void rotated_k(const Where &x, int hf, const uint4 (&res)[4], float (&v)[32], uint4 (&out)[4]) const {
-        const qvg_tree_step &t = a.t;
-        const int64_t at = min((int64_t)x.page_index * L + x.first + min(16 * hf + c, x.count - 1), t.rope_tokens - 1);
-        const uint4 *rp = reinterpret_cast<const uint4 *>(static_cast<const f16_t *>(t.k_rope_f16) + at * kHeadDim + 32 * kb);
-    #pragma unroll
+    // K_hat as fragments of the residual's order, rotated if ROPE: the rows' sums v and the residual meet in fp32
+    template <bool ROPE>
+    __device__ __forceinline__ void whole_k(const Raw &f, int hf, float (&v)[32], const uint4 (&rp)[4], uint4 (&out)[4]) const {
+        const halfx2_t none[4] = {};
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t rw[4] = {res[i].x, res[i].y, res[i].z, res[i].w};
+            uint4 res;
+            residual_k<false>(f, hf, i, none, res);
+            const uint32_t rw[4] = {res.x, res.y, res.z, res.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int ca = channel(i, e), cb = ca + pair_step;
                 const halfx2_t r2 = as_half2(rw[e]);
-                v[ca] += (float)r2[0];
-                v[cb] += (float)r2[1];
+                v[channel(i, e)] += (float)r2[0];
+                v[channel(i, e) + pair_step] += (float)r2[1];
             }
         }
+        if (ROPE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rotate_octet(v + 8 * i, rp[i]);
+            for (int i = 0; i < 4; ++i) rotate_octet(v + 8 * i, rp[i]);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t x4[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int ca = channel(i, e), cb = ca + pair_step;
-                x4[e] = pack_f16x2_rne(v[ca], v[cb]);
-            }
+            for (int e = 0; e < 4; ++e) x4[e] = pack_f16x2_rne(v[channel(i, e)], v[channel(i, e) + pair_step]);
             out[i] = make_uint4(x4[0], x4[1], x4[2], x4[3]);
         }
     }

@@ -213,7 +213,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             D.park(f, kTable ? kRows * 4 : kHeadDim * 2);
             D.order_lds();
             uint4 krow[2][4], vrow[8];
-            if (!kTable) D.template gather_k<ROPE>(cur, 0, krow);
+            if (!kTable && !ROPE) D.template gather_k<false>(cur, 0, krow);
             const bool more = ti + kTrWaves < stop;                      // uniform
             Where nxt = cur;
             if (more) {
@@ -229,35 +229,21 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             };
             if (kTable) scores_of_ids(); else R.clear_scores();
             if (ROPE) {
-                uint4 res[2][4];
+                uint4 row[S][4], rp[2][4], kf[2][4];
+                D.gather_half(cur, 0, row);
+                D.gather_rope(cur, 0, rp[0]);
+                D.gather_rope(cur, 1, rp[1]);
 #pragma unroll
-                for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) D.template residual_k<false>(f, hf, i, none, res[hf][i]);
-                if (S == 1) ahead();
-                float cen[2][32];
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) unpack_bf16x8(krow[hf][i], cen[hf] + 8 * i);
-                for (int st = 1; st < S; ++st) {
-                    D.template gather_k<ROPE>(cur, st, krow);
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float x[8];
-                            unpack_bf16x8(krow[hf][i], x);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) cen[hf][8 * i + e] += x[e];
-                        }
+                for (int hf = 0; hf < 2; ++hf) {
+                    float v[32];
+                    D.sum_rows(row, v);
+                    if (hf == 0) D.gather_half(cur, 1, row);
+                    D.template whole_k<true>(f, hf, v, rp[hf], kf[hf]);
                 }
-                uint4 rot[2][4];
-                if (S > 1) ahead();
-                D.rotated_k(cur, 0, res[0], cen[0], rot[0]);
-                D.rotated_k(cur, 1, res[1], cen[1], rot[1]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) scores_of_residual(i, rot[0][i], rot[1][i]);
+                for (int i = 0; i < 4; ++i) scores_of_residual(i, kf[0][i], kf[1][i]);
+                __builtin_amdgcn_sched_barrier(0);
+                ahead();
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -269,7 +255,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                 if (!kTable) {
                     scores_of_rows(krow);
                     for (int st = 1; st < S; ++st) {
-                        D.template gather_k<ROPE>(cur, st, krow);
+                        D.template gather_k<false>(cur, st, krow);
                         scores_of_rows(krow);
                     }
                 }

@@ -75,8 +75,7 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
         if (ti < stop) {
             D.park(f, kHeadDim * 2);
             D.order_lds();
-            uint4 krow[2][4], vrow[8];
-            D.template gather_k<true>(cur, 0, krow);
+            uint4 vrow[8];
             const bool more = ti + kTrWaves < stop;                      // uniform
             typename Lane::Where nxt = cur;
             if (more) {
@@ -85,48 +84,23 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
                 nxt = D.place(pi, in_page, cur);
             }
             if (ROPE || S > 1) {                                         // rows and residual meet in fp32
+                uint4 row[S][4], rp[2][4];
+                D.gather_half(cur, 0, row);
+                if (ROPE) { D.gather_rope(cur, 0, rp[0]); D.gather_rope(cur, 1, rp[1]); }
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
-                    const halfx2_t none[4] = {};
                     float v[32];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) unpack_bf16x8(krow[hf][i], v + 8 * i);
-                    for (int st = 1; st < S; ++st) {
-                        uint4 row[4];
-                        const uint32_t off = D.offs[st * kTrTile + 16 * hf + c] + 64 * kb;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) row[i] = D.load16(D.ks.cent + cur.page * S * a.K * kHeadDim, off + 16 * i);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float x[8];
-                            unpack_bf16x8(row[i], x);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[8 * i + e] += x[e];
-                        }
-                    }
-                    uint4 res[4], out[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) D.template residual_k<false>(f, hf, i, none, res[i]);
-                    if (ROPE) D.rotated_k(cur, hf, res, v, out);
-                    else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t rw[4] = {res[i].x, res[i].y, res[i].z, res[i].w};
-                            uint32_t x4[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int ca = Lane::channel(i, e);
-                                const halfx2_t r2 = as_half2(rw[e]);
-                                x4[e] = pack_f16x2_rne(v[ca] + (float)r2[0], v[ca + Lane::pair_step] + (float)r2[1]);
-                            }
-                            out[i] = make_uint4(x4[0], x4[1], x4[2], x4[3]);
-                        }
-                    }
+                    uint4 out[4];
+                    D.sum_rows(row, v);
+                    if (hf == 0) D.gather_half(cur, 1, row);
+                    else D.gather_v(cur, 0, vrow);
+                    D.template whole_k<ROPE>(f, hf, v, rp[hf], out);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mine[(hf * 4 + i) * 64] = out[i];
                 }
-                D.gather_v(cur, 0, vrow);
             } else {
+                uint4 krow[2][4];
+                D.template gather_k<true>(cur, 0, krow);
                 D.gather_v(cur, 0, vrow);
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
@@ -142,7 +116,6 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
             // (the loads that this tile still needs are asked for; the next tile's have the rest of the round to arrive)
             typename Lane::Levels lv;
             D.read_levels(lv);
-            uint4 more_rows[S > 1 ? 8 : 1];
             halfx2_t sum[S > 1 ? 8 : 1][4];
             if (S > 1) {
 #pragma unroll
@@ -157,7 +130,6 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
                         for (int pr = 0; pr < 4; ++pr) sum[S > 1 ? j : 0][pr] += D.pair_f16(vrow[2 * pr], vrow[2 * pr + 1], j);
                 }
             }
-            (void)more_rows;
             D.order_lds();                                               // (staging is read before the fragments go over it)
             if (more) D.fetch(nxt, f);
 #pragma unroll
