@@ -55,11 +55,13 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
     // workgroups are dealt to the 8 XCDs round-robin: the parts of one KV head run on one, whose L2 then keeps its tables
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const int part = w % a.parts, rblk = w / a.parts % a.row_blocks, bh = w / a.parts / a.row_blocks;
+    const BlockPlace at = place_block(a, w, a.t.k_rope_f16 != nullptr);
+    const int part = at.part, rblk = at.rblk, bh = at.bh;
     const int b = bh / a.H, h = bh - b * a.H;
     const qvg_tree_step &t = a.t;
     const SeqTiles sq = tiles_of_sequence(t, b);
-    const int lo = (int)((int64_t)sq.total * part / a.parts), hi = (int)((int64_t)sq.total * (part + 1) / a.parts);
+    const PartTiles pt = tiles_of_part(a, sq, part);
+    const int hi = pt.hi;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
     const int64_t rows = (int64_t)t.group * t.n_nodes;
@@ -123,7 +125,7 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
         for (int j = 0; j < 8; ++j) O[rb][j] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    for (int ti = lo + wave; ti < hi; ti += kTrWaves) {
+    for (int ti = pt.first + wave; ti < hi; ti += pt.step) {
         // the tile: its first token (in the page, the tail or the new tokens) and how many it has
         int kind = 0, first, count;
         int64_t page = 0, pool_tok = 0;
@@ -297,7 +299,7 @@ static bool packed_format(const qvg_params &p) {
                        p.n_smooth_stages);
 }
 TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t) {
-    TreePlan p{1, 1, 0};
+    TreePlan p{1, 1, 1, 0};
     const int64_t rows = (int64_t)t.group * t.n_nodes;
     const int br = tree_block_rows(rows, packed_format(prm));
     p.row_blocks = (int)((rows + br - 1) / br);
@@ -310,6 +312,9 @@ TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t) {
     const int64_t most = tiles / (2 * kTrWaves);
     if (parts > most) parts = most;
     if (parts > 1) {
+#ifdef SHARE
+        p.share = parts >= 2 * SHARE ? SHARE : 1; parts = parts / p.share * p.share;
+#endif
         p.parts = (int)parts;
         p.state_bytes = (size_t)units * parts * tree_state_floats(br) * sizeof(float);
     }

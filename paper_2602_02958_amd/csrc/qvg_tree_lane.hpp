@@ -54,6 +54,30 @@ __device__ __forceinline__ halfx8_t pack_f16x8(const float *v) {
                                                    pack_f16x2_rne(v[4], v[5]), pack_f16x2_rne(v[6], v[7])));
 }
 
+// A workgroup's part, row block, and sequence and head, from its number on its XCD (consecutive numbers run on one): the parts
+// of one head together, whose pages' tables the L2 keeps, or with a rotation the same parts of all heads, which read the same
+// rows of its table at about the same time.
+struct BlockPlace { int part, rblk, bh; };
+__device__ __forceinline__ BlockPlace place_block(const TreeArgs &a, int w, bool rotated) {
+    const int units = a.t.n_seqs * a.H * a.row_blocks;
+    BlockPlace p;
+    const int unit = rotated ? w % units : w / a.parts;
+    p.part = rotated ? w / units : w % a.parts;
+    p.rblk = unit % a.row_blocks; p.bh = unit / a.row_blocks;
+    return p;
+}
+
+// The tiles of a part: range [lo, hi), of which the part's wavefronts take first, first + step, .. (a round of kTrWaves each).
+// Parts that share a range walk it together: the tables of its pages, which they gather rows from, then stay in their XCD's L2.
+struct PartTiles { int lo, hi, first, step; };
+__device__ __forceinline__ PartTiles tiles_of_part(const TreeArgs &a, const SeqTiles &sq, int part) {
+    const int groups = a.parts / a.share, g = part / a.share;
+    PartTiles p;
+    p.lo = (int)((int64_t)sq.total * g / groups); p.hi = (int)((int64_t)sq.total * (g + 1) / groups);
+    p.first = p.lo + (part - g * a.share) * kTrWaves; p.step = a.share * kTrWaves;
+    return p;
+}
+
 // Where a query row of the batch lies: head h * group + r / n_nodes, node r % n_nodes.
 struct RowPlace { int64_t head; int node; };
 __device__ __forceinline__ RowPlace place_row(const TreeArgs &a, int h, int64_t r) {

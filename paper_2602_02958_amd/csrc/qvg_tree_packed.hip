@@ -34,11 +34,13 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     __shared__ float ms[kTrWaves][kRows], ls[kTrWaves][kRows];
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const int part = w % a.parts, rblk = w / a.parts % a.row_blocks, bh = w / a.parts / a.row_blocks;
+    const BlockPlace at = place_block(a, w, ROPE);
+    const int part = at.part, rblk = at.rblk, bh = at.bh;
     const int b = bh / a.H, h = bh - b * a.H;
     const qvg_tree_step &t = a.t;
     const SeqTiles sq = tiles_of_sequence(t, b);
-    const int lo = (int)((int64_t)sq.total * part / a.parts), hi = (int)((int64_t)sq.total * (part + 1) / a.parts);
+    const PartTiles pt = tiles_of_part(a, sq, part);
+    const int hi = pt.hi;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
     uint4 *qlds = reinterpret_cast<uint4 *>(smem);                       // [RB][8][64] fragments
@@ -191,8 +193,8 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
 
     const halfx2_t none[4] = {};
     const int stop = min(hi, sq.kv_tiles);
-    if (lo < stop) {                                                     // uniform over the workgroup
-        int ti = lo + wave, pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
+    if (pt.lo < stop) {                                                     // uniform over the workgroup
+        int ti = pt.first + wave, pi = ti / sq.per_page, in_page = ti - pi * sq.per_page;
         Where cur{-1, 0, 0, 0, 0};
         Raw f;
         if (ti < stop) {
@@ -201,7 +203,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
         }
         // page by page; a wavefront without tiles in a page still helps with its table
         Where held{-1, 0, 0, 0, 0};
-        for (int pg = lo / sq.per_page; pg * sq.per_page < stop; ++pg) {
+        for (int pg = pt.lo / sq.per_page; pg * sq.per_page < stop; ++pg) {
             if (kTable) {
                 held = D.place(pg, 0, held);
                 __syncthreads();
@@ -214,30 +216,37 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             D.order_lds();
             uint4 krow[2][4], vrow[8];
             if (!kTable && !ROPE) D.template gather_k<false>(cur, 0, krow);
-            const bool more = ti + kTrWaves < stop;                      // uniform
+            const bool more = ti + pt.step < stop;                      // uniform
             Where nxt = cur;
             if (more) {
-                in_page += kTrWaves;
+                in_page += pt.step;
                 while (in_page >= sq.per_page) { in_page -= sq.per_page; ++pi; }
                 nxt = D.place(pi, in_page, cur);
             }
             // The load counter is in order: the rows that this tile still needs are asked for before the next tile's data, which
             // then has the rest of the tile to arrive
+            // (rows of V: at once where all of a tile's rows fit the registers)
+            constexpr bool kEarlyV = S == 1;
             auto ahead = [&]() {
-                D.gather_v(cur, 0, vrow);
+                if (!kEarlyV) D.gather_v(cur, 0, vrow);
                 if (more) D.fetch(nxt, f);
             };
-            if (kTable) scores_of_ids(); else R.clear_scores();
+            uint4 kh[2][S][4], rp[2][4];
             if (ROPE) {
-                uint4 row[S][4], rp[2][4], kf[2][4];
-                D.gather_half(cur, 0, row);
+                D.gather_half(cur, 0, kh[0]);
                 D.gather_rope(cur, 0, rp[0]);
                 D.gather_rope(cur, 1, rp[1]);
+                if (S == 1) D.gather_half(cur, 1, kh[1]);
+            }
+            if (kEarlyV) D.gather_v(cur, 0, vrow);
+            if (kTable) scores_of_ids(); else R.clear_scores();
+            if (ROPE) {
+                uint4 kf[2][4];
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
                     float v[32];
-                    D.sum_rows(row, v);
-                    if (hf == 0) D.gather_half(cur, 1, row);
+                    D.sum_rows(kh[S == 1 ? hf : 0], v);
+                    if (S > 1 && hf == 0) D.gather_half(cur, 1, kh[0]);
                     D.template whole_k<true>(f, hf, v, rp[hf], kf[hf]);
                 }
 #pragma unroll
@@ -297,14 +306,16 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                 add_residual([&](int j, int pr) { return sum[j][pr]; });
             }
             D.order_lds();
-            ti += kTrWaves;
+            ti += pt.step;
             cur = nxt;
             }
         }
     }
 
     // ---- the tail's and the new tokens' tiles ---------------------------------------------------
-    for (int ti = max(lo, sq.kv_tiles) + wave; ti < hi; ti += kTrWaves) {
+    int tail_at = pt.first + wave;
+    if (tail_at < sq.kv_tiles) tail_at += (sq.kv_tiles - tail_at + pt.step - 1) / pt.step * pt.step;
+    for (int ti = tail_at; ti < hi; ti += pt.step) {
         const bool fresh = ti >= sq.kv_tiles + sq.tail_tiles;
         const int first = (ti - sq.kv_tiles - (fresh ? sq.tail_tiles : 0)) * kTrTile;
         const int count = min(kTrTile, (fresh ? sq.nodes : sq.tail) - first);

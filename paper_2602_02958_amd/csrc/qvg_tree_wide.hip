@@ -23,11 +23,13 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
     __shared__ int tile_first[kTrWaves], tile_count[kTrWaves];           // first: of a tile of new tokens, else -1
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const int part = w % a.parts, rblk = w / a.parts % a.row_blocks, bh = w / a.parts / a.row_blocks;
+    const BlockPlace at = place_block(a, w, ROPE);
+    const int part = at.part, rblk = at.rblk, bh = at.bh;
     const int b = bh / a.H, h = bh - b * a.H;
     const qvg_tree_step &t = a.t;
     const SeqTiles sq = tiles_of_sequence(t, b);
-    const int lo = (int)((int64_t)sq.total * part / a.parts), hi = (int)((int64_t)sq.total * (part + 1) / a.parts);
+    const PartTiles pt = tiles_of_part(a, sq, part);
+    const int hi = pt.hi;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4, rs = wave % RS, ts = wave / RS;
     const int64_t row0 = (int64_t)rblk * kRows;
@@ -54,8 +56,8 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
     typename Lane::Where cur{-1, 0, 0, 0, 0};
     typename Lane::Raw f;
     const int stop = min(hi, sq.kv_tiles);
-    int pi = (lo + wave) / sq.per_page, in_page = lo + wave - pi * sq.per_page;
-    if (lo + wave < stop) {
+    int pi = (pt.first + wave) / sq.per_page, in_page = pt.first + wave - pi * sq.per_page;
+    if (pt.first + wave < stop) {
         cur = D.place(pi, in_page, cur);
         D.fetch(cur, f);
     }
@@ -69,17 +71,17 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
         }
     };
 
-    for (int r0 = lo; r0 < hi; r0 += kTrWaves) {
+    for (int r0 = pt.first; r0 < hi; r0 += pt.step) {
         // ---- decode: the wavefront's tile -------------------------------------------------------
         const int ti = r0 + wave;
         if (ti < stop) {
             D.park(f, kHeadDim * 2);
             D.order_lds();
             uint4 vrow[8];
-            const bool more = ti + kTrWaves < stop;                      // uniform
+            const bool more = ti + pt.step < stop;                      // uniform
             typename Lane::Where nxt = cur;
             if (more) {
-                in_page += kTrWaves;
+                in_page += pt.step;
                 while (in_page >= sq.per_page) { in_page -= sq.per_page; ++pi; }
                 nxt = D.place(pi, in_page, cur);
             }
