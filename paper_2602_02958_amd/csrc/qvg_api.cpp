@@ -709,8 +709,8 @@ int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t, const void *k_cen
     a.fmt = format_of(p); a.id_wide = id_wide(p); a.t = *t; a.scale = softmax_scale;
     const TreePlan plan = tree_plan(*p, *t);
     a.row_blocks = plan.row_blocks;
-    a.parts = scratch && scratch_bytes >= plan.state_bytes ? plan.parts : 1;
-    a.share = a.parts > 1 ? plan.share : 1;
+    a.slots = scratch && scratch_bytes >= plan.state_bytes ? plan.slots : 0;
+    a.share = plan.share;
     a.state = static_cast<float *>(scratch);
     return launch_attn_tree(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
 }

@@ -55,12 +55,12 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
     // workgroups are dealt to the 8 XCDs round-robin: the parts of one KV head run on one, whose L2 then keeps its tables
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const BlockPlace at = place_block(a, w, a.t.k_rope_f16 != nullptr);
-    const int part = at.part, rblk = at.rblk, bh = at.bh;
-    const int b = bh / a.H, h = bh - b * a.H;
+    const BlockPlace at = place_block(a, w, a.t.k_rope_f16 != nullptr, kRows);
+    if (at.parts == 0) return;                                           // uniform, before any barrier
+    const int b = at.b, h = at.h, rblk = at.rblk;
     const qvg_tree_step &t = a.t;
     const SeqTiles sq = tiles_of_sequence(t, b);
-    const PartTiles pt = tiles_of_part(a, sq, part);
+    const PartTiles pt = tiles_of_part(a, sq, at.part, at.parts);
     const int hi = pt.hi;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
@@ -245,7 +245,7 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
         }
     }
 
-    finish_block<RB>(a, b, h, bh, rblk, part, sq.nodes, meet, ms, ls, O, m, l);
+    finish_block<RB>(a, at, sq.nodes, meet, ms, ls, O, m, l);
 }
 
 // Joins a query row's parts: a workgroup to a row, 16 lanes (8 channels each) to a part, so that 16 parts are read at a time.
@@ -255,20 +255,20 @@ void tree_join_kernel(TreeArgs a, int block_rows) {
     const int64_t rows = (int64_t)a.t.group * a.t.n_nodes;
     const int64_t bh = (int64_t)(blockIdx.x / (unsigned)rows), r = (int64_t)blockIdx.x - bh * rows;
     const int b = (int)(bh / a.H), h = (int)(bh - (int64_t)b * a.H);
-    const int64_t block = bh * a.row_blocks + r / block_rows;
     const int row = (int)(r % block_rows), grp = threadIdx.x >> 4, c8 = threadIdx.x & 15;
     const int step = (int)tree_state_floats(block_rows);
-    const float *st = a.state + block * a.parts * step;
+    const SlotPlace at = place_slot(a, b, true);
+    const float *st = a.state + (((int64_t)h * a.row_blocks + r / block_rows) * a.slots + at.first) * step;
     const float *mp = st + block_rows * kHeadDim + row, *lp = mp + block_rows, *op = st + row * kHeadDim + c8 * 8;
     float m = kTrNoScore, l = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
     // every lane finds the maximum over all parts: lane i of 64 looks at parts i, i + 64, ..
-    for (int p = threadIdx.x & 63; p < a.parts; p += 64) m = fmaxf(m, mp[(int64_t)p * step]);
+    for (int p = threadIdx.x & 63; p < at.parts; p += 64) m = fmaxf(m, mp[(int64_t)p * step]);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
 #pragma unroll 4
-    for (int p = grp; p < a.parts; p += 16) {
+    for (int p = grp; p < at.parts; p += 16) {
         const float f = __builtin_amdgcn_exp2f(mp[(int64_t)p * step] - m);
         const float4 x = *reinterpret_cast<const float4 *>(op + (int64_t)p * step), y = *reinterpret_cast<const float4 *>(op + (int64_t)p * step + 4);
         l += lp[(int64_t)p * step] * f;
@@ -299,24 +299,26 @@ static bool packed_format(const qvg_params &p) {
                        p.n_smooth_stages);
 }
 TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t) {
-    TreePlan p{1, 1, 1, 0};
+    TreePlan p{1, 0, 1, 0};
     const int64_t rows = (int64_t)t.group * t.n_nodes;
     const int br = tree_block_rows(rows, packed_format(prm));
     p.row_blocks = (int)((rows + br - 1) / br);
-    const int64_t units = (int64_t)t.n_seqs * prm.n_heads * p.row_blocks;
-    if (units < 1) return p;
+    const int64_t units = (int64_t)prm.n_heads * p.row_blocks;           // of a sequence
+    if (t.n_seqs < 1 || rows < 1) return p;
     const int64_t tiles = t.table_pages * ((t.page_len + kTrTile - 1) / kTrTile) + (t.tail_capacity + kTrTile - 1) / kTrTile +
                           (t.n_nodes + kTrTile - 1) / kTrTile;
-    // as many workgroups as the chip holds at once (two to a CU), two tiles to a wavefront at least
-    int64_t parts = 512 / units;
-    const int64_t most = tiles / (2 * kTrWaves);
-    if (parts > most) parts = most;
-    if (parts > 1) {
-#ifdef SHARE
-        p.share = parts >= 2 * SHARE ? SHARE : 1; parts = parts / p.share * p.share;
-#endif
-        p.parts = (int)parts;
-        p.state_bytes = (size_t)units * parts * tree_state_floats(br) * sizeof(float);
+    // As many workgroups as the chip holds at once (two to a CU), two tiles to a wavefront at least; not divided where that is
+    // less than two workgroups to a sequence
+    int64_t slots = 512 / units;
+    const int64_t most = t.n_seqs * (tiles / (2 * kTrWaves));
+    if (slots > most) slots = most;
+    if (slots >= 2 * (int64_t)t.n_seqs) {
+        p.slots = (int)slots;
+        p.state_bytes = (size_t)(units * slots * tree_state_floats(br)) * sizeof(float);
+        // Several smoothing stages' rows gathered for both sides (with a rotation, or beyond 16 rows) are more than an XCD's L2
+        // holds for 64 workgroups in pages of their own: 12 heads x 187200 tokens, four stages, 736 -> 560 us rotated, 32 rows
+        // 528 -> 435 us.  Elsewhere sharing costs more tables than it saves (one token, one round: 92 -> 114 us).
+        if (prm.n_smooth_stages > 1 && (t.k_rope_f16 || rows > 16)) p.share = 8;
     }
     return p;
 }
@@ -334,8 +336,7 @@ static void launch_fmt(const TreeArgs &a, int blocks, int block_rows, hipStream_
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     const bool packed = tree_packed(a.T, kHeadDim / a.B, a.fmt, a.S);
     const int br = tree_block_rows((int64_t)a.t.group * a.t.n_nodes, packed);
-    const int64_t units = (int64_t)a.t.n_seqs * a.H * a.row_blocks;
-    const int blocks = (int)(units * a.parts);
+    const int blocks = (int)((int64_t)(a.slots ? a.slots : a.t.n_seqs) * a.H * a.row_blocks);
     hipError_t e = hipSuccess;
     if (packed) e = br > 32 ? launch_tree_wide(a, blocks, br, s) : launch_tree_packed(a, blocks, br, s);
     else switch (a.fmt) {
@@ -345,7 +346,7 @@ hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
         default: launch_fmt<kFmtE4M3 | kFmtInt4>(a, blocks, br, s); break;
     }
     if (e != hipSuccess) return e;
-    if (a.parts > 1) {
+    if (a.slots) {
         const int64_t n = (int64_t)a.t.n_seqs * a.H * a.t.group * a.t.n_nodes;
         tree_join_kernel<<<dim3((unsigned)n), dim3(256), 0, s>>>(a, br);
     }

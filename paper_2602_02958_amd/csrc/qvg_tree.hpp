@@ -13,9 +13,10 @@ struct TreeArgs {
     int H, K, B, T, S, fmt, id_wide;
     qvg_tree_step t;
     float scale;
-    int row_blocks, parts;         // blocks of a KV head's query rows; workgroups that share a block's tokens
-    int share;                     // consecutive parts that walk the same range of tiles together, a round each in turn (divides parts)
-    float *state;                  // partial results, parts > 1
+    int row_blocks;                // blocks of a KV head's query rows
+    int slots;                     // workgroups of a block of all sequences, dealt to them by their lengths; 0: one to each, undivided
+    int share;                     // consecutive parts of a sequence that walk the same range of tiles together, a round each in turn
+    float *state;                  // partial results of the slots
 };
 // The stored formats of the package's configurations and of the paper's presets, and their neighbours in group size: X(rounds,
 // groups per token, E4M3 scales, 4-bit levels, smoothing stages).  They have kernels of their own; any other one is decoded
@@ -33,7 +34,7 @@ inline bool tree_packed(int T, int G, int fmt, int S) {
 // Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32, in the packed formats up to 128: a wavefront holds 32 rows
 // at most, and several of them share what they decode.
 inline int tree_block_rows(int64_t rows, bool packed) { return rows <= 16 ? 16 : rows <= 32 || !packed ? 32 : rows <= 64 ? 64 : 128; }
-struct TreePlan { int row_blocks, parts, share; size_t state_bytes; };
+struct TreePlan { int row_blocks, slots, share; size_t state_bytes; };
 TreePlan tree_plan(const qvg_params &p, const qvg_tree_step &t);
 hipError_t launch_tree_packed(const TreeArgs &a, int blocks, int block_rows, hipStream_t s);
 hipError_t launch_tree_wide(const TreeArgs &a, int blocks, int block_rows, hipStream_t s);

@@ -54,27 +54,85 @@ __device__ __forceinline__ halfx8_t pack_f16x8(const float *v) {
                                                    pack_f16x2_rne(v[4], v[5]), pack_f16x2_rne(v[6], v[7])));
 }
 
-// A workgroup's part, row block, and sequence and head, from its number on its XCD (consecutive numbers run on one): the parts
-// of one head together, whose pages' tables the L2 keeps, or with a rotation the same parts of all heads, which read the same
-// rows of its table at about the same time.
-struct BlockPlace { int part, rblk, bh; };
-__device__ __forceinline__ BlockPlace place_block(const TreeArgs &a, int w, bool rotated) {
-    const int units = a.t.n_seqs * a.H * a.row_blocks;
+// A block's partial result: [rows][128] sums, then the rows' references, then their sums of weights.
+__host__ __device__ inline int64_t tree_state_floats(int rows) { return (int64_t)rows * (kHeadDim + 2); }
+
+// How the slots of a divided call (a.slots of them, the same for every head and row block) are dealt to the sequences: a slot
+// for every q tiles or part of them, and one at least, with q so large that the slots suffice: the sum of ceil(T / q) over n
+// sequences is at most total / q + n.  Every wavefront works that out for itself from the lengths, which only the device knows
+// (n <= 256: a call of more sequences is not divided).  Slots that are left over have nothing to do.
+struct SlotPlace { int b, part, parts, first; };                         // first: the sequence's first slot; parts: 0, none
+__device__ __forceinline__ int parts_of_sequence(const TreeArgs &a, int b, int q) {
+    const int total = tiles_of_sequence(a.t, b).total, p = (total + q - 1) / q;
+    return p < 1 ? 1 : p;
+}
+// The place of slot `slot`, or with by_sequence that of sequence `slot`'s first part.  Uniform over a wavefront.
+__device__ __forceinline__ SlotPlace place_slot(const TreeArgs &a, int slot, bool by_sequence) {
+    const int lane = threadIdx.x & 63, n = a.t.n_seqs;
+    int64_t total = 0;
+    for (int i = lane; i < n; i += 64) total += tiles_of_sequence(a.t, i).total;
+    if (n > 1) {
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) total += __shfl_xor(total, off, 64);
+    } else total = __shfl(total, 0, 64);
+    const int room = n > 1 ? a.slots - n : a.slots;
+    int q = (int)((total + room - 1) / room);
+    if (q < 2 * kTrWaves) q = 2 * kTrWaves;                              // two tiles to a wavefront
+    SlotPlace p{0, 0, 0, 0};
+    int before = 0;
+    for (int base = 0; base < n; base += 64) {                           // uniform
+        const int i = base + lane, mine = i < n ? parts_of_sequence(a, i, q) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const int x = __shfl_up(upto, off, 64);
+            if (lane >= off) upto += x;
+        }
+        upto += before;
+        const unsigned long long hit = __ballot(by_sequence ? i == slot : (mine > 0 && slot >= upto - mine && slot < upto));
+        if (hit) {
+            const int at = __builtin_ctzll(hit);
+            p.b = base + at; p.parts = __shfl(mine, at, 64); p.first = __shfl(upto, at, 64) - p.parts;
+            p.part = by_sequence ? 0 : slot - p.first;
+            break;
+        }
+        before = __shfl(upto, 63, 64);
+    }
+    p.b = __builtin_amdgcn_readfirstlane(p.b); p.part = __builtin_amdgcn_readfirstlane(p.part);
+    p.parts = __builtin_amdgcn_readfirstlane(p.parts); p.first = __builtin_amdgcn_readfirstlane(p.first);
+    if (a.share > 1 && p.parts >= 2 * a.share) p.parts = p.parts / a.share * a.share;       // whole groups
+    return p;
+}
+
+// A workgroup's sequence, head, row block and part, from its number on its XCD (consecutive numbers run on one): the parts of one
+// head together, whose pages' tables the L2 keeps, or with a rotation the same parts of all heads, which read the same rows of
+// its table at about the same time.  parts: 0 where there is nothing to do.
+struct BlockPlace { int b, h, rblk, part, parts; int64_t state; };       // state: floats of the part's place in a.state
+__device__ __forceinline__ BlockPlace place_block(const TreeArgs &a, int w, bool rotated, int block_rows) {
+    const int units = a.H * a.row_blocks;                                // of a sequence
     BlockPlace p;
-    const int unit = rotated ? w % units : w / a.parts;
-    p.part = rotated ? w / units : w % a.parts;
-    p.rblk = unit % a.row_blocks; p.bh = unit / a.row_blocks;
+    if (a.slots == 0) {
+        p.b = w / units; p.part = 0; p.parts = 1; p.state = 0;
+        const int unit = w - p.b * units;
+        p.rblk = unit % a.row_blocks; p.h = unit / a.row_blocks;
+        return p;
+    }
+    const int unit = rotated ? w % units : w / a.slots, slot = rotated ? w / units : w % a.slots;
+    const SlotPlace s = place_slot(a, slot, false);
+    p.b = s.b; p.part = s.part; p.parts = s.part < s.parts ? s.parts : 0;
+    p.rblk = unit % a.row_blocks; p.h = unit / a.row_blocks;
+    p.state = ((int64_t)unit * a.slots + slot) * tree_state_floats(block_rows);
     return p;
 }
 
 // The tiles of a part: range [lo, hi), of which the part's wavefronts take first, first + step, .. (a round of kTrWaves each).
 // Parts that share a range walk it together: the tables of its pages, which they gather rows from, then stay in their XCD's L2.
 struct PartTiles { int lo, hi, first, step; };
-__device__ __forceinline__ PartTiles tiles_of_part(const TreeArgs &a, const SeqTiles &sq, int part) {
-    const int groups = a.parts / a.share, g = part / a.share;
+__device__ __forceinline__ PartTiles tiles_of_part(const TreeArgs &a, const SeqTiles &sq, int part, int parts) {
+    const int share = a.slots && parts >= 2 * a.share ? a.share : 1, groups = parts / share, g = part / share;
     PartTiles p;
     p.lo = (int)((int64_t)sq.total * g / groups); p.hi = (int)((int64_t)sq.total * (g + 1) / groups);
-    p.first = p.lo + (part - g * a.share) * kTrWaves; p.step = a.share * kTrWaves;
+    p.first = p.lo + (part - g * share) * kTrWaves; p.step = share * kTrWaves;
     return p;
 }
 
@@ -103,8 +161,6 @@ __device__ __forceinline__ void store_row8(const TreeArgs &a, int b, int h, int6
             seen ? (m + __builtin_log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// A block's partial result: [rows][128] sums, then the rows' references, then their sums of weights.
-__host__ __device__ inline int64_t tree_state_floats(int rows) { return (int64_t)rows * (kHeadDim + 2); }
 
 constexpr int kTrRowPitch = 36;                     // 16-bit words per row of 32 tokens (72 bytes: 8-byte aligned, spread over the banks)
 
@@ -510,7 +566,7 @@ struct QueryRow {
 // The wavefronts' results meet: O, m and l of each (m the same in a row's four lanes, l a lane's share), the block's result
 // to `state` or, undivided, to the output.  meet: [kTrWaves][16][kTrPitch] floats.
 template <int RB>
-__device__ __forceinline__ void finish_block(const TreeArgs &a, int b, int h, int bh, int rblk, int part, int nodes, float (*meet)[16][kTrPitch],
+__device__ __forceinline__ void finish_block(const TreeArgs &a, const BlockPlace &at, int nodes, float (*meet)[16][kTrPitch],
                                              float (*ms)[16 * RB], float (*ls)[16 * RB], const floatx4_t (&O)[RB][8], const float (&m)[RB], float (&l)[RB]) {
     constexpr int kRows = 16 * RB;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, kb = lane >> 4;
@@ -536,7 +592,7 @@ __device__ __forceinline__ void finish_block(const TreeArgs &a, int b, int h, in
                 *reinterpret_cast<float4 *>(&meet[wave][c][32 * kb + 8 * r + j]) =
                     make_float4(O[rb][j][r] * f, O[rb][j + 1][r] * f, O[rb][j + 2][r] * f, O[rb][j + 3][r] * f);
         __syncthreads();
-        const int64_t r = (int64_t)rblk * kRows + rb * 16 + row;
+        const int64_t r = (int64_t)at.rblk * kRows + rb * 16 + row;
         float o[8], mt = ms[0][rb * 16 + row], lt = 0.0f;
 #pragma unroll
         for (int v = 1; v < kTrWaves; ++v) mt = fmaxf(mt, ms[v][rb * 16 + row]);
@@ -548,13 +604,13 @@ __device__ __forceinline__ void finish_block(const TreeArgs &a, int b, int h, in
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] += meet[v][row][c8 * 8 + e];
         }
-        if (a.parts > 1) {
-            float *st = a.state + (((int64_t)bh * a.row_blocks + rblk) * a.parts + part) * tree_state_floats(kRows);
+        if (a.slots) {
+            float *st = a.state + at.state;
             float *op = st + (rb * 16 + row) * kHeadDim + c8 * 8;
             *reinterpret_cast<float4 *>(op) = make_float4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<float4 *>(op + 4) = make_float4(o[4], o[5], o[6], o[7]);
             if (c8 == 0) { st[kRows * kHeadDim + rb * 16 + row] = mt; st[kRows * (kHeadDim + 1) + rb * 16 + row] = lt; }
-        } else if (r < rows) store_row8(a, b, h, r, nodes, c8, o, mt, lt);
+        } else if (r < rows) store_row8(a, at.b, at.h, r, nodes, c8, o, mt, lt);
         if (rb + 1 < RB) __syncthreads();
     }
 }

@@ -34,12 +34,12 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     __shared__ float ms[kTrWaves][kRows], ls[kTrWaves][kRows];
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const BlockPlace at = place_block(a, w, ROPE);
-    const int part = at.part, rblk = at.rblk, bh = at.bh;
-    const int b = bh / a.H, h = bh - b * a.H;
+    const BlockPlace at = place_block(a, w, ROPE, kRows);
+    if (at.parts == 0) return;                                           // uniform, before any barrier
+    const int b = at.b, h = at.h, rblk = at.rblk;
     const qvg_tree_step &t = a.t;
     const SeqTiles sq = tiles_of_sequence(t, b);
-    const PartTiles pt = tiles_of_part(a, sq, part);
+    const PartTiles pt = tiles_of_part(a, sq, at.part, at.parts);
     const int hi = pt.hi;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
@@ -355,7 +355,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
         add_rows(vrow);
     }
     __syncthreads();                                                     // (the meeting place lies over the wavefronts' own LDS)
-    finish_block<RB>(a, b, h, bh, rblk, part, sq.nodes, reinterpret_cast<float (*)[16][kTrPitch]>(smem), ms, ls, R.o, R.m, R.l);
+    finish_block<RB>(a, at, sq.nodes, reinterpret_cast<float (*)[16][kTrPitch]>(smem), ms, ls, R.o, R.m, R.l);
 }
 
 template <class F, bool ROPE, int RB>

@@ -23,12 +23,12 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
     __shared__ int tile_first[kTrWaves], tile_count[kTrWaves];           // first: of a tile of new tokens, else -1
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const BlockPlace at = place_block(a, w, ROPE);
-    const int part = at.part, rblk = at.rblk, bh = at.bh;
-    const int b = bh / a.H, h = bh - b * a.H;
+    const BlockPlace at = place_block(a, w, ROPE, kRows);
+    if (at.parts == 0) return;                                           // uniform, before any barrier
+    const int b = at.b, h = at.h, rblk = at.rblk;
     const qvg_tree_step &t = a.t;
     const SeqTiles sq = tiles_of_sequence(t, b);
-    const PartTiles pt = tiles_of_part(a, sq, part);
+    const PartTiles pt = tiles_of_part(a, sq, at.part, at.parts);
     const int hi = pt.hi;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4, rs = wave % RS, ts = wave / RS;
@@ -242,7 +242,7 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
     __syncthreads();
     const int row = tid >> 4, c8 = tid & 15;
     const int64_t rows = (int64_t)t.group * t.n_nodes;
-    float *st = a.state + (((int64_t)bh * a.row_blocks + rblk) * a.parts + part) * tree_state_floats(kRows);
+    float *st = a.state + at.state;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         float mm = ms[rs][rb * 16 + c];
@@ -258,7 +258,7 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < RS; ++g) {                                   // the rows of wavefronts g, g + RS, ..
-            const int at = g * 32 + rb * 16 + row;                       // in the block
+            const int br = g * 32 + rb * 16 + row;                       // in the block
             float o[8], mt = ms[g][rb * 16 + row], lt = 0.0f;
 #pragma unroll
             for (int v = 1; v < TS; ++v) mt = fmaxf(mt, ms[g + v * RS][rb * 16 + row]);
@@ -270,12 +270,12 @@ void tree_attn_wide(TreeArgs a, int blocks, int per_xcd) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] += meet[g + v * RS][row][c8 * 8 + e];
             }
-            if (a.parts > 1) {
-                float *op = st + at * kHeadDim + c8 * 8;
+            if (a.slots) {
+                float *op = st + br * kHeadDim + c8 * 8;
                 *reinterpret_cast<float4 *>(op) = make_float4(o[0], o[1], o[2], o[3]);
                 *reinterpret_cast<float4 *>(op + 4) = make_float4(o[4], o[5], o[6], o[7]);
-                if (c8 == 0) { st[kRows * kHeadDim + at] = mt; st[kRows * (kHeadDim + 1) + at] = lt; }
-            } else if (row0 + at < rows) store_row8(a, b, h, row0 + at, sq.nodes, c8, o, mt, lt);
+                if (c8 == 0) { st[kRows * kHeadDim + br] = mt; st[kRows * (kHeadDim + 1) + br] = lt; }
+            } else if (row0 + br < rows) store_row8(a, b, h, row0 + br, sq.nodes, c8, o, mt, lt);
         }
         __syncthreads();
     }
