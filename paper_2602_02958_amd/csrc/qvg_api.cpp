@@ -656,7 +656,7 @@ int check_step_sizes(const qvg_params *p, const qvg_tree_step *t) {
     if (t->table_pages > 0 && t->page_len > kMaxInt / t->table_pages) return QVG_ERR_BAD_PARAM;
     // (tiles of 32 tokens, and blocks of query rows, are counted in 32 bits)
     if (t->table_pages * ((t->page_len + 31) / 32) + (t->tail_capacity + 31) / 32 + (t->n_nodes + 31) / 32 > kMaxInt - 1024) return QVG_ERR_BAD_PARAM;
-    const int64_t rows = (int64_t)t->group * t->n_nodes, br = tree_block_rows(rows, false);
+    const int64_t rows = (int64_t)t->group * t->n_nodes, br = tree_block_rows(rows, false, false);
     if ((int64_t)t->n_seqs * p->n_heads * ((rows + br - 1) / br) > (1 << 30)) return QVG_ERR_BAD_PARAM;
     return QVG_OK;
 }
@@ -670,7 +670,9 @@ int qvg_attn_tree_scratch_bytes(const qvg_params *p, const qvg_tree_step *t, siz
     if (st != QVG_OK) return st;
     if (!out) return QVG_ERR_NULL;
     if ((st = check_step_sizes(p, t)) != QVG_OK) return st;
-    *out = tree_plan(*p, *t).state_bytes;
+    // (with a rotation or without)
+    const size_t plain = tree_plan(*p, *t, false).state_bytes, rotated = tree_plan(*p, *t, true).state_bytes;
+    *out = plain > rotated ? plain : rotated;
     return QVG_OK;
 }
 
@@ -707,8 +709,9 @@ int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t, const void *k_cen
     a.v = PoolSide{static_cast<const bf16_t *>(v_centroids), v_ids, v_codes, static_cast<const uint8_t *>(v_scales)};
     a.H = p->n_heads; a.K = p->n_clusters; a.B = p->group_size; a.T = p->n_stages; a.S = p->n_smooth_stages;
     a.fmt = format_of(p); a.id_wide = id_wide(p); a.t = *t; a.scale = softmax_scale;
-    const TreePlan plan = tree_plan(*p, *t);
+    const TreePlan plan = tree_plan(*p, *t, t->k_rope_f16 != nullptr);
     a.row_blocks = plan.row_blocks;
+    a.rows = plan.rows;
     a.slots = scratch && scratch_bytes >= plan.state_bytes ? plan.slots : 0;
     a.share = plan.share;
     a.state = static_cast<float *>(scratch);

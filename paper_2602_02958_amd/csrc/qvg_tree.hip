@@ -298,10 +298,10 @@ static bool packed_format(const qvg_params &p) {
     return tree_packed(p.n_stages, kHeadDim / p.group_size, (p.bits == 4 ? kFmtInt4 : 0) | (p.scale_format == QVG_SCALE_E4M3 ? kFmtE4M3 : 0),
                        p.n_smooth_stages);
 }
-TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t) {
-    TreePlan p{1, 0, 1, 0};
+TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t, bool rotated) {
+    TreePlan p{16, 1, 0, 1, 0};
     const int64_t rows = (int64_t)t.group * t.n_nodes;
-    const int br = tree_block_rows(rows, packed_format(prm));
+    const int br = p.rows = tree_block_rows(rows, packed_format(prm), rotated);
     p.row_blocks = (int)((rows + br - 1) / br);
     const int64_t units = (int64_t)prm.n_heads * p.row_blocks;           // of a sequence
     if (t.n_seqs < 1 || rows < 1) return p;
@@ -318,7 +318,7 @@ TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t) {
         // Several smoothing stages' rows gathered for both sides (with a rotation, or beyond 16 rows) are more than an XCD's L2
         // holds for 64 workgroups in pages of their own: 12 heads x 187200 tokens, four stages, 736 -> 560 us rotated, 32 rows
         // 528 -> 435 us.  Elsewhere sharing costs more tables than it saves (one token, one round: 92 -> 114 us).
-        if (prm.n_smooth_stages > 1 && (t.k_rope_f16 || rows > 16)) p.share = 8;
+        if (prm.n_smooth_stages > 1 && (rotated || rows > 16)) p.share = 8;
     }
     return p;
 }
@@ -335,7 +335,7 @@ static void launch_fmt(const TreeArgs &a, int blocks, int block_rows, hipStream_
 }
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     const bool packed = tree_packed(a.T, kHeadDim / a.B, a.fmt, a.S);
-    const int br = tree_block_rows((int64_t)a.t.group * a.t.n_nodes, packed);
+    const int br = a.rows;
     const int blocks = (int)((int64_t)(a.slots ? a.slots : a.t.n_seqs) * a.H * a.row_blocks);
     hipError_t e = hipSuccess;
     if (packed) e = br > 32 ? launch_tree_wide(a, blocks, br, s) : launch_tree_packed(a, blocks, br, s);

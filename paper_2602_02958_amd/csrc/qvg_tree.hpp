@@ -13,7 +13,7 @@ struct TreeArgs {
     int H, K, B, T, S, fmt, id_wide;
     qvg_tree_step t;
     float scale;
-    int row_blocks;                // blocks of a KV head's query rows
+    int rows, row_blocks;          // rows of a block of a KV head's query rows, and the blocks
     int slots;                     // workgroups of a block of all sequences, dealt to them by their lengths; 0: one to each, undivided
     int share;                     // consecutive parts of a sequence that walk the same range of tiles together, a round each in turn
     float *state;                  // partial results of the slots
@@ -31,11 +31,14 @@ inline bool tree_packed(int T, int G, int fmt, int S) {
 #undef QVG_TREE_IS
     return false;
 }
-// Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32, in the packed formats up to 128: a wavefront holds 32 rows
-// at most, and several of them share what they decode.
-inline int tree_block_rows(int64_t rows, bool packed) { return rows <= 16 ? 16 : rows <= 32 || !packed ? 32 : rows <= 64 ? 64 : 128; }
-struct TreePlan { int row_blocks, slots, share; size_t state_bytes; };
-TreePlan tree_plan(const qvg_params &p, const qvg_tree_step &t);
+// Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32, which a wavefront holds, and in the packed formats of 64 or
+// 128, whose wavefronts share what they decode: beyond 64 rows (12 heads x 187200 tokens, two rounds, 128 rows: 335 us, in
+// blocks of 32 503 us; 64 rows 272 and 250), with a rotation, which costs more, beyond 32 (64 rows: 355 us, in blocks of 32 460).
+inline int tree_block_rows(int64_t rows, bool packed, bool rotated) {
+    return rows <= 16 ? 16 : rows <= 32 || !packed ? 32 : rows > 64 ? 128 : rotated ? 64 : 32;
+}
+struct TreePlan { int rows, row_blocks, slots, share; size_t state_bytes; };      // (as in TreeArgs)
+TreePlan tree_plan(const qvg_params &p, const qvg_tree_step &t, bool rotated);
 hipError_t launch_tree_packed(const TreeArgs &a, int blocks, int block_rows, hipStream_t s);
 hipError_t launch_tree_wide(const TreeArgs &a, int blocks, int block_rows, hipStream_t s);
 hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s);

@@ -1,4 +1,4 @@
-// Attention over a paged cache for more than 32 query rows of a KV head: the wavefronts of a workgroup share what they decode.
+// Attention over a paged cache for more than 64 query rows of a KV head (32 where keys are rotated): the wavefronts of a workgroup share what they decode.
 //
 // A workgroup takes 64 or 128 rows, RS wavefronts of 32 rows each, and walks its tiles in rounds of four: every wavefront decodes
 // one of them into the fragments of both contractions (8 KB each, K_hat and V_hat as binary16) in LDS, and then contracts
@@ -291,7 +291,7 @@ hipError_t launch_tree_wide(const TreeArgs &a, int blocks, int block_rows, hipSt
     return tree_format(a.T, kHeadDim / a.B, a.fmt, a.S, [&](auto f) {
         typedef decltype(f) F;
         if (a.t.k_rope_f16) return block_rows == 64 ? launch_wide_rs<F, true, 2>(a, blocks, s) : launch_wide_rs<F, true, 4>(a, blocks, s);
-        return block_rows == 64 ? launch_wide_rs<F, false, 2>(a, blocks, s) : launch_wide_rs<F, false, 4>(a, blocks, s);
+        return launch_wide_rs<F, false, 4>(a, blocks, s);
     });
 }
 
