@@ -16,6 +16,7 @@ struct TreeArgs {
     int rows, row_blocks;          // rows of a block of a KV head's query rows, and the blocks
     int slots;                     // workgroups of a block of all sequences, dealt to them by their lengths; 0: one to each, undivided
     int share;                     // consecutive parts of a sequence that walk the same range of tiles together, a round each in turn
+    int table_cols;                // query rows of a table of the centroids' scores: a power of two
     float *state;                  // partial results of the slots
 };
 // The stored formats of the package's configurations and of the paper's presets, and their neighbours in group size: X(rounds,

@@ -19,7 +19,11 @@ namespace qvg {
 template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB * 8 * 1024; }
 constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
 
-template <class F, bool ROPE, int RB>
+// Where the centroids' scores may lie in LDS: not where keys are rotated, nor where four stages' tables and 32 rows would leave a
+// CU one workgroup.
+template <class F, bool ROPE, int RB> __host__ __device__ constexpr bool table_fits() { return !ROPE && (F::S == 1 || RB == 1); }
+
+template <class F, bool ROPE, int RB, bool kTable>
 __global__ __launch_bounds__(kTrThreads, 2)
 void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     constexpr int S = F::S;
@@ -27,9 +31,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     // One block of 16 rows takes V's rows as they are and P twice; for more rows the values are put together in binary16, 96
     // instructions a tile, and P is taken once, which saves 24 instructions, eight registers and 16 contractions a block
     constexpr bool kSplitV = RB == 1;
-    // the scores of the centroids in LDS; not where keys are rotated, nor where four stages' tables and 32 rows would leave a
-    // CU one workgroup
-    constexpr bool kTable = !ROPE && (S == 1 || RB == 1);
+    static_assert(!kTable || table_fits<F, ROPE, RB>(), "");
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float ms[kTrWaves][kRows], ls[kTrWaves][kRows];
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
@@ -44,7 +46,8 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
     uint4 *qlds = reinterpret_cast<uint4 *>(smem);                       // [RB][8][64] fragments
-    float *table = reinterpret_cast<float *>(smem + tree_query_bytes<RB>() + kTrWaves * F::wave_bytes);   // [S * K][kRows], kTable
+    float *table = reinterpret_cast<float *>(smem + tree_query_bytes<RB>() + kTrWaves * F::wave_bytes);   // [S * K][cols], kTable
+    const int cols = S > 1 ? a.table_cols : kRows, col = S > 1 ? c & (cols - 1) : c;
 
     // ---- Q: fragments 0..3 as bf16 in the order of gather_k, 4..7 as binary16 in the order of the residual's ----
     TreeRows<RB> R;
@@ -170,7 +173,8 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                 for (int i = 0; i < 4; ++i)
                     x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, row[i]), __builtin_bit_cast(bf16x8_t, qfrag(rb, i)), x, 0, 0, 0);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) table[(r0 + 4 * kb + r) * kRows + rb * 16 + c] = x[r];
+                for (int r = 0; r < 4; ++r)
+                    if (S == 1 || c < cols) table[(r0 + 4 * kb + r) * cols + rb * 16 + c] = x[r];
             }
         }
     };
@@ -185,7 +189,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
                 for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float x = *reinterpret_cast<const float *>(reinterpret_cast<const unsigned char *>(table) + at[r] + (rb * 16 + c) * 4);
+                        const float x = *reinterpret_cast<const float *>(reinterpret_cast<const unsigned char *>(table) + at[r] + (rb * 16 + col) * 4);
                         Sc[rb][hf][r] = st ? Sc[rb][hf][r] + x : x;
                     }
             }
@@ -212,7 +216,7 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
             }
             const int page_end = min(stop, (pg + 1) * sq.per_page);
             while (ti < page_end) {
-            D.park(f, kTable ? kRows * 4 : kHeadDim * 2);
+            D.park(f, kTable ? cols * 4 : kHeadDim * 2);
             D.order_lds();
             uint4 krow[2][4], vrow[8];
             if (!kTable && !ROPE) D.template gather_k<false>(cur, 0, krow);
@@ -358,29 +362,46 @@ void tree_attn_packed(TreeArgs a, int blocks, int per_xcd) {
     finish_block<RB>(a, at, sq.nodes, reinterpret_cast<float (*)[16][kTrPitch]>(smem), ms, ls, R.o, R.m, R.l);
 }
 
-template <class F, bool ROPE, int RB>
-static hipError_t launch_packed_rb(const TreeArgs &a, int blocks, hipStream_t s) {
+template <class F, bool ROPE, int RB, bool TABLE>
+static hipError_t launch_packed_form(const TreeArgs &a, int blocks, int lds, hipStream_t s) {
     const int per_xcd = (blocks + 7) / 8;
-    constexpr bool table = !ROPE && (F::S == 1 || RB == 1);               // (as in the kernel)
-    constexpr int own = tree_query_bytes<RB>() + kTrWaves * F::wave_bytes;
-    int lds = own + (table ? (F::S * a.K + 15) / 16 * 16 * 16 * RB * 4 : 0);
     if (lds < kTrMeetBytes) lds = kTrMeetBytes;
     if (lds > 64 * 1024) {
         static LdsHighWater mark;
-        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(tree_attn_packed<F, ROPE, RB>), (size_t)lds, mark);
+        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(tree_attn_packed<F, ROPE, RB, TABLE>), (size_t)lds, mark);
         if (e != hipSuccess) return e;
     }
-    tree_attn_packed<F, ROPE, RB><<<dim3((unsigned)(per_xcd * 8)), dim3(kTrThreads), (size_t)lds, s>>>(a, blocks, per_xcd);
+    tree_attn_packed<F, ROPE, RB, TABLE><<<dim3((unsigned)(per_xcd * 8)), dim3(kTrThreads), (size_t)lds, s>>>(a, blocks, per_xcd);
     return hipSuccess;
+}
+// A table costs a contraction for each 16 of its rows, and saves a row's gather for each token that a workgroup meets in a page:
+// those of the page, or of the workgroup's part where that is shorter.  One token over 12 heads x 187200 tokens, K = 256, one
+// round: pages of 512 tokens 158 us with tables and 153 gathered, of 1024 124 and 141, of 4680 91 and 124; four stages,
+// 1024 tokens, 391 and 538.  For 32 rows, whose tables are twice as large, 1024 tokens 140 and 148, four rounds 267 and 261,
+// and not where a CU holds one workgroup (K = 512, 4680 tokens: 164 and 162, 1024 tokens 251 and 172).
+template <class F, bool ROPE, int RB>
+static hipError_t launch_packed_rb(TreeArgs a, int blocks, hipStream_t s) {
+    constexpr int own = tree_query_bytes<RB>() + kTrWaves * F::wave_bytes;
+    if constexpr (table_fits<F, ROPE, RB>()) {
+        static_assert(own + F::S * kMaxClusters * 16 * RB * 4 + kTrWaves * 16 * RB * 8 <= 160 * 1024, "the largest table must fit a CU");
+        int64_t met = a.t.page_len;
+        if (a.slots && a.t.n_seqs * a.t.table_pages < a.slots) met = a.t.n_seqs * a.t.table_pages * a.t.page_len / a.slots;
+        // Several stages' tables: columns for the rows that there are, where 16 would leave a CU one workgroup (one token, four
+        // stages, 495 -> 391 us)
+        const int64_t rows = (int64_t)a.t.group * a.t.n_nodes;
+        auto bytes = [&](int cols) { return own + (F::S * a.K + 15) / 16 * 16 * cols * 4; };
+        a.table_cols = 16 * RB;
+        while (F::S > 1 && a.table_cols / 2 >= rows && bytes(a.table_cols) > 79 * 1024) a.table_cols /= 2;
+        const int lds = bytes(a.table_cols);
+        if (met >= (RB == 1 ? 3 : 4) * (int64_t)a.K && (RB == 1 || lds <= 79 * 1024)) return launch_packed_form<F, ROPE, RB, true>(a, blocks, lds, s);
+    }
+    return launch_packed_form<F, ROPE, RB, false>(a, blocks, own, s);
 }
 template <class F>
 static hipError_t launch_packed(const TreeArgs &a, int blocks, int br, hipStream_t s) {
-    hipError_t e;
     if (a.t.k_rope_f16)
-        e = br == 16 ? launch_packed_rb<F, true, 1>(a, blocks, s) : launch_packed_rb<F, true, 2>(a, blocks, s);
-    else
-        e = br == 16 ? launch_packed_rb<F, false, 1>(a, blocks, s) : launch_packed_rb<F, false, 2>(a, blocks, s);
-    return e;
+        return br == 16 ? launch_packed_rb<F, true, 1>(a, blocks, s) : launch_packed_rb<F, true, 2>(a, blocks, s);
+    return br == 16 ? launch_packed_rb<F, false, 1>(a, blocks, s) : launch_packed_rb<F, false, 2>(a, blocks, s);
 }
 hipError_t launch_tree_packed(const TreeArgs &a, int blocks, int block_rows, hipStream_t s) {
     return tree_format(a.T, kHeadDim / a.B, a.fmt, a.S, [&](auto f) { return launch_packed<decltype(f)>(a, blocks, block_rows, s); });
