@@ -8,7 +8,8 @@ namespace qvg {
 // nodes, its ancestors and the parent of the topmost one (five pointer doublings by lane exchange, all blocks at once);
 // then the blocks take turns: the rows of a block are complete below its own word once the row of that outside ancestor is
 // copied, which lies in an earlier block.  So a tree of n nodes takes n / 32 steps however deep it is.  The rows go out at the
-// end: a store in every step made its barrier wait for memory (64 trees of 1000 nodes 36 us instead of ...).
+// end: a store in every step made its barrier wait for memory (64 trees of 1000 nodes 36 us instead of 22; the rows
+// that they write, 8 MB, take 2 us at the rate of a copy: what bounds a tree is its 32 steps of a barrier and two LDS accesses).
 __global__ __launch_bounds__(1024)
 void tree_mask_kernel(int n, int words, const int32_t *parents, const int32_t *nodes, uint32_t *mask, int32_t *depth) {
     extern __shared__ uint32_t lds[];
@@ -71,7 +72,8 @@ hipError_t launch_tree_mask(int n_seqs, int n_nodes, const int32_t *parents, con
 }
 
 // ---- kept tokens --------------------------------------------------------------------------------------
-// 16 lanes to a row of 128 bf16, both sides.
+// 16 lanes to a row of 128 bf16, both sides.  Bound by the launch: 64 paths over 40 heads, 31 MB both ways, take 7 us at the rate of
+// a copy and 12 us a call, which is the host's time for one.
 __global__ __launch_bounds__(256)
 void keep_nodes_kernel(KeepArgs a) {
     const unsigned unit = blockIdx.x / (unsigned)a.blocks;                // sequence and unit (K heads, then V heads)
@@ -114,7 +116,6 @@ struct CopyArgs {
     PageArray array[4];
     int width[4];                             // bytes of a piece: what the array's pages are all aligned to, up to 16
     int first_block[5];                       // workgroups of a page, array by array
-    int units;
     int32_t src[kCpPairs], dst[kCpPairs];
 };
 template <typename W>
@@ -133,7 +134,7 @@ __device__ __forceinline__ void copy_pieces(const uint8_t *src, uint8_t *dst, in
 }
 // Every field that a workgroup needs is asked for at once, the arrays' four descriptions among them: the arguments lie in memory
 // that is far away, and one after the other (or as a value, which indexed at run time every thread keeps in scratch memory)
-// they took 16 us of a copy of 1 MB.
+// they took 16 us of a copy of 1 MB, which takes 3 us so.  20 pages of 4680 tokens of 24 units, 714 MB both ways: 125 us, 5.7 TB/s.
 __global__ __launch_bounds__(256)
 void copy_pages_kernel(CopyArgs) {
     const CopyArgs &a = *(const CopyArgs *)__builtin_amdgcn_kernarg_segment_ptr();
@@ -158,7 +159,6 @@ void copy_pages_kernel(CopyArgs) {
 hipError_t launch_copy_pages(const PageArray (&arrays)[4], int units, int64_t n_pairs, const int32_t *src, const int32_t *dst,
                              hipStream_t s) {
     CopyArgs a{};
-    a.units = units;
     for (int k = 0; k < 4; ++k) {
         a.array[k] = arrays[k];
         const uint64_t all = (uint64_t)reinterpret_cast<uintptr_t>(arrays[k].src) | (uint64_t)reinterpret_cast<uintptr_t>(arrays[k].dst) |

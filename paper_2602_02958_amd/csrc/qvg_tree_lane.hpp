@@ -58,30 +58,55 @@ __device__ __forceinline__ halfx8_t pack_f16x8(const float *v) {
 __host__ __device__ inline int64_t tree_state_floats(int rows) { return (int64_t)rows * (kHeadDim + 2); }
 
 // How the slots of a divided call (a.slots of them, the same for every head and row block) are dealt to the sequences: a slot
-// for every q tiles or part of them, and one at least, with q so large that the slots suffice: the sum of ceil(T / q) over n
-// sequences is at most total / q + n.  Every wavefront works that out for itself from the lengths, which only the device knows
-// (n <= 256: a call of more sequences is not divided).  Slots that are left over have nothing to do.
+// for every q tiles or part of them, and one at least, with the smallest q for which the slots suffice, or nearly: it lies between
+// total / slots and total / (slots - n), since the sum of ceil(T / q) over n sequences is at most total / q + n, and is found in
+// five halvings (16 ragged sequences on 64 slots, whose parts the upper end makes a third longer: 116 -> 109 us).  Every wavefront
+// works that out for itself from the lengths, which only the device knows (n <= 256: a call of more sequences is not divided).
+// Slots that are left over have nothing to do.
 struct SlotPlace { int b, part, parts, first; };                         // first: the sequence's first slot; parts: 0, none
-__device__ __forceinline__ int parts_of_sequence(const TreeArgs &a, int b, int q) {
-    const int total = tiles_of_sequence(a.t, b).total, p = (total + q - 1) / q;
+__device__ __forceinline__ int parts_of_tiles(int total, int q) {
+    const int p = (int)(((uint32_t)total + (uint32_t)q - 1u) / (uint32_t)q);
     return p < 1 ? 1 : p;
+}
+template <typename N>
+__device__ __forceinline__ N sum_of_lanes(N x) {
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) x += __shfl_xor(x, off, 64);
+    return x;
 }
 // The place of slot `slot`, or with by_sequence that of sequence `slot`'s first part.  Uniform over a wavefront.
 __device__ __forceinline__ SlotPlace place_slot(const TreeArgs &a, int slot, bool by_sequence) {
     const int lane = threadIdx.x & 63, n = a.t.n_seqs;
-    int64_t total = 0;
-    for (int i = lane; i < n; i += 64) total += tiles_of_sequence(a.t, i).total;
-    if (n > 1) {
+    int tiles[4];                                                        // of sequences lane, 64 + lane, ..
 #pragma unroll
-        for (int off = 1; off < 64; off *= 2) total += __shfl_xor(total, off, 64);
-    } else total = __shfl(total, 0, 64);
-    const int room = n > 1 ? a.slots - n : a.slots;
-    int q = (int)((total + room - 1) / room);
+    for (int k = 0; k < 4; ++k) {
+        tiles[k] = 0;
+        if (64 * k < n && 64 * k + lane < n) tiles[k] = tiles_of_sequence(a.t, 64 * k + lane).total;
+    }
+    int q;
+    if (n == 1) q = (__builtin_amdgcn_readfirstlane(tiles[0]) + a.slots - 1) / a.slots;
+    else {
+        const int64_t total = sum_of_lanes((int64_t)tiles[0] + tiles[1] + tiles[2] + tiles[3]);
+        int lo = (int)((total + a.slots - 1) / a.slots);
+        q = (int)((total + a.slots - n - 1) / (a.slots - n));
+        for (int i = 0; i < 5 && lo < q; ++i) {                          // uniform
+            const int mid = lo + (q - lo) / 2;
+            int need = 0;
+            if (mid > 0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (64 * k < n) need += 64 * k + lane < n ? parts_of_tiles(tiles[k], mid) : 0;
+            if (mid > 0 && sum_of_lanes(need) <= a.slots) q = mid; else lo = mid + 1;
+        }
+    }
     if (q < 2 * kTrWaves) q = 2 * kTrWaves;                              // two tiles to a wavefront
     SlotPlace p{0, 0, 0, 0};
     int before = 0;
-    for (int base = 0; base < n; base += 64) {                           // uniform
-        const int i = base + lane, mine = i < n ? parts_of_sequence(a, i, q) : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int base = 64 * k, i = base + lane;
+        if (base >= n) break;                                            // uniform
+        const int mine = i < n ? parts_of_tiles(tiles[k], q) : 0;
         int upto = mine;
 #pragma unroll
         for (int off = 1; off < 64; off *= 2) {
