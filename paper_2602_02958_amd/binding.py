@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+from array import array
 from dataclasses import dataclass
 
 import torch
@@ -494,15 +495,19 @@ def _here(*tensors):
 
 
 def _check_pool(e: Encoded, name):
-    """The arrays of a pool agree with each other: whole pages, a set of tables to each."""
-    ids, codes, scales, cent, S, L = e.ids.shape, e.codes.shape, e.scales.shape, e.centroids.shape, e.n_smooth, e.chunk_len
-    units, tokens = ids[0], ids[1]
-    if tokens % L or tokens < L:
+    """The arrays of a pool agree with each other: whole pages, a set of tables to each.  Returns (units, pages, K, d)."""
+    cent, S, L = e.centroids.shape, e.n_smooth, e.chunk_len
+    units, tokens, T, _ = e.codes.shape
+    s_units, s_tokens, s_T, _ = e.scales.shape
+    pages = tokens // L
+    if pages * L != tokens or pages < 1:
         raise ValueError(f"{name}: the pool must hold whole pages of {L} tokens")
-    if (codes[:3] != scales[:3] or codes[:2] != ids[:2] or cent[0] != units or cent[1] != tokens // L or
-            (len(cent) != 4 or len(ids) != 2 if S == 1 else len(cent) != 5 or cent[2] != S or ids[2:] != (S,))):
+    if (units != s_units or tokens != s_tokens or T != s_T or cent[:-2] != ((units, pages) if S == 1 else (units, pages, S)) or
+            e.ids.shape != ((units, tokens) if S == 1 else (units, tokens, S))):
         raise ValueError(f"{name}: the pool's arrays are of different sizes")
-    _check_stored(e.centroids, e.ids, e.codes, e.scales, cent[-2])
+    K, d = cent[-2:]
+    _check_stored(e.centroids, e.ids, e.codes, e.scales, K)
+    return units, pages, K, d
 
 
 @functools.lru_cache(maxsize=256)
@@ -555,7 +560,7 @@ def attn_tree(q, k: Encoded, v: Encoded, page_table, kv_len, k_new, v_new, tail_
             (k.ids.shape, k.codes.shape, k.scales.shape, k.scales.dtype, k.centroids.shape, k.chunk_len, k.n_smooth):
         raise ValueError("K and V pools must share shapes and parameters")
     _check_pool(k, "k")
-    _check_pool(v, "v")
+    _check_stored(v.centroids, v.ids, v.codes, v.scales, v.centroids.shape[-2])          # (the shapes are k's)
     return _attn_tree(q, k, (k.centroids.data_ptr(), k.ids.data_ptr(), k.codes.data_ptr(), k.scales.data_ptr()),
                       (v.centroids.data_ptr(), v.ids.data_ptr(), v.codes.data_ptr(), v.scales.data_ptr()), k.ids.shape[0], page_table,
                       kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
@@ -578,7 +583,9 @@ def _attn_tree(q, k: Encoded, kp, vp, H, page_table, kv_len, k_new, v_new, tail_
     n, hq, m, d = q.shape
     if hq < H or hq % H:
         raise ValueError("q: the number of query heads must be a multiple of the KV heads'")
-    K = k.centroids.shape[-2]
+    K, pool_d = k.centroids.shape[-2:]
+    if pool_d != d:
+        raise ValueError(f"q: the pools hold heads of {pool_d} channels")
     _, _, T, code_bytes = k.codes.shape
     L = k.chunk_len
     ns = _same_rows(k_new, v_new, ("k_new", "v_new"), (n, H, m, d))
@@ -644,22 +651,23 @@ def copy_pages(cache: Encoded, src, dst, into: Encoded | None = None) -> Encoded
     """qvg_copy_pages: page src[i] of every unit of the pool `cache` becomes page dst[i] of the pool `into` (the same one
     without).  src, dst: sequences of Python integers; no destination twice, and none that is a source in the same pool."""
     into = cache if into is None else into
-    K, d = cache.centroids.shape[-2:]
-    if (into.chunk_len, into.n_smooth, into.ids.shape[0], into.codes.shape[2:], into.scales.shape[2:], into.scales.dtype,
-            into.centroids.shape[2:]) != (cache.chunk_len, cache.n_smooth, cache.ids.shape[0], cache.codes.shape[2:],
-                                          cache.scales.shape[2:], cache.scales.dtype, cache.centroids.shape[2:]):
+    if into is not cache and (into.chunk_len, into.n_smooth, into.ids.shape[0], into.codes.shape[2:], into.scales.shape[2:], into.scales.dtype,
+                              into.centroids.shape[2:]) != (cache.chunk_len, cache.n_smooth, cache.ids.shape[0], cache.codes.shape[2:],
+                                                            cache.scales.shape[2:], cache.scales.dtype, cache.centroids.shape[2:]):
         raise ValueError("the pools were allocated for different parameters")
     if len(src) != len(dst):
         raise ValueError("src and dst must have the same length")
     L = cache.chunk_len
-    _check_pool(cache, "cache")
-    _check_pool(into, "into")
+    units, pages, K, d = _check_pool(cache, "cache")
+    into_pages = pages if into is cache else _check_pool(into, "into")[1]
     _here(cache.ids, into.ids)
     T, code_bytes = cache.codes.shape[2:]
-    p = QvgParams(cache.ids.shape[0], d, K, d // cache.scales.shape[3], T, code_bytes * 8 // d, cache.n_smooth, 0, cache.scale_format)
+    p = QvgParams(units, d, K, d // cache.scales.shape[3], T, code_bytes * 8 // d, cache.n_smooth, 0, cache.scale_format)
     ints = C.c_int32 * len(src)
-    ptrs = [(c.ids.shape[1] // L, c.centroids.data_ptr(), c.ids.data_ptr(), c.codes.data_ptr(), c.scales.data_ptr()) for c in (cache, into)]
-    st = lib().qvg_copy_pages(p, L, len(src), ints(*src), ints(*dst), *ptrs[0], *ptrs[1], _stream())
+    ptrs = [(n, c.centroids.data_ptr(), c.ids.data_ptr(), c.codes.data_ptr(), c.scales.data_ptr()) for n, c in ((pages, cache), (into_pages, into))]
+    # (array: a number that does not fit 32 bits is an error, not another page)
+    st = lib().qvg_copy_pages(p, L, len(src), ints.from_buffer(array("i", src)), ints.from_buffer(array("i", dst)), *ptrs[0], *ptrs[1],
+                              _stream())
     if st != 0:
         raise QvgError(st, "qvg_copy_pages")
     return into
@@ -902,6 +910,10 @@ class PagedCache:
 
     def append(self, seq, kv):
         """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence."""
+        units, _, d = self.tail.shape[1:]
+        if kv.dim() != 3 or kv.shape[0] != units or kv.shape[2] != d:
+            raise ValueError(f"kv: need [{units}, n, {d}]")
+        _check(kv, torch.bfloat16, "kv")
         n, L = kv.shape[1], self.page_len
         self._need({seq: n})
         at = 0

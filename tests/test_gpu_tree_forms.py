@@ -221,3 +221,36 @@ def test_masks_kept_tokens_and_copies_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         expect()
+
+
+def test_refusals_that_need_tensors_of_the_gpu():
+    pool = Pool(4, 3, 32, K=8, T=1, seed=60)
+    e, half = pool.encoded(0, 4), pool.encoded(0, 2)
+    q = torch.zeros(1, 2, 1, D, dtype=torch.bfloat16, device="cuda")
+    for src, dst in (([3], [0]), ([0], [3]), ([-1], [0]), ([0], [0]), ([0, 1], [2, 2]), ([0, 1], [1, 2])):
+        with pytest.raises(B.QvgError):
+            B.copy_pages(e, src, dst)
+    with pytest.raises(OverflowError):                     # not page 0
+        B.copy_pages(e, [1 << 32], [1])
+    with pytest.raises(ValueError):
+        B.copy_pages(e, [0], [1], into=half)               # fewer units
+    narrow = B.Encoded(half.centroids[..., :64].contiguous(), half.ids, half.codes, half.scales, 32)
+    short = B.Encoded(half.centroids[:, :2].contiguous(), half.ids, half.codes, half.scales, 32)
+    for bad in (narrow, short):
+        with pytest.raises(ValueError):
+            B.attn_tree(q, bad, bad, None, None, q, q)
+    with pytest.raises(ValueError):                        # a V pool of another page length
+        B.attn_tree(q, half, B.Encoded(half.centroids, half.ids, half.codes, half.scales, 16), None, None, q, q)
+    with pytest.raises(ValueError):                        # three query heads to two KV heads
+        B.attn_tree(torch.zeros(1, 3, 1, D, dtype=torch.bfloat16, device="cuda"), half, half, None, None, q, q)
+    with pytest.raises(ValueError):                        # K and V of other strides
+        B.attn_tree(q, half, half, None, None, q.expand(1, 2, 1, D).clone(), torch.zeros(1, 2, 1, 2 * D, dtype=torch.bfloat16, device="cuda")[..., ::2])
+    init = torch.zeros(2, 8, D, dtype=torch.bfloat16, device="cuda")
+    cache = B.PagedCache(1, 2, 3, 32, 2, 4, 8, 64, 1, init)
+    s = cache.open()
+    for bad in (torch.zeros(1, 5, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 5, 64, dtype=torch.bfloat16, device="cuda")):
+        with pytest.raises(ValueError):
+            cache.append(s, bad)
+    with pytest.raises(TypeError):
+        cache.append(s, torch.zeros(2, 5, D, device="cuda"))
+    assert cache.length(s) == 0
