@@ -401,12 +401,17 @@ typedef struct qvg_tree_step {
  * A new token that no row sees may hold anything (also what is no number); every other value must be finite, keys, values
  * and decoded values of magnitude up to 65504.
  *   k_*, v_*  the K and the V pool, [n_heads] units each, layout of a cache of pool_pages * page_len tokens per unit
+ *   out       may be q with q's strides; it overlaps no other input
  *   scratch   optional, 16-byte aligned: with qvg_attn_tree_scratch_bytes bytes the sequences' tokens are dealt to several
- *             workgroups per KV head and one more launch joins their partial results.  NULL or less: one workgroup per
- *             sequence, KV head and 64 query rows, whose result differs by the order of fp32 sums.  Equal calls give equal bits.
+ *             workgroups per KV head, by the sequences' lengths, and one more launch joins their partial results.  NULL or
+ *             less: one workgroup per sequence, KV head and block of query rows, whose result differs by the order of fp32
+ *             sums.  Equal calls give equal bits; among others a sequence's result may differ by that order too.
  *             Contents are scratch: nothing has to be initialised and nothing survives the call.
- * What is rounded: queries, keys, values and probabilities enter the two contractions as binary16 (queries scaled by a power
- * of two per row, probabilities by one per row and workgroup); scores, normaliser and output are accumulated in fp32.
+ * What is rounded: queries, keys, values and probabilities enter the two contractions with 11 bits or more, as binary16
+ * (queries scaled by a power of two per row, probabilities by one per row and workgroup; keys and values as they are, with
+ * binary16's step of 2^-24 below 2^-14), or where centroid rows and new tokens enter as stored in bf16 with probabilities of
+ * 16 bits.  Sums of Eq. 7's rounds are formed in binary16 (one rounding a round, after the first) or fp32.  Scores,
+ * normaliser and output are accumulated in fp32.
  */
 int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t,
                   const void *k_centroids, const uint8_t *k_ids, const uint8_t *k_codes, const void *k_scales,

@@ -715,6 +715,7 @@ int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t, const void *k_cen
     a.slots = scratch && scratch_bytes >= plan.state_bytes ? plan.slots : 0;
     a.share = plan.share;
     a.state = static_cast<float *>(scratch);
+    if (a.slots) a.places = reinterpret_cast<int2 *>(static_cast<char *>(scratch) + plan.state_bytes - (size_t)t->n_seqs * sizeof(int2));
     return launch_attn_tree(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
 }
 

@@ -3,16 +3,22 @@
 //     o = sum_n w_n v_n / sum_n w_n,   w_n = exp(scale q.k_n),   k_n, v_n = sum_s c_s[id_s(n)] + sum_t s_t(n) q_t(n)  (Eq. 7)
 // in one pass over the tokens with the running maximum and sum of the soft-max.
 //
-// A workgroup takes a block of 16, 32 or 64 query rows of one KV head (rows = group x new tokens) and a part of the
-// sequence's tiles of 32 tokens; each of its wavefronts walks tiles of its own and nothing is exchanged before the end, so
-// there is no barrier in the loop.  The contractions run on v_mfma_f32_16x16x32_f16 with the operands where the decoding
-// puts them, so a decoded tile passes through registers only:
+// A workgroup takes a block of 16 or 32 query rows of one KV head (rows = group x new tokens; 64 or 128 in qvg_tree_wide.hip)
+// and a part of the sequence's tiles of 32 tokens; each of its wavefronts walks tiles of its own, so a tile costs no barrier.
+// The contractions run on v_mfma_f32_16x16x32_f16 with the operands where the decoding puts them, so a decoded tile passes
+// through registers only:
 //   S^T = K Q^T:   lane (c, kb) decodes channels 32 kb .. 32 kb + 31 of tokens c and 16 + c; the order of a contraction is
 //                  free, so MFMA i takes channels 32 kb + 8 i + e and Q's fragments are loaded the same way;
 //   O^T += V^T P:  lane (c, kb) decodes the octet of channels 8 c .. 8 c + 7 of tokens 4 kb + r and 16 + 4 kb + r, which are
 //                  the tokens whose scores S^T leaves in the lane: P needs no movement, and pairs of tokens are packed as
 //                  they are rounded, which is the transposition.  MFMA j makes channels 8 c + j; the lane ends up with
 //                  channels 32 kb .. 32 kb + 31 of query row c.
+// Tokens that are not there, and new ones that a row does not see, get the score -inf; the row's reference is finite from the
+// start, so their weights are zero whatever comes first.
+//
+// The kernel here decodes a tile element by element with the format's sizes at run time: any format that the encoder
+// writes.  Its vector instructions bound it: a format of two rounds that took its way took ten times the packed form's time.  The formats of the package's configurations and presets
+// have qvg_tree_packed.hip and qvg_tree_wide.hip.
 #include "qvg_tree_lane.hpp"
 
 namespace qvg {
@@ -248,50 +254,65 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
     finish_block<RB>(a, at, sq.nodes, meet, ms, ls, O, m, l);
 }
 
-// Joins a query row's parts: a workgroup to a row, 16 lanes (8 channels each) to a part, so that 16 parts are read at a time.
-__global__ __launch_bounds__(256)
+// Joins a query row's parts: a workgroup to a row, 16 lanes (8 channels each) to a part, so that GROUPS parts are read at a time.
+// One wavefront to a row where there are many rows of few parts: shuffles alone, and all rows at once.
+template <int GROUPS>
+__global__ __launch_bounds__(16 * GROUPS)
 void tree_join_kernel(TreeArgs a, int block_rows) {
-    __shared__ float sums[16][kTrPitch], weights[16];
     const int64_t rows = (int64_t)a.t.group * a.t.n_nodes;
     const int64_t bh = (int64_t)(blockIdx.x / (unsigned)rows), r = (int64_t)blockIdx.x - bh * rows;
     const int b = (int)(bh / a.H), h = (int)(bh - (int64_t)b * a.H);
     const int row = (int)(r % block_rows), grp = threadIdx.x >> 4, c8 = threadIdx.x & 15;
     const int step = (int)tree_state_floats(block_rows);
-    const SlotPlace at = place_slot(a, b, true);
-    const float *st = a.state + (((int64_t)h * a.row_blocks + r / block_rows) * a.slots + at.first) * step;
+    const int2 place = a.places[b];                                      // first slot, parts
+    int nodes = a.t.n_nodes;
+    if (a.t.nodes) { nodes = a.t.nodes[b]; nodes = nodes < 0 ? 0 : (nodes > a.t.n_nodes ? a.t.n_nodes : nodes); }
+    const float *st = a.state + (((int64_t)h * a.row_blocks + r / block_rows) * a.slots + place.x) * step;
     const float *mp = st + block_rows * kHeadDim + row, *lp = mp + block_rows, *op = st + row * kHeadDim + c8 * 8;
     float m = kTrNoScore, l = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
     // every lane finds the maximum over all parts: lane i of 64 looks at parts i, i + 64, ..
-    for (int p = threadIdx.x & 63; p < at.parts; p += 64) m = fmaxf(m, mp[(int64_t)p * step]);
+    for (int p = threadIdx.x & 63; p < place.y; p += 64) m = fmaxf(m, mp[(int64_t)p * step]);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
 #pragma unroll 4
-    for (int p = grp; p < at.parts; p += 16) {
+    for (int p = grp; p < place.y; p += GROUPS) {
         const float f = __builtin_amdgcn_exp2f(mp[(int64_t)p * step] - m);
-        const float4 x = *reinterpret_cast<const float4 *>(op + (int64_t)p * step), y = *reinterpret_cast<const float4 *>(op + (int64_t)p * step + 4);
+        const float4 x = *reinterpret_cast<const float4 *>(op + (int64_t)p * step);
+        const float4 y = *reinterpret_cast<const float4 *>(op + (int64_t)p * step + 4);
         l += lp[(int64_t)p * step] * f;
         o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
         o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
     }
-    *reinterpret_cast<float4 *>(&sums[grp][c8 * 8]) = make_float4(o[0], o[1], o[2], o[3]);
-    *reinterpret_cast<float4 *>(&sums[grp][c8 * 8 + 4]) = make_float4(o[4], o[5], o[6], o[7]);
-    if (c8 == 0) weights[grp] = l;
-    __syncthreads();
-    if (grp) return;
-    l = 0.0f;
+    // the four parts of a wavefront, then the wavefronts
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+    for (int off = 16; off < 64; off *= 2) {
+        l += __shfl_xor(l, off, 64);
 #pragma unroll
-    for (int g = 0; g < 16; ++g) {
-        l += weights[g];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] += sums[g][c8 * 8 + e];
+        for (int e = 0; e < 8; ++e) o[e] += __shfl_xor(o[e], off, 64);
     }
-    int nodes = a.t.n_nodes;
-    if (a.t.nodes) { nodes = a.t.nodes[b]; nodes = nodes < 0 ? 0 : (nodes > a.t.n_nodes ? a.t.n_nodes : nodes); }
-    store_row8(a, b, h, r, nodes, c8, o, m, l);
+    if constexpr (GROUPS > 4) {
+        constexpr int W = GROUPS / 4;
+        __shared__ float sums[W][kTrPitch], weights[W];
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) < 16) {
+            *reinterpret_cast<float4 *>(&sums[wave][c8 * 8]) = make_float4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<float4 *>(&sums[wave][c8 * 8 + 4]) = make_float4(o[4], o[5], o[6], o[7]);
+            if (c8 == 0) weights[wave] = l;
+        }
+        __syncthreads();
+        l = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll
+        for (int g = 0; g < W; ++g) {
+            l += weights[g];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += sums[g][c8 * 8 + e];
+        }
+    }
+    if (grp == 0) store_row8(a, b, h, r, nodes, c8, o, m, l);
 }
 
 static bool packed_format(const qvg_params &p) {
@@ -314,7 +335,7 @@ TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t, bool rotated) 
     if (slots > most) slots = most;
     if (slots >= 2 * (int64_t)t.n_seqs) {
         p.slots = (int)slots;
-        p.state_bytes = (size_t)(units * slots * tree_state_floats(br)) * sizeof(float);
+        p.state_bytes = (size_t)(units * slots * tree_state_floats(br)) * sizeof(float) + (size_t)t.n_seqs * sizeof(int2);
         // Several smoothing stages' rows gathered for both sides (with a rotation, or beyond 16 rows) are more than an XCD's L2
         // holds for 64 workgroups in pages of their own: 12 heads x 187200 tokens, four stages, 736 -> 560 us rotated, 32 rows
         // 528 -> 435 us.  Elsewhere sharing costs more tables than it saves (one token, one round: 92 -> 114 us).
@@ -348,7 +369,9 @@ hipError_t launch_attn_tree(const TreeArgs &a, hipStream_t s) {
     if (e != hipSuccess) return e;
     if (a.slots) {
         const int64_t n = (int64_t)a.t.n_seqs * a.H * a.t.group * a.t.n_nodes;
-        tree_join_kernel<<<dim3((unsigned)n), dim3(256), 0, s>>>(a, br);
+        // (more rows than the chip holds workgroups of 256: 4960 rows of 13 parts 9.0 us so and 13.8; 12 of 42 parts 7.9 and 7.1)
+        if (n > 2048) tree_join_kernel<4><<<dim3((unsigned)n), dim3(64), 0, s>>>(a, br);
+        else tree_join_kernel<16><<<dim3((unsigned)n), dim3(256), 0, s>>>(a, br);
     }
     return hipGetLastError();
 }

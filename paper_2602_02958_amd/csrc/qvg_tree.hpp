@@ -18,6 +18,7 @@ struct TreeArgs {
     int share;                     // consecutive parts of a sequence that walk the same range of tiles together, a round each in turn
     int table_cols;                // query rows of a table of the centroids' scores: a power of two
     float *state;                  // partial results of the slots
+    int2 *places;                  // [n_seqs] a sequence's first slot and its parts, for the joining launch
 };
 // The stored formats of the package's configurations and of the paper's presets, and their neighbours in group size: X(rounds,
 // groups per token, E4M3 scales, 4-bit levels, smoothing stages).  They have kernels of their own; any other one is decoded

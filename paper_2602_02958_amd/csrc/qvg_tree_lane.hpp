@@ -74,8 +74,8 @@ __device__ __forceinline__ N sum_of_lanes(N x) {
     for (int off = 1; off < 64; off *= 2) x += __shfl_xor(x, off, 64);
     return x;
 }
-// The place of slot `slot`, or with by_sequence that of sequence `slot`'s first part.  Uniform over a wavefront.
-__device__ __forceinline__ SlotPlace place_slot(const TreeArgs &a, int slot, bool by_sequence) {
+// The place of slot `slot`.  Uniform over a wavefront.
+__device__ __forceinline__ SlotPlace place_slot(const TreeArgs &a, int slot) {
     const int lane = threadIdx.x & 63, n = a.t.n_seqs;
     int tiles[4];                                                        // of sequences lane, 64 + lane, ..
 #pragma unroll
@@ -114,11 +114,11 @@ __device__ __forceinline__ SlotPlace place_slot(const TreeArgs &a, int slot, boo
             if (lane >= off) upto += x;
         }
         upto += before;
-        const unsigned long long hit = __ballot(by_sequence ? i == slot : (mine > 0 && slot >= upto - mine && slot < upto));
+        const unsigned long long hit = __ballot(mine > 0 && slot >= upto - mine && slot < upto);
         if (hit) {
             const int at = __builtin_ctzll(hit);
             p.b = base + at; p.parts = __shfl(mine, at, 64); p.first = __shfl(upto, at, 64) - p.parts;
-            p.part = by_sequence ? 0 : slot - p.first;
+            p.part = slot - p.first;
             break;
         }
         before = __shfl(upto, 63, 64);
@@ -143,9 +143,10 @@ __device__ __forceinline__ BlockPlace place_block(const TreeArgs &a, int w, bool
         return p;
     }
     const int unit = rotated ? w % units : w / a.slots, slot = rotated ? w / units : w % a.slots;
-    const SlotPlace s = place_slot(a, slot, false);
+    const SlotPlace s = place_slot(a, slot);
     p.b = s.b; p.part = s.part; p.parts = s.part < s.parts ? s.parts : 0;
     p.rblk = unit % a.row_blocks; p.h = unit / a.row_blocks;
+    if (unit == 0 && p.part == 0 && p.parts > 0 && threadIdx.x == 0) a.places[p.b] = make_int2(s.first, s.parts);
     p.state = ((int64_t)unit * a.slots + slot) * tree_state_floats(block_rows);
     return p;
 }
@@ -207,8 +208,8 @@ __device__ __forceinline__ halfx2_t level4(uint32_t x, int k) {
 }
 
 // A stored format at compile time: with sizes that are known every load of the loop has one form, and nothing waits for it
-// before it is used (with run-time branches between forms the loop waited for loads where the forms meet: one token over 12 heads x 187200 tokens of four
-// rounds 239 us instead of 219).
+// before it is used (with run-time branches between forms the loop waited for loads where the forms meet: one token over 12 heads
+// x 187200 tokens of four rounds 239 us instead of 219).
 template <int T_, int G_, bool FP8_, bool I4_, int S_>
 struct TreeFormat {
     static constexpr int T = T_, G = G_, S = S_, TG = T * G;             // rounds, groups per token, smoothing stages

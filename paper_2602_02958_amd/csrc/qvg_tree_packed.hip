@@ -1,4 +1,4 @@
-// Attention over a paged cache, packed form: up to 32 query rows to a block (see qvg_tree.hip for the layout that all forms share).
+// Attention over a paged cache, packed form: up to 32 query rows to a block (qvg_tree.hip has the layout that all forms share).
 #include "qvg_tree_lane.hpp"
 
 namespace qvg {
@@ -12,10 +12,14 @@ namespace qvg {
 // A token's part q.c of a score depends on its centroid alone: at the start of a page the workgroup contracts the page's tables
 // with its queries once and keeps the scores of all rows in LDS, where the tokens' accumulators start from what their ids name.
 // (Gathering K's rows as well, 256 bytes per token and side, the loop was bound by what the L2s give to gathers, about 10 TB/s:
-// one token over 12 heads x 187200
-// tokens of one round 125 us instead of 93.)  V's rows are gathered, 16 bytes per lane, row and octet.
-// A tile's codes and scales come in with a few wide loads a tile ahead; the V side's codes, all scales and ids pass through a
-// few KB of LDS that are the wavefront's own, where they are transposed: tokens become contiguous, so that a lane reads four tokens' levels or scales, already paired, at once.
+// one token over 12 heads x 187200 tokens of one round 125 us instead of 91.)  V's rows are gathered, 16 bytes per lane, row and
+// octet.  A tile's codes and scales come in with a few wide loads a tile ahead; the V side's codes, all scales and ids pass
+// through a few KB of LDS that are the wavefront's own, where they are transposed: tokens become contiguous, so that a lane
+// reads four tokens' levels or scales, already paired, at once.
+// What bounds it: without a rotation the vector instructions, 370 a tile for 16 rows of one round, two wavefronts to a SIMD
+// (registers); one token over 12 heads x 187200 tokens takes 91 us in one round (1.8 TB/s of stored bytes), 126 in two, 196 in
+// four (4.0 TB/s, near what a large copy reads).  With a rotation its rows, 256 bytes a token: 202 us in one round, of which the
+// L2s miss three quarters.
 template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB * 8 * 1024; }
 constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
 
@@ -382,6 +386,7 @@ static hipError_t launch_packed_form(const TreeArgs &a, int blocks, int lds, hip
 template <class F, bool ROPE, int RB>
 static hipError_t launch_packed_rb(TreeArgs a, int blocks, hipStream_t s) {
     constexpr int own = tree_query_bytes<RB>() + kTrWaves * F::wave_bytes;
+    // (two workgroups to a CU: 79 KB each and what the kernel declares itself)
     if constexpr (table_fits<F, ROPE, RB>()) {
         static_assert(own + F::S * kMaxClusters * 16 * RB * 4 + kTrWaves * 16 * RB * 8 <= 160 * 1024, "the largest table must fit a CU");
         int64_t met = a.t.page_len;

@@ -1,4 +1,5 @@
-// Attention over a paged cache for more than 64 query rows of a KV head (32 where keys are rotated): the wavefronts of a workgroup share what they decode.
+// Attention over a paged cache for more than 64 query rows of a KV head (32 where keys are rotated): the wavefronts of a workgroup
+// share what they decode.
 //
 // A workgroup takes 64 or 128 rows, RS wavefronts of 32 rows each, and walks its tiles in rounds of four: every wavefront decodes
 // one of them into the fragments of both contractions (8 KB each, K_hat and V_hat as binary16) in LDS, and then contracts
@@ -6,6 +7,8 @@
 // (RS = 2).  Decoding costs about 300 vector instructions a side, whatever the number of rows; a wavefront that decodes for 32
 // rows alone does it four times for 128.  While one workgroup of a CU decodes, the other contracts.
 // Between the barriers the V codes, scales and ids of the tile that is decoded lie where its V fragments will.
+// What bounds it: two workgroups of 64 KB to a CU, two wavefronts to a SIMD, which do not hide all waits (64 rows, two rounds:
+// vector instructions for 935 of 2057 cycles of a tile).  128 rows over 12 heads x 187200 tokens: 291 us in one round, 326 in two.
 #include "qvg_tree_lane.hpp"
 
 namespace qvg {
