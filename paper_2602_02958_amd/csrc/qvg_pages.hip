@@ -72,8 +72,9 @@ hipError_t launch_tree_mask(int n_seqs, int n_nodes, const int32_t *parents, con
 }
 
 // ---- kept tokens --------------------------------------------------------------------------------------
-// 16 lanes to a row of 128 bf16, both sides.  Bound by the launch: 64 paths over 40 heads, 31 MB both ways, take 7 us at the rate of
-// a copy and 12 us a call, which is the host's time for one.
+// 16 lanes to a row of 128 bf16, 16 rows of a path in one unit of a sequence to a workgroup.  64 paths over 40 heads, 31 MB both
+// ways, which a large copy takes 6 us for: 11.8 us, three loads one after the other in 15360 small workgroups (eight units to one
+// with all their loads in flight: 12.8).  A sequence alone takes 2.7 us (4.6).
 __global__ __launch_bounds__(256)
 void keep_nodes_kernel(KeepArgs a) {
     const unsigned unit = blockIdx.x / (unsigned)a.blocks;                // sequence and unit (K heads, then V heads)
@@ -134,7 +135,8 @@ __device__ __forceinline__ void copy_pieces(const uint8_t *src, uint8_t *dst, in
 }
 // Every field that a workgroup needs is asked for at once, the arrays' four descriptions among them: the arguments lie in memory
 // that is far away, and one after the other (or as a value, which indexed at run time every thread keeps in scratch memory)
-// they took 16 us of a copy of 1 MB, which takes 3 us so.  20 pages of 4680 tokens of 24 units, 714 MB both ways: 125 us, 5.7 TB/s.
+// they took 16 us of a copy of 1 MB, which takes 3 us so.  20 pages of 4680 tokens of 24 units, 714 MB both ways: 141 us,
+// 5.1 TB/s, the rate of a large copy.
 __global__ __launch_bounds__(256)
 void copy_pages_kernel(CopyArgs) {
     const CopyArgs &a = *(const CopyArgs *)__builtin_amdgcn_kernarg_segment_ptr();
