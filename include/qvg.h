@@ -398,8 +398,9 @@ typedef struct qvg_tree_step {
  *   - the tail_len[b] tokens of its tail,
  *   - the new tokens j < nodes[b] that the mask's row i names.
  * Rows i >= nodes[b] and rows that see no token at all get a zero output row and lse = -infinity.
- * A new token that no row sees may hold anything (also what is no number); every other value must be finite, keys, values
- * and decoded values of magnitude up to 65504.
+ * A new token that no row sees may hold anything (also what is no number), and so may what lies behind a sequence's new tokens
+ * or tail; every other value must be finite, keys, values, decoded values and the parts they are summed from of magnitude up
+ * to 65504, and so must the scaled scores be.
  *   k_*, v_*  the K and the V pool, [n_heads] units each, layout of a cache of pool_pages * page_len tokens per unit
  *   out       may be q with q's strides; it overlaps no other input
  *   scratch   optional, 16-byte aligned: with qvg_attn_tree_scratch_bytes bytes the sequences' tokens are dealt to several

@@ -613,7 +613,10 @@ def _attn_tree(q, k: Encoded, kp, vp, H, page_table, kv_len, k_new, v_new, tail_
         os_ = _rows4(out, "out", q.shape)
     lse = torch.empty(n, hq, m, dtype=torch.float32, device=q.device) if want_lse else None
     B, bits, fp8 = d // k.scales.shape[3], code_bytes * 8 // d, k.scale_format
-    if scratch is None:
+    if scratch is not None:
+        if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
+            raise ValueError("scratch: need a contiguous uint8 tensor")
+    else:
         scratch = _scratch(_tree_scratch_bytes(H, B, T, bits, k.n_smooth, fp8, n, hq // H, m, pages, L, R), q.device)
     # (fields in the struct's order: naming them costs more than the smallest call's launches)
     t = QvgTreeStep(n, hq // H, m, pages, L, max(1, k.ids.shape[1] // L), table, lens, q.data_ptr(), *qs,

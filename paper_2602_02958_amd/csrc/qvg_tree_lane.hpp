@@ -577,7 +577,10 @@ struct QueryRow {
     __device__ __forceinline__ void octet(int oct, float *v) const {
         unpack_bf16x8(at ? *reinterpret_cast<const uint4 *>(at + 8 * oct) : make_uint4(0u, 0u, 0u, 0u), v);
     }
-    __device__ __forceinline__ float scale(const TreeArgs &a) const { return __builtin_amdgcn_ldexpf(a.scale * 1.4426950408889634f, ex - 9); }
+    // (never zero: a hidden token's score is -inf times it; scores that small are zero against any other)
+    __device__ __forceinline__ float scale(const TreeArgs &a) const {
+        return fmaxf(__builtin_amdgcn_ldexpf(a.scale * 1.4426950408889634f, ex - 9), 1.17549435e-38f);
+    }
     // fragment i in the residual's order, of the lane's channels v (scaled already)
     template <class F>
     static __device__ __forceinline__ uint4 residual_fragment(const float (&v)[32], int i) {

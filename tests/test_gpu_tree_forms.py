@@ -254,3 +254,23 @@ def test_refusals_that_need_tensors_of_the_gpu():
     with pytest.raises(TypeError):
         cache.append(s, torch.zeros(2, 5, D, device="cuda"))
     assert cache.length(s) == 0
+
+
+@pytest.mark.parametrize("fmt", [dict(T=2), dict(T=1, B=16, S=4, fp8=True), dict(T=8, B=128)], ids=name)
+@pytest.mark.parametrize("g,m,rope", [(1, 3, False), (2, 9, False), (3, 15, True), (4, 40, False)])
+@pytest.mark.parametrize("q,scale", [(2.0 ** -126, 1e-3), (2.0 ** -133, 0.1), (2.0 ** -133, 1e-6), (0.0, 0.1), (1.0, 1e-38)])
+def test_queries_so_small_that_all_scores_are_zero(fmt, g, m, rope, q, scale):
+    """The row's scale leaves fp32's range; hidden tokens stay hidden, all others count alike."""
+    pool = Pool(2, 3, 50, K=12, seed=61, **fmt)
+    x = make(pool, 1, g, m, [110, 20], [5, 0], [m, 2], seed=62, rope=rope)
+    x["q"] = (torch.sign(x["q"].float()) * q).to(torch.bfloat16)
+    check(pool, x, call(pool, x, softmax_scale=scale), scale=scale)
+
+
+def test_a_scratch_that_is_no_plain_memory_is_refused():
+    pool = Pool(2, 6, 200, K=16, T=2, seed=63)
+    x = make(pool, 1, 1, 2, [1100], [9], [2], seed=64)
+    for bad in (torch.empty(1 << 21, dtype=torch.uint8, device="cuda")[::2], torch.empty(1 << 20, dtype=torch.float32, device="cuda"),
+                torch.empty(1 << 20, dtype=torch.uint8)):
+        with pytest.raises(ValueError):
+            call(pool, x, scratch=bad)
