@@ -812,16 +812,20 @@ class PagedCache:
     shares them and copies the tail only; `close` gives back those that no other sequence holds; `compact` moves the used ones
     to the pool's front.  A step attends with a row of new tokens for every place 0 .. max_seqs - 1 (places that are not open
     have none) and then keeps those that were accepted.
+    Keys are stored as they are attended to, or with pre_rope=True as they were before the rotary embedding (the codec's own
+    scheme): pages then hold them so and attend rotates them by their place (k_rope), while the tail holds both forms, the one
+    for the encoder and the one that is attended to.  append and keep take the stored form, and the rotated one beside it.
     Argument marshalling and page numbers only: every step runs in the library's kernels."""
 
     def __init__(self, heads, max_seqs, n_pages, page_len, max_pages, max_new, n_clusters, group_size, n_stages, init, head_dim=128,
-                 device="cuda", n_smooth=1, bits=2, scale_format=SCALE_F16, warm_iters=3, cold_iters=10):
-        self.heads, self.page_len, self.max_new = heads, page_len, max_new
+                 device="cuda", n_smooth=1, bits=2, scale_format=SCALE_F16, warm_iters=3, cold_iters=10, pre_rope=False):
+        self.heads, self.page_len, self.max_new, self.pre_rope = heads, page_len, max_new, pre_rope
         self.group_size, self.n_stages = group_size, n_stages
         self.init, self.warm_iters, self.cold_iters = init, warm_iters, cold_iters
         self.pool = alloc_cache(2 * heads, n_pages * page_len, page_len, n_clusters, group_size, n_stages, head_dim, device,
                                 n_smooth=n_smooth, bits=bits, scale_format=scale_format)
-        self.tail = torch.empty(max_seqs, 2 * heads, page_len + max_new, head_dim, dtype=torch.bfloat16, device=device)
+        # (units: K heads as stored, V heads, and with pre_rope the K heads as attended to)
+        self.tail = torch.empty(max_seqs, (3 if pre_rope else 2) * heads, page_len + max_new, head_dim, dtype=torch.bfloat16, device=device)
         self.table = torch.zeros(max_seqs, max_pages, dtype=torch.int32, device=device)
         self.kv_len = torch.zeros(max_seqs, dtype=torch.int32, device=device)
         self.tail_len = torch.zeros(max_seqs, dtype=torch.int32, device=device)
@@ -842,6 +846,15 @@ class PagedCache:
         if not 0 <= seq < len(self.pages) or self.pages[seq] is None:
             raise ValueError(f"sequence {seq} is not open")
         return self.pages[seq]
+
+    def _tails(self):
+        """The tails' K as attended to, and V."""
+        h = self.heads
+        return self.tail[:, 2 * h:] if self.pre_rope else self.tail[:, :h], self.tail[:, h:2 * h]
+
+    def _check_rotated(self, k_rotated):
+        if (k_rotated is not None) != self.pre_rope:
+            raise ValueError("k_rotated: needed by a cache of pre_rope keys, and by no other")
 
     def _place(self):
         if None not in self.pages:
@@ -904,19 +917,25 @@ class PagedCache:
         L, n = self.page_len, self.tails[seq]
         full = n // L * L
         for at in range(0, full, L):
-            self._encode(seq, self.tail[seq, :, at:at + L])
+            self._encode(seq, self.tail[seq, :2 * self.heads, at:at + L])
         if full and n > full:
             self.tail[seq, :, :n - full].copy_(self.tail[seq, :, full:n].clone())
         self.tails[seq] = n - full
         if full:
             self._tell(seq)
 
-    def append(self, seq, kv):
-        """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence."""
-        units, _, d = self.tail.shape[1:]
+    def append(self, seq, kv, k_rotated=None):
+        """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence.  pre_rope: kv
+        holds the keys before the rotary embedding, k_rotated [heads, n, d] bf16 the same ones rotated by their places."""
+        units, d = 2 * self.heads, self.tail.shape[3]
         if kv.dim() != 3 or kv.shape[0] != units or kv.shape[2] != d:
             raise ValueError(f"kv: need [{units}, n, {d}]")
         _check(kv, torch.bfloat16, "kv")
+        self._check_rotated(k_rotated)
+        if k_rotated is not None:
+            if k_rotated.shape != (self.heads, kv.shape[1], d):
+                raise ValueError(f"k_rotated: need [{self.heads}, {kv.shape[1]}, {d}]")
+            _check(k_rotated, torch.bfloat16, "k_rotated")
         n, L = kv.shape[1], self.page_len
         self._need({seq: n})
         at = 0
@@ -926,7 +945,10 @@ class PagedCache:
                 at += L
         while at < n:
             m = min(n - at, L - self.tails[seq])
-            self.tail[seq, :, self.tails[seq]:self.tails[seq] + m].copy_(kv[:, at:at + m])
+            rows = self.tail[seq, :, self.tails[seq]:self.tails[seq] + m]
+            rows[:units].copy_(kv[:, at:at + m])
+            if k_rotated is not None:
+                rows[units:].copy_(k_rotated[:, at:at + m])
             self.tails[seq] += m
             at += m
             self._seal(seq)
@@ -935,26 +957,33 @@ class PagedCache:
     def attend(self, q, k_new, v_new, n_nodes=None, mask=None, k_rope=None, softmax_scale=None, want_lse=False, out=None,
                scratch=None):
         """attn_tree of q [max_seqs, heads * group, N, d] over the sequences and the new tokens k_new, v_new
-        [max_seqs, heads, N, d].  n_nodes [max_seqs] int32: a place's new tokens (None: all N; pass 0 for places that are not
-        open, or ignore their rows)."""
+        [max_seqs, heads, N, d] (k_new as attended to).  n_nodes [max_seqs] int32: a place's new tokens (None: all N; pass 0 for
+        places that are not open, or ignore their rows).  k_rope [n, d/2, 2] float16: the rotary table of a cache of pre_rope
+        keys; no other takes one (its pages hold keys that are rotated already, or none is)."""
+        if (k_rope is not None) != self.pre_rope:
+            raise ValueError("k_rope: needed by a cache of pre_rope keys, and by no other")
         c, h = self.pool, self.heads
         kp = (c.centroids.data_ptr(), c.ids.data_ptr(), c.codes.data_ptr(), c.scales.data_ptr())
         vp = (kp[0] + h * c.centroids.stride(0) * 2, kp[1] + h * c.ids.stride(0) * c.ids.element_size(),
               kp[2] + h * c.codes.stride(0), kp[3] + h * c.scales.stride(0) * c.scales.element_size())
-        return _attn_tree(q, c, kp, vp, h, self.table, self.kv_len, k_new, v_new, self.tail[:, :h], self.tail[:, h:], self.tail_len,
-                          n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
+        return _attn_tree(q, c, kp, vp, h, self.table, self.kv_len, k_new, v_new, *self._tails(), self.tail_len, n_nodes, mask,
+                          softmax_scale, k_rope, want_lse, out, scratch)
 
-    def keep(self, k_new, v_new, path, n_keep):
+    def keep(self, k_new, v_new, path, n_keep, k_rotated=None):
         """Accepted new tokens become part of the sequences: path [max_seqs, M] int32 on the device (M <= max_new), the indices of
-        the kept ones in order; n_keep: how many of each, max_seqs Python integers."""
+        the kept ones in order; n_keep: how many of each, max_seqs Python integers.  pre_rope: k_new holds the keys before the
+        rotary embedding, k_rotated [max_seqs, heads, N, d] those that attend was given."""
+        self._check_rotated(k_rotated)
         n_keep = [int(n) for n in n_keep]
         if len(n_keep) != len(self.pages) or path.shape[1] > self.max_new or any(not 0 <= n <= path.shape[1] for n in n_keep):
             raise ValueError(f"n_keep: need {len(self.pages)} counts of at most {min(path.shape[1], self.max_new)} tokens")
         kept = {s: n for s, n in enumerate(n_keep) if n}
         self._need(kept)
         h = self.heads
-        keep_nodes(k_new, v_new, path, torch.tensor(n_keep, dtype=torch.int32, device=path.device), self.tail[:, :h],
-                   self.tail[:, h:], self.tail_len, out_len=self.tail_len)
+        count, (tail_k, tail_v) = torch.tensor(n_keep, dtype=torch.int32, device=path.device), self._tails()
+        if k_rotated is not None:                      # (and V, which comes again with the same values)
+            keep_nodes(k_rotated, v_new, path, count, tail_k, tail_v, self.tail_len)
+        keep_nodes(k_new, v_new, path, count, self.tail[:, :h], tail_v, self.tail_len, out_len=self.tail_len)
         for seq, n in kept.items():
             self.tails[seq] += n
             self._seal(seq)
