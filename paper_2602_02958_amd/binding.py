@@ -913,16 +913,19 @@ class PagedCache:
         pages.append(page)
 
     def _seal(self, seq):
-        """Full pages leave the tail."""
+        """Full pages leave the tail.  Those that an encoder's error kept there wait for the next call."""
         L, n = self.page_len, self.tails[seq]
-        full = n // L * L
-        for at in range(0, full, L):
-            self._encode(seq, self.tail[seq, :2 * self.heads, at:at + L])
-        if full and n > full:
-            self.tail[seq, :, :n - full].copy_(self.tail[seq, :, full:n].clone())
-        self.tails[seq] = n - full
-        if full:
-            self._tell(seq)
+        full = 0
+        try:
+            while n - full >= L:
+                self._encode(seq, self.tail[seq, :2 * self.heads, full:full + L])
+                full += L
+        finally:
+            if full:
+                if n > full:
+                    self.tail[seq, :, :n - full].copy_(self.tail[seq, :, full:n].clone())
+                self.tails[seq] = n - full
+                self._tell(seq)
 
     def append(self, seq, kv, k_rotated=None):
         """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence.  pre_rope: kv
@@ -938,21 +941,24 @@ class PagedCache:
             _check(k_rotated, torch.bfloat16, "k_rotated")
         n, L = kv.shape[1], self.page_len
         self._need({seq: n})
-        at = 0
-        if self.tails[seq] == 0:                       # whole pages need no way through the tail
-            while n - at >= L:
-                self._encode(seq, kv[:, at:at + L])
-                at += L
-        while at < n:
-            m = min(n - at, L - self.tails[seq])
-            rows = self.tail[seq, :, self.tails[seq]:self.tails[seq] + m]
-            rows[:units].copy_(kv[:, at:at + m])
-            if k_rotated is not None:
-                rows[units:].copy_(k_rotated[:, at:at + m])
-            self.tails[seq] += m
-            at += m
+        try:
             self._seal(seq)
-        self._tell(seq)
+            at = 0
+            if self.tails[seq] == 0:                   # whole pages need no way through the tail
+                while n - at >= L:
+                    self._encode(seq, kv[:, at:at + L])
+                    at += L
+            while at < n:
+                m = min(n - at, L - self.tails[seq])
+                rows = self.tail[seq, :, self.tails[seq]:self.tails[seq] + m]
+                rows[:units].copy_(kv[:, at:at + m])
+                if k_rotated is not None:
+                    rows[units:].copy_(k_rotated[:, at:at + m])
+                self.tails[seq] += m
+                at += m
+                self._seal(seq)
+        finally:                                       # (after an error: the tokens that length counts are there)
+            self._tell(seq)
 
     def attend(self, q, k_new, v_new, n_nodes=None, mask=None, k_rope=None, softmax_scale=None, want_lse=False, out=None,
                scratch=None):
@@ -979,6 +985,8 @@ class PagedCache:
             raise ValueError(f"n_keep: need {len(self.pages)} counts of at most {min(path.shape[1], self.max_new)} tokens")
         kept = {s: n for s, n in enumerate(n_keep) if n}
         self._need(kept)
+        for seq in kept:                               # (room for max_new behind less than a page)
+            self._seal(seq)
         h = self.heads
         count, (tail_k, tail_v) = torch.tensor(n_keep, dtype=torch.int32, device=path.device), self._tails()
         if k_rotated is not None:                      # (and V, which comes again with the same values)
@@ -986,6 +994,7 @@ class PagedCache:
         keep_nodes(k_new, v_new, path, count, self.tail[:, :h], tail_v, self.tail_len, out_len=self.tail_len)
         for seq, n in kept.items():
             self.tails[seq] += n
+        for seq in kept:
             self._seal(seq)
 
     def compact(self) -> int:

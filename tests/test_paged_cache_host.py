@@ -45,3 +45,73 @@ def test_append_takes_the_rotated_keys_beside_the_stored_ones(monkeypatch):
     assert plain.tail.shape[1] == 2 and torch.equal(plain.tail[s, :, :5], kv)
     u = pre.fork(t)
     assert torch.equal(pre.tail[u, :, :5], pre.tail[t, :, :5])
+
+
+class Host:
+    """The cache's kernels on the host: pages hold the tokens themselves; the n-th encode fails."""
+
+    def __init__(self, monkeypatch, fail_at):
+        self.pages, self.left = {}, fail_at
+        monkeypatch.setattr(B, "_check", lambda *a: None)
+        monkeypatch.setattr(B, "encode_chunk", self.encode)
+        monkeypatch.setattr(B, "keep_nodes", self.keep)
+
+    def encode(self, x, *a, chunk_index, **kw):
+        self.left -= 1
+        if self.left == 0:
+            raise B.QvgError(-6, "qvg_encode_chunk")
+        self.pages[chunk_index] = x.clone()
+
+    @staticmethod
+    def keep(k_new, v_new, path, n_keep, tail_k, tail_v, tail_len, out_len=None):
+        for b, n in enumerate(n_keep.tolist()):
+            at = int(tail_len[b])
+            tail_k[b, :, at:at + n], tail_v[b, :, at:at + n] = k_new[b, :, path[b, :n].long()], v_new[b, :, path[b, :n].long()]
+        out_len.copy_(tail_len + n_keep)
+
+    def tokens(self, c, s):
+        """What a sequence holds, as the device's copies of its pages and lengths say."""
+        n = int(c.kv_len[s]) // c.page_len
+        return torch.cat([self.pages[p] for p in c.table[s, :n].tolist()] + [c.tail[s, :, :int(c.tail_len[s])]], 1)
+
+
+@pytest.mark.parametrize("fail_at", [1, 2, 3])
+@pytest.mark.parametrize("first", [0, 5])
+def test_an_append_that_fails_leaves_what_it_has_taken_in(monkeypatch, fail_at, first):
+    c, kv = cache(n_pages=12, max_pages=8), torch.randn(2, 60, 128).to(torch.bfloat16)
+    host = Host(monkeypatch, fail_at)
+    s = c.open()
+    c.append(s, kv[:, :first])
+    with pytest.raises(B.QvgError):
+        c.append(s, kv[:, first:30])
+    for _ in range(2):
+        n = c.length(s)
+        assert n == int(c.kv_len[s]) + int(c.tail_len[s]) and len(c.pages[s]) == int(c.kv_len[s]) // 8 == 12 - c.free_pages()
+        assert torch.equal(host.tokens(c, s), kv[:, :n])
+        c.append(s, kv[:, n:n + 21])                       # and goes on from there
+    assert c.tails[s] < 8
+
+
+@pytest.mark.parametrize("fail_at", [1, 2, 3, 4])
+def test_a_keep_that_fails_while_encoding_has_kept_all(monkeypatch, fail_at):
+    """Two sequences with more new tokens than two pages hold: whichever encode fails, no token is lost or comes twice."""
+    c = cache(n_pages=12, max_pages=6)
+    host = Host(monkeypatch, fail_at)
+    kv = torch.randn(2, 2, 50, 128).to(torch.bfloat16)      # [sequence, unit, token]
+    path = torch.arange(20, dtype=torch.int32).expand(2, 20).contiguous()
+    for s in range(2):
+        c.open()
+        c.append(s, kv[s, :, :6])
+
+    def keep(at):
+        new = kv[:, :, at:at + 20]
+        c.keep(new[:, :1], new[:, 1:], path, [20, 20])
+
+    with pytest.raises(B.QvgError):
+        keep(6)
+    for s in range(2):
+        assert c.length(s) == int(c.kv_len[s]) + int(c.tail_len[s]) == 26
+        assert torch.equal(host.tokens(c, s), kv[s, :, :26])
+    keep(26)
+    for s in range(2):
+        assert c.length(s) == 46 and c.tails[s] == int(c.tail_len[s]) == 6 and torch.equal(host.tokens(c, s), kv[s, :, :46])
