@@ -655,7 +655,8 @@ int check_step_sizes(const qvg_params *p, const qvg_tree_step *t) {
     if (t->page_len < 1 || t->page_len > kMaxInt || t->pool_pages < 1 || t->pool_pages > kMaxInt) return QVG_ERR_BAD_PARAM;
     if (t->table_pages > 0 && t->page_len > kMaxInt / t->table_pages) return QVG_ERR_BAD_PARAM;
     // (tiles of 32 tokens, and blocks of query rows, are counted in 32 bits)
-    if (t->table_pages * ((t->page_len + 31) / 32) + (t->tail_capacity + 31) / 32 + (t->n_nodes + 31) / 32 > kMaxInt - 1024) return QVG_ERR_BAD_PARAM;
+    if ((int64_t)t->table_pages * tree_tiles((int)t->page_len) + tree_tiles(t->tail_capacity) + tree_tiles(t->n_nodes) > kMaxInt - 1024)
+        return QVG_ERR_BAD_PARAM;
     const int64_t rows = (int64_t)t->group * t->n_nodes, br = tree_block_rows(rows, false, false);
     if ((int64_t)t->n_seqs * p->n_heads * ((rows + br - 1) / br) > (1 << 30)) return QVG_ERR_BAD_PARAM;
     return QVG_OK;

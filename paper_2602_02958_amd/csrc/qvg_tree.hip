@@ -326,8 +326,7 @@ TreePlan tree_plan(const qvg_params &prm, const qvg_tree_step &t, bool rotated) 
     p.row_blocks = (int)((rows + br - 1) / br);
     const int64_t units = (int64_t)prm.n_heads * p.row_blocks;           // of a sequence
     if (t.n_seqs < 1 || rows < 1) return p;
-    const int64_t tiles = t.table_pages * ((t.page_len + kTrTile - 1) / kTrTile) + (t.tail_capacity + kTrTile - 1) / kTrTile +
-                          (t.n_nodes + kTrTile - 1) / kTrTile;
+    const int64_t tiles = (int64_t)t.table_pages * tree_tiles((int)t.page_len) + tree_tiles(t.tail_capacity) + tree_tiles(t.n_nodes);
     // As many workgroups as the chip holds at once (two to a CU), two tiles to a wavefront at least; not divided where that is
     // less than two workgroups to a sequence
     int64_t slots = 512 / units;

@@ -5,6 +5,10 @@
 
 namespace qvg {
 
+constexpr int kTrTile = 32;        // tokens of a tile
+// Tiles of 0 .. 2^31 - 1 tokens (the sum that rounds up may pass 31 bits).
+__host__ __device__ inline int tree_tiles(int tokens) { return (int)(((uint32_t)tokens + (uint32_t)(kTrTile - 1)) / (uint32_t)kTrTile); }
+
 struct PoolSide {                  // K or V pool: [H] units of pool_tokens tokens, pool_pages tables
     const bf16_t *cent; const uint8_t *ids; const uint8_t *codes; const uint8_t *scales;
 };

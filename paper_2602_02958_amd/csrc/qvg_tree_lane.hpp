@@ -7,7 +7,7 @@ namespace qvg {
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
 
-constexpr int kTrThreads = 256, kTrWaves = kTrThreads / 64, kTrTile = 32;
+constexpr int kTrThreads = 256, kTrWaves = kTrThreads / 64;
 constexpr float kTrNoScore = -3.402823466e38f;      // the running reference before any score (finite: see kNoScore)
 // Probabilities are taken against a reference kTrBelow under the row's maximum and the reference moves when a score is
 // kTrBelow + kTrLag above it: they stay below 2^14, and the small ones keep their bits in binary16 for longer.
@@ -29,11 +29,11 @@ __device__ __forceinline__ SeqTiles tiles_of_sequence(const qvg_tree_step &t, in
     if (s.nodes == 0) s.kv = s.tail = 0;                                 // no row: nothing to read
     // (table_pages * page_len < 2^31, so a page that holds a token is shorter)
     const int L = s.kv ? (int)t.page_len : 1;
-    s.per_page = (L + kTrTile - 1) / kTrTile;
+    s.per_page = tree_tiles(L);
     const int full = s.kv / L;
-    s.kv_tiles = full * s.per_page + (s.kv - full * L + kTrTile - 1) / kTrTile;
-    s.tail_tiles = (s.tail + kTrTile - 1) / kTrTile;
-    s.total = s.kv_tiles + s.tail_tiles + (s.nodes + kTrTile - 1) / kTrTile;
+    s.kv_tiles = full * s.per_page + tree_tiles(s.kv - full * L);
+    s.tail_tiles = tree_tiles(s.tail);
+    s.total = s.kv_tiles + s.tail_tiles + tree_tiles(s.nodes);
     return s;
 }
 

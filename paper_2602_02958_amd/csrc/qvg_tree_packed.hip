@@ -390,7 +390,8 @@ static hipError_t launch_packed_rb(TreeArgs a, int blocks, hipStream_t s) {
     if constexpr (table_fits<F, ROPE, RB>()) {
         static_assert(own + F::S * kMaxClusters * 16 * RB * 4 + kTrWaves * 16 * RB * 8 <= 160 * 1024, "the largest table must fit a CU");
         int64_t met = a.t.page_len;
-        if (a.slots && a.t.n_seqs * a.t.table_pages < a.slots) met = a.t.n_seqs * a.t.table_pages * a.t.page_len / a.slots;
+        const int64_t pages = (int64_t)a.t.n_seqs * a.t.table_pages;
+        if (a.slots && pages < a.slots) met = pages * a.t.page_len / a.slots;
         // Several stages' tables: columns for the rows that there are, where 16 would leave a CU one workgroup (one token, four
         // stages, 495 -> 391 us)
         const int64_t rows = (int64_t)a.t.group * a.t.n_nodes;
