@@ -85,8 +85,9 @@ void keep_nodes_kernel(KeepArgs a) {
     keep = keep < 0 ? 0 : (keep > a.n_path ? a.n_path : keep);
     len = len < 0 ? 0 : (len > a.capacity ? a.capacity : len);
     // (where the new lengths have a place of their own; else they wait for the rows to be done with the old ones)
-    if (a.lengths_here && u == 0 && i == 0 && c8 == 0) a.tail_len_out[b] = len + keep > a.capacity ? a.capacity : len + keep;
-    if (i >= keep || len + i >= a.capacity) return;
+    const int room = a.capacity - len;                                  // (len + keep may pass 31 bits)
+    if (a.lengths_here && u == 0 && i == 0 && c8 == 0) a.tail_len_out[b] = len + (keep < room ? keep : room);
+    if (i >= keep || i >= room) return;
     const int from = a.path[(int64_t)b * a.n_path + i];
     if (from < 0 || from >= a.n_nodes) return;
     const bf16_t *src = (side ? a.v_new : a.k_new) + b * a.new_seq + h * a.new_head + from * a.new_node;
@@ -101,7 +102,7 @@ void keep_lengths_kernel(KeepArgs a) {
     int keep = a.keep[b], len = a.tail_len[b];
     keep = keep < 0 ? 0 : (keep > a.n_path ? a.n_path : keep);
     len = len < 0 ? 0 : (len > a.capacity ? a.capacity : len);
-    a.tail_len_out[b] = len + keep > a.capacity ? a.capacity : len + keep;
+    a.tail_len_out[b] = len + (keep < a.capacity - len ? keep : a.capacity - len);
 }
 hipError_t launch_keep_nodes(const KeepArgs &a, hipStream_t s) {
     if (a.blocks > 0)

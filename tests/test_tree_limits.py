@@ -80,3 +80,18 @@ def test_a_tail_of_all_the_tokens_that_a_number_counts():
     # 128 products and the sum of weights in fp32, the logarithm: as tree_util.reference counts them
     e = 2.0 ** -20 * (float((q.double() * k.double()).abs().sum()) / math.sqrt(D) + 1 + abs(s + 31 * math.log(2)))
     assert abs(lse.item() - (s + math.log(TOP))) <= e
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+def test_kept_tokens_of_a_tail_that_is_nearly_as_long_as_a_number_counts(in_place):
+    """No path entry names a token, so no row is written; the lengths stop at the tail's end."""
+    B_, M = 3, 40
+    k = torch.zeros(B_, 1, 4, D, dtype=torch.bfloat16, device="cuda")
+    row = torch.full((1, 1, 1, D), 3.0, dtype=torch.bfloat16, device="cuda")
+    tail = row.expand(B_, 1, TOP, D)
+    path = torch.full((B_, M), -1, dtype=torch.int32, device="cuda")
+    keep = torch.tensor([M, 2, 3], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([TOP - 1, TOP - 2, TOP - 9], dtype=torch.int32, device="cuda")
+    got = B.keep_nodes(k, k, path, keep, tail, tail, lens, out_len=lens if in_place else None)
+    assert got.tolist() == [TOP, TOP, TOP - 6] and (row == 3.0).all()
