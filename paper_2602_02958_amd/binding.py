@@ -561,6 +561,7 @@ def attn_tree(q, k: Encoded, v: Encoded, page_table, kv_len, k_new, v_new, tail_
         raise ValueError("K and V pools must share shapes and parameters")
     _check_pool(k, "k")
     _check_stored(v.centroids, v.ids, v.codes, v.scales, v.centroids.shape[-2])          # (the shapes are k's)
+    _here(k.centroids, k.codes, k.scales, v.centroids, v.ids, v.codes, v.scales)
     return _attn_tree(q, k, (k.centroids.data_ptr(), k.ids.data_ptr(), k.codes.data_ptr(), k.scales.data_ptr()),
                       (v.centroids.data_ptr(), v.ids.data_ptr(), v.codes.data_ptr(), v.scales.data_ptr()), k.ids.shape[0], page_table,
                       kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
@@ -663,7 +664,7 @@ def copy_pages(cache: Encoded, src, dst, into: Encoded | None = None) -> Encoded
     L = cache.chunk_len
     units, pages, K, d = _check_pool(cache, "cache")
     into_pages = pages if into is cache else _check_pool(into, "into")[1]
-    _here(cache.ids, into.ids)
+    _here(*(t for c in (cache, into) for t in (c.centroids, c.ids, c.codes, c.scales)))
     T, code_bytes = cache.codes.shape[2:]
     p = QvgParams(units, d, K, d // cache.scales.shape[3], T, code_bytes * 8 // d, cache.n_smooth, 0, cache.scale_format)
     ints = C.c_int32 * len(src)
@@ -939,6 +940,7 @@ class PagedCache:
             if k_rotated.shape != (self.heads, kv.shape[1], d):
                 raise ValueError(f"k_rotated: need [{self.heads}, {kv.shape[1]}, {d}]")
             _check(k_rotated, torch.bfloat16, "k_rotated")
+        _here(self.tail, self.init, kv, k_rotated)
         n, L = kv.shape[1], self.page_len
         self._need({seq: n})
         try:

@@ -30,6 +30,7 @@ def test_keys_before_the_rotary_embedding_need_a_cache_of_such_keys():
 
 def test_append_takes_the_rotated_keys_beside_the_stored_ones(monkeypatch):
     monkeypatch.setattr(B, "_check", lambda *a: None)
+    monkeypatch.setattr(B, "_here", lambda *a: None)
     kv, rot = torch.randn(2, 5, 128).to(torch.bfloat16), torch.randn(1, 5, 128).to(torch.bfloat16)
     plain, pre = cache(), cache(pre_rope=True)
     s, t = plain.open(), pre.open()
@@ -53,6 +54,7 @@ class Host:
     def __init__(self, monkeypatch, fail_at):
         self.pages, self.left = {}, fail_at
         monkeypatch.setattr(B, "_check", lambda *a: None)
+        monkeypatch.setattr(B, "_here", lambda *a: None)
         monkeypatch.setattr(B, "encode_chunk", self.encode)
         monkeypatch.setattr(B, "keep_nodes", self.keep)
 
