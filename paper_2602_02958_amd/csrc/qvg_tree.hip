@@ -211,7 +211,7 @@ void tree_attn_kernel(TreeArgs a, int blocks, int per_xcd) {
             float top = x[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-            if (__ballot(top > m[rb] + (kTrBelow + kTrLag))) {            // uniform: some row's reference moves
+            if (__ballot(top - m[rb] > kTrBelow + kTrLag)) {            // uniform: some row's reference moves
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
                 const float m_new = fmaxf(m[rb], top - kTrBelow), alpha = __builtin_amdgcn_exp2f(m[rb] - m_new);

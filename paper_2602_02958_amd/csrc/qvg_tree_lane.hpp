@@ -519,7 +519,9 @@ struct TreeRows {
             for (int e = 0; e < 8; ++e)
                 s[rb][e >> 2][e & 3] = (see[rb] >> (16 * (e >> 2) + 4 * kb + (e & 3))) & 1u ? s[rb][e >> 2][e & 3] : -INFINITY;
     }
-    // The weights of the tile's scores: use(rb, x) gets the eight of block rb.
+    // The weights of the tile's scores: use(rb, x) gets the eight of block rb.  A score is rounded before the reference is taken
+    // from it, as the reference was, and the two are compared by their difference: fused, or against a rounded sum, a weight of
+    // scores beyond 2^24 left binary16's range.
     template <class Use>
     __device__ __forceinline__ void weights(Use use) {
         float top[RB];
@@ -528,7 +530,7 @@ struct TreeRows {
         for (int rb = 0; rb < RB; ++rb) {
             const floatx4_t &x = s[rb][0], &y = s[rb][1];
             top[rb] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))) * qs[rb];
-            move |= top[rb] > m[rb] + (kTrBelow + kTrLag);
+            move |= top[rb] - m[rb] > kTrBelow + kTrLag;
         }
         if (__ballot(move)) {                                            // uniform: some row's reference moves
 #pragma unroll
@@ -545,7 +547,7 @@ struct TreeRows {
         for (int rb = 0; rb < RB; ++rb) {
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][e >> 2][e & 3], qs[rb], -m[rb])); l[rb] += x[e]; }
+            for (int e = 0; e < 8; ++e) { x[e] = __builtin_amdgcn_exp2f(s[rb][e >> 2][e & 3] * qs[rb] - m[rb]); l[rb] += x[e]; }
             use(rb, x);
         }
     }
