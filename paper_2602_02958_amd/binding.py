@@ -494,6 +494,18 @@ def _here(*tensors):
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
 
 
+def _check_arrays(e: Encoded, K):
+    """A pool's arrays, all on one device (cheaper than asking each of them twice); returns it."""
+    cent, ids, codes, scales = e.centroids, e.ids, e.codes, e.scales
+    at = ids.get_device()
+    if not (cent.dtype is torch.bfloat16 and ids.dtype is id_dtype(K) and codes.dtype is torch.uint8 and
+            at >= 0 and cent.get_device() == at and codes.get_device() == at and scales.get_device() == at and
+            cent.is_contiguous() and ids.is_contiguous() and codes.is_contiguous() and scales.is_contiguous()):
+        _check_stored(cent, ids, codes, scales, K)
+        _here(cent, ids, codes, scales)
+    return at
+
+
 def _check_pool(e: Encoded, name):
     """The arrays of a pool agree with each other: whole pages, a set of tables to each.  Returns (units, pages, K, d)."""
     cent, S, L = e.centroids.shape, e.n_smooth, e.chunk_len
@@ -506,7 +518,7 @@ def _check_pool(e: Encoded, name):
             e.ids.shape != ((units, tokens) if S == 1 else (units, tokens, S))):
         raise ValueError(f"{name}: the pool's arrays are of different sizes")
     K, d = cent[-2:]
-    _check_stored(e.centroids, e.ids, e.codes, e.scales, K)
+    _check_arrays(e, K)
     return units, pages, K, d
 
 
@@ -560,8 +572,8 @@ def attn_tree(q, k: Encoded, v: Encoded, page_table, kv_len, k_new, v_new, tail_
             (k.ids.shape, k.codes.shape, k.scales.shape, k.scales.dtype, k.centroids.shape, k.chunk_len, k.n_smooth):
         raise ValueError("K and V pools must share shapes and parameters")
     _check_pool(k, "k")
-    _check_stored(v.centroids, v.ids, v.codes, v.scales, v.centroids.shape[-2])          # (the shapes are k's)
-    _here(k.centroids, k.codes, k.scales, v.centroids, v.ids, v.codes, v.scales)
+    if _check_arrays(v, v.centroids.shape[-2]) != k.ids.get_device():                    # (the shapes are k's)
+        _here(k.ids, v.ids)
     return _attn_tree(q, k, (k.centroids.data_ptr(), k.ids.data_ptr(), k.codes.data_ptr(), k.scales.data_ptr()),
                       (v.centroids.data_ptr(), v.ids.data_ptr(), v.codes.data_ptr(), v.scales.data_ptr()), k.ids.shape[0], page_table,
                       kv_len, k_new, v_new, tail_k, tail_v, tail_len, n_nodes, mask, softmax_scale, k_rope, want_lse, out, scratch)
@@ -664,7 +676,7 @@ def copy_pages(cache: Encoded, src, dst, into: Encoded | None = None) -> Encoded
     L = cache.chunk_len
     units, pages, K, d = _check_pool(cache, "cache")
     into_pages = pages if into is cache else _check_pool(into, "into")[1]
-    _here(*(t for c in (cache, into) for t in (c.centroids, c.ids, c.codes, c.scales)))
+    _here(cache.ids, into.ids)
     T, code_bytes = cache.codes.shape[2:]
     p = QvgParams(units, d, K, d // cache.scales.shape[3], T, code_bytes * 8 // d, cache.n_smooth, 0, cache.scale_format)
     ints = C.c_int32 * len(src)
