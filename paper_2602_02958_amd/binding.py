@@ -832,6 +832,8 @@ class PagedCache:
 
     def __init__(self, heads, max_seqs, n_pages, page_len, max_pages, max_new, n_clusters, group_size, n_stages, init, head_dim=128,
                  device="cuda", n_smooth=1, bits=2, scale_format=SCALE_F16, warm_iters=3, cold_iters=10, pre_rope=False):
+        if scale_format == SCALE_F16 and page_len * n_stages * (head_dim // group_size) % 8:
+            raise ValueError("page_len: a page's binary16 scales must fill multiples of 16 bytes (8 tokens always do)")
         self.heads, self.page_len, self.max_new, self.pre_rope = heads, page_len, max_new, pre_rope
         self.group_size, self.n_stages = group_size, n_stages
         self.init, self.warm_iters, self.cold_iters = init, warm_iters, cold_iters

@@ -117,3 +117,17 @@ def test_a_keep_that_fails_while_encoding_has_kept_all(monkeypatch, fail_at):
     keep(26)
     for s in range(2):
         assert c.length(s) == 46 and c.tails[s] == int(c.tail_len[s]) == 6 and torch.equal(host.tokens(c, s), kv[s, :, :46])
+
+
+@pytest.mark.parametrize("page_len,group_size,n_stages,fits", [(8, 128, 1, True), (7, 128, 1, False), (4, 64, 1, True), (6, 64, 1, False),
+                                                               (2, 64, 2, True), (1, 16, 1, True), (33, 64, 2, False), (33, 32, 2, True)])
+def test_pages_whose_scales_would_not_be_aligned_are_refused(page_len, group_size, n_stages, fits):
+    """The encoder writes binary16 scales from 16-byte boundaries on: the second page of such a pool could never be written."""
+    args = dict(page_len=page_len, group_size=group_size, n_stages=n_stages)
+    cache(scale_format=B.SCALE_E4M3, **args)
+    if fits:
+        c = cache(**args)
+        assert c.pool.scales[0, page_len:].data_ptr() % 16 == c.pool.scales.data_ptr() % 16
+    else:
+        with pytest.raises(ValueError, match="page_len"):
+            cache(**args)
