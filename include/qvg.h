@@ -399,8 +399,8 @@ typedef struct qvg_tree_step {
  *   - the new tokens j < nodes[b] that the mask's row i names.
  * Rows i >= nodes[b] and rows that see no token at all get a zero output row and lse = -infinity.
  * A new token that no row sees may hold anything (also what is no number), and so may what lies behind a sequence's new tokens
- * or tail; every other value must be finite, keys, values, decoded values and the parts they are summed from of magnitude up
- * to 65504, and so must the scaled scores be.
+ * or tail; every other value must be finite, and so must the scaled scores be.  Keys (also the rotated ones), values and the sums
+ * of any of the parts of decoded ones are of magnitude up to 65504.
  *   k_*, v_*  the K and the V pool, [n_heads] units each, layout of a cache of pool_pages * page_len tokens per unit
  *   out       may be q with q's strides; it overlaps no other input
  *   scratch   optional, 16-byte aligned: with qvg_attn_tree_scratch_bytes bytes the sequences' tokens are dealt to several
@@ -413,6 +413,9 @@ typedef struct qvg_tree_step {
  * binary16's step of 2^-24 below 2^-14), or where centroid rows and new tokens enter as stored in bf16 with probabilities of
  * 16 bits.  Sums of Eq. 7's rounds are formed in binary16 (one rounding a round, after the first) or fp32.  Scores,
  * normaliser and output are accumulated in fp32.
+ * What is fast: one smoothing stage of one to four rounds of 2-bit levels with binary16 scales (B = 64; 32 from two rounds on), or of
+ * one round with E4M3 scales (2-bit levels: B = 64 or 16, 4-bit: 64); four stages of one round with E4M3 scales (either levels, B = 16).
+ * Every other format that the encoder writes takes a general kernel, five to ten times as long.
  */
 int qvg_attn_tree(const qvg_params *p, const qvg_tree_step *t,
                   const void *k_centroids, const uint8_t *k_ids, const uint8_t *k_codes, const void *k_scales,

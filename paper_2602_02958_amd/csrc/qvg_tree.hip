@@ -17,8 +17,8 @@
 // start, so their weights are zero whatever comes first.
 //
 // The kernel here decodes a tile element by element with the format's sizes at run time: any format that the encoder
-// writes.  Its vector instructions bound it: a format of two rounds that took its way took ten times the packed form's time.  The formats of the package's configurations and presets
-// have qvg_tree_packed.hip and qvg_tree_wide.hip.
+// writes.  Its vector instructions bound it: five to ten times the packed form's time (qvg_tree.hpp).  The formats of the package's
+// configurations and presets have qvg_tree_packed.hip and qvg_tree_wide.hip.
 #include "qvg_tree_lane.hpp"
 
 namespace qvg {

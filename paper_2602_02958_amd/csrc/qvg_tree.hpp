@@ -26,7 +26,8 @@ struct TreeArgs {
 };
 // The stored formats of the package's configurations and of the paper's presets, and their neighbours in group size: X(rounds,
 // groups per token, E4M3 scales, 4-bit levels, smoothing stages).  They have kernels of their own; any other one is decoded
-// element by element (one token over 12 heads x 187200 tokens: 125 us in the packed form of two rounds, 1.2 ms so).
+// element by element (one token over 12 heads x 187200 tokens: two rounds 133 us in the packed form and, with E4M3 scales, 1.1 ms so;
+// one round of 4-bit levels with binary16 scales 0.7 ms, two smoothing stages 1.15 ms).
 #define QVG_TREE_FORMATS(X)                                                                                              \
     X(1, 2, true, false, 1) X(1, 8, true, false, 1) X(1, 8, true, false, 4) X(1, 2, true, true, 1) X(1, 8, true, true, 4) \
     X(1, 2, false, false, 1) X(2, 2, false, false, 1) X(2, 4, false, false, 1) X(3, 2, false, false, 1)                   \
@@ -38,8 +39,9 @@ inline bool tree_packed(int T, int G, int fmt, int S) {
     return false;
 }
 // Rows of a KV head (group * n_nodes) are taken in blocks of 16 or 32, which a wavefront holds, and in the packed formats of 64 or
-// 128, whose wavefronts share what they decode: beyond 64 rows (12 heads x 187200 tokens, two rounds, 128 rows: 335 us, in
-// blocks of 32 503 us; 64 rows 272 and 250), with a rotation, which costs more, beyond 32 (64 rows: 355 us, in blocks of 32 460).
+// 128, whose wavefronts share what they decode: beyond 64 rows (12 heads x 187200 tokens, two rounds, each pair timed on one box:
+// 128 rows shared 335 us and 503 in blocks of 32; 64 rows 272 and 255), with a rotation, which costs more, beyond 32 (64 rows 355
+// and 460).  As they are now: 128 rows 312 us, 64 rows in two blocks 245, rotated 64 rows 360.
 inline int tree_block_rows(int64_t rows, bool packed, bool rotated) {
     return rows <= 16 ? 16 : rows <= 32 || !packed ? 32 : rows > 64 ? 128 : rotated ? 64 : 32;
 }

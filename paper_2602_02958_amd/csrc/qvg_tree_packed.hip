@@ -3,7 +3,7 @@
 
 namespace qvg {
 
-// Up to four rounds of 2-bit levels, or one of 4-bit levels (any scale format, id width and number of smoothing stages).
+// The formats of QVG_TREE_FORMATS: up to four rounds of 2-bit levels, or one of 4-bit levels; any id width.
 // The sum over Eq. 7's parts is left to the contractions where that saves vector instructions, of which the decoding is
 // made: the centroid rows go to the matrix cores as they are stored, as bf16, and only the residual of the rounds,
 // sum_t s_t q_t, is formed, two elements at a time in packed binary16 arithmetic (one round: exact).  So S^T = C Q^T + R Q^T
@@ -16,10 +16,9 @@ namespace qvg {
 // octet.  A tile's codes and scales come in with a few wide loads a tile ahead; the V side's codes, all scales and ids pass
 // through a few KB of LDS that are the wavefront's own, where they are transposed: tokens become contiguous, so that a lane
 // reads four tokens' levels or scales, already paired, at once.
-// What bounds it: without a rotation the vector instructions, 370 a tile for 16 rows of one round, two wavefronts to a SIMD
-// (registers); one token over 12 heads x 187200 tokens takes 91 us in one round (1.8 TB/s of stored bytes), 126 in two, 196 in
-// four (4.0 TB/s, near what a large copy reads).  With a rotation its rows, 256 bytes a token: 202 us in one round, of which the
-// L2s miss three quarters.
+// What bounds it: without a rotation the vector instructions, 378 a tile for 16 rows of one round, two wavefronts to a SIMD
+// (registers); one token over 12 heads x 187200 tokens takes 93 us in one round (2.4 TB/s of stored bytes and tables), 133 in two,
+// 188 in four (3.8 TB/s).  With a rotation its rows, 256 bytes a token, of which the L2s miss three quarters: 192 us in one round.
 template <int RB> __host__ __device__ constexpr int tree_query_bytes() { return RB * 8 * 1024; }
 constexpr int kTrMeetBytes = kTrWaves * 16 * kTrPitch * 4;
 

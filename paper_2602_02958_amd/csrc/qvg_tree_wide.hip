@@ -7,8 +7,9 @@
 // (RS = 2).  Decoding costs about 300 vector instructions a side, whatever the number of rows; a wavefront that decodes for 32
 // rows alone does it four times for 128.  While one workgroup of a CU decodes, the other contracts.
 // Between the barriers the V codes, scales and ids of the tile that is decoded lie where its V fragments will.
-// What bounds it: two workgroups of 64 KB to a CU, two wavefronts to a SIMD, which do not hide all waits (64 rows, two rounds:
-// vector instructions for 935 of 2057 cycles of a tile).  128 rows over 12 heads x 187200 tokens: 291 us in one round, 326 in two.
+// What bounds it: two workgroups of 64 KB to a CU, two wavefronts to a SIMD, which do not hide all waits (two rounds over 12 heads x
+// 187200 tokens: with 128 rows vector instructions 48 % of the SIMDs' time and the matrix pipe 19 %, with 64 rotated rows 42 and 8 %).
+// 128 rows take 258 us in one round and 312 in two, rotated 439 in two; 64 rotated rows 281 and 360.
 #include "qvg_tree_lane.hpp"
 
 namespace qvg {
