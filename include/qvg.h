@@ -467,6 +467,124 @@ int qvg_copy_pages(const qvg_params *p, int64_t page_len, int64_t n_pairs, const
                    void *stream);
 
 /*
+ * Rotary positions.  A table holds (cos, sin) of an angle for every place and pair of channels; a row of a head's channels is turned
+ * pair by pair by the table's row of its place.
+ */
+enum {                     /* element types */
+    QVG_BF16 = 0, QVG_F16 = 1, QVG_F32 = 2
+};
+
+/* How rows are turned (a HOST structure; its pointers are device pointers). */
+typedef struct qvg_rotary {
+    const void *table;         /* [n_rows][n_pairs][2] (cos, sin); aligned to a pair (4 or 8 bytes), faster from 16 on            */
+    int32_t type;              /* QVG_F16 or QVG_F32                                                                              */
+    int32_t n_pairs;           /* 1 .. head_dim / 2: channels 0 .. 2 n_pairs - 1 of a row are turned, the others stay as they are  */
+    int64_t n_rows;            /* 1 .. 2^31 - 1; a place outside 0 .. n_rows - 1 takes the nearest row                             */
+    int32_t half;              /* 0: pair p is channels (2p, 2p + 1), as in qvg_attn_decode_ex; 1: channels (p, p + n_pairs)       */
+    int32_t reserved;          /* 0 */
+    const int32_t *positions;  /* [n_seqs][n_tokens] the tokens' places, or NULL: see the entry point                             */
+} qvg_rotary;
+
+/*
+ * The table of n_rows places:  out[i][p] = amplitude * (cos, sin)(place(i, axis[p]) * frequencies[p]).
+ *   frequencies  [n_pairs] double, device: radians per place, finite; the product with the place is taken in 64 bits and reduced there
+ *                to less than a turn, so a far place loses 2^-51 of its angle and no more
+ *   positions    [n_rows][n_axes] int32, device, or NULL (n_axes 1): place i is first + i
+ *   axis         [n_pairs] int32, HOST, read before the call returns: values in 0 .. n_axes - 1; or NULL: all 0
+ *   amplitude    finite (long contexts; 1 else)
+ *   out          [n_rows][n_pairs][2] of `type`, QVG_F16 or QVG_F32, 16-byte aligned
+ * n_pairs 1 .. 256, n_axes 1 .. 8, n_rows 0 .. 2^31 - 1; first 0 .. 2^31 - 1 and first + n_rows at most 2^31.
+ */
+int qvg_rope_table(int64_t n_rows, int32_t n_pairs, const double *frequencies, int64_t first, const int32_t *positions, int32_t n_axes,
+                   const int32_t *axis, float amplitude, int32_t type, void *out, void *stream);
+
+/*
+ * Rows turned:  (y0, y1) = (cos x0 - sin x1, sin x0 + cos x1) for every pair, one product and one fma in fp32 each, rounded to the type;
+ * backward: the gradient with respect to x of a gradient x with respect to y, (cos x0 + sin x1, cos x1 - sin x0).
+ *   type         QVG_BF16, QVG_F16 or QVG_F32, of x and out
+ *   x, out       [n_seqs][n_heads][n_tokens][head_dim], strides in elements; every row is 16-byte aligned and contiguous.  out may
+ *                be x with x's strides, and overlaps it in no other way
+ *   r            token i of sequence b stands at r->positions[b][i]; without positions at first[b] + i; without first at i
+ *   first        [n_seqs] int32, device, or NULL
+ * head_dim a multiple of 8 up to 512; n_seqs * n_tokens below 2^31.  Slower: half with n_pairs no multiple of 8.
+ */
+int qvg_rope(const qvg_rotary *r, int32_t type, int64_t n_seqs, int32_t n_heads, int64_t n_tokens, int32_t head_dim,
+             const void *x, int64_t x_stride_seq, int64_t x_stride_head, int64_t x_stride_token, const int32_t *first, int32_t backward,
+             void *out, int64_t out_stride_seq, int64_t out_stride_head, int64_t out_stride_token, void *stream);
+
+/*
+ * Caches of 16-bit pages: what is not compressed, or not yet.  A pool holds pages of page_len tokens of every KV head; a sequence is a
+ * list of pages, the same ones for all heads, of which it fills the first kv_len tokens.
+ */
+typedef struct qvg_page_cache {    /* a HOST structure; its pointers are device pointers */
+    int32_t type;              /* QVG_BF16 or QVG_F16                                                                             */
+    int32_t n_seqs;            /* 0 .. 65535                                                                                      */
+    int32_t n_heads;           /* KV heads, 1 .. 65535                                                                            */
+    int32_t head_dim;
+    int32_t table_pages;       /* entries of page_table per sequence, >= 0                                                        */
+    int32_t reserved;          /* 0 */
+    int64_t page_len;          /* tokens of a page, >= 1; table_pages * page_len at most 2^30                                     */
+    int64_t pool_pages;        /* pages of the pool, 1 .. 2^31 - 1                                                                */
+    const int32_t *page_table; /* [n_seqs][table_pages]: the sequence's pages in order; those behind its last are not looked at   */
+    const int32_t *kv_len;     /* [n_seqs] tokens, clamped to 0 .. table_pages * page_len                                         */
+    void *k_pages, *v_pages;   /* token t of page p of KV head h at h * stride_head + p * stride_page + t * stride_token elements;
+                                  rows of head_dim contiguous elements, 16-byte aligned                                           */
+    int64_t stride_head, stride_page;
+    int64_t stride_token;      /* 0 .. 2^24 */
+} qvg_page_cache;
+
+/*
+ * The new tokens' keys and values go behind the sequences:  token i of sequence b, i < n_live[b], to place kv_len[b] + i, its key turned
+ * on the way if r is given (without r->positions by the row of that place), its value as it is.
+ *   k_new, v_new  [n_seqs][n_heads][n_new][head_dim] of c->type, strides in elements, rows 16-byte aligned
+ *   n_live        [n_seqs] int32, device, clamped to 0 .. n_new; NULL: n_new
+ *   len_out       [n_seqs] int32 or NULL: kv_len[b] + n_live[b], at most table_pages * page_len; may be kv_len
+ * A token beyond the table, or whose page is outside 0 .. pool_pages - 1, is not written; nothing else of the pool is touched.
+ * Sequences that share a page must not write to the same places of it.  head_dim a multiple of 8 up to 512; n_seqs * n_new below 2^31.
+ */
+int qvg_append_pages(const qvg_page_cache *c, int64_t n_new, const void *k_new, const void *v_new, int64_t new_stride_seq,
+                     int64_t new_stride_head, int64_t new_stride_token, const int32_t *n_live, const qvg_rotary *r, int32_t *len_out,
+                     void *stream);
+
+/* What attends to a cache of 16-bit pages (a HOST structure; its pointers are device pointers). */
+typedef struct qvg_page_step {
+    int32_t group;             /* query heads per KV head, >= 1: query head h reads KV head h / group                             */
+    int32_t n_new;             /* query rows per sequence and head, >= 0; group * n_new <= 2^20                                   */
+    const int32_t *n_live;     /* [n_seqs], clamped to 0 .. n_new: rows that are there; NULL: n_new                               */
+    const void *q;             /* [n_seqs][n_heads * group][n_new][head_dim] of the cache's type, turned already; strides in
+                                  elements, rows 16-byte aligned                                                                  */
+    int64_t q_stride_seq, q_stride_head, q_stride_token;
+    int32_t causal;            /* 1: row i, at place kv_len - n_live + i, sees the tokens up to its place; 0: all kv_len           */
+    int32_t window;            /* > 0: of these only those from place - window + 1 on, and the first `sink`; 0: all                */
+    int32_t sink;              /* >= 0 */
+    int32_t reserved;          /* 0 */
+    void *out;                 /* like q, strides of its own                                                                      */
+    int64_t out_stride_seq, out_stride_head, out_stride_token;
+    float *lse;                /* [n_seqs][n_heads * group][n_new] fp32 natural-log sum of exp, or NULL                            */
+} qvg_page_step;
+
+/*
+ * Attention of a step's tokens over their sequences' pages, themselves among them (qvg_append_pages has put them there; kv_len counts
+ * them):  O = softmax(softmax_scale * Q K^T) V per query head.
+ * Rows i >= n_live[b], and rows that see no token, get a zero row and lse = -infinity.  What no row of a sequence sees may hold anything (also
+ * what is no number): tokens behind kv_len, tokens between the first `sink` and the first row's window, whose pages may be
+ * gone.  A page of a token that is seen, outside 0 .. pool_pages - 1, reads the nearest page of the pool.  All else must be
+ * finite, and so must the scaled scores.
+ *   head_dim 64, 96, 128, 192 or 256; n_seqs times n_heads times blocks of 32 of a KV head's query rows at most 2^23
+ *   out      may be q with q's strides; it overlaps no other input
+ *   scratch  optional, 16-byte aligned: with qvg_attn_pages_scratch_bytes bytes the sequences' tokens are dealt to several workgroups
+ *            per KV head, by the sequences' lengths, and one more launch joins their partial results.  NULL or less: undivided, which
+ *            differs by the order of fp32 sums.  Equal calls give equal bits; among others a sequence's result may differ by
+ *            that order too.  Contents are scratch: nothing has to be initialised and nothing survives the call.
+ * What is rounded: queries, keys and values enter the two contractions as they are, weights with 16 bits or more (two
+ * numbers of the type); scores, sums and output are fp32 until the output is rounded.
+ */
+int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softmax_scale, void *scratch, size_t scratch_bytes, void *stream);
+
+/* Bytes of scratch that let qvg_attn_pages divide a call of these sizes (the pointers are not looked at); 0 when it would not be. */
+int qvg_attn_pages_scratch_bytes(const qvg_page_cache *c, const qvg_page_step *t, size_t *out);
+
+/*
  * The two k-means steps on their own (Sec. 4.1), as the encoder runs them.
  * assign: ids_out[h][n] = index of the nearest centroid of unit h; workspace
  *         qvg_workspace_bytes(p, QVG_ENTRY_KMEANS_ASSIGN, N, 0) bytes.

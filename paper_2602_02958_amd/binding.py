@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import math
 import os
 from array import array
 from dataclasses import dataclass
@@ -21,11 +22,13 @@ _lib = None
 
 ENTRY_ENCODE, ENTRY_DECODE, ENTRY_ATTN, ENTRY_KMEANS_UPDATE, ENTRY_KMEANS_ASSIGN = 0, 1, 2, 3, 4
 SCALE_F16, SCALE_E4M3 = 0, 1
+TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # QVG_BF16, QVG_F16, QVG_F32
 
 EXPORTS = ["qvg_encode_chunk", "qvg_encode_chunk_static", "qvg_decode", "qvg_decode_ex", "qvg_attn_decode", "qvg_attn_decode_ex",
            "qvg_attn_decode_causal", "qvg_attn_decode_f32", "qvg_attn_decode_parts", "qvg_attn_scratch_bytes", "qvg_attn_scratch_bytes_causal",
            "qvg_attn_merge",
            "qvg_attn_tree", "qvg_attn_tree_scratch_bytes", "qvg_tree_mask", "qvg_keep_nodes", "qvg_copy_pages",
+           "qvg_rope_table", "qvg_rope", "qvg_append_pages", "qvg_attn_pages", "qvg_attn_pages_scratch_bytes",
            "qvg_kmeans_assign",
            "qvg_kmeans_update", "qvg_workspace_bytes", "qvg_compressed_bytes",
            "qvg_status_string", "qvg_version"]
@@ -49,6 +52,25 @@ class QvgTreeStep(C.Structure):
                 ("nodes", C.c_void_p), ("mask", C.c_void_p), ("k_rope_f16", C.c_void_p), ("rope_tokens", C.c_int64),
                 ("out", C.c_void_p), ("out_stride_seq", C.c_int64), ("out_stride_head", C.c_int64), ("out_stride_node", C.c_int64),
                 ("lse", C.c_void_p)]
+
+
+class QvgRotary(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("type", C.c_int32), ("n_pairs", C.c_int32), ("n_rows", C.c_int64), ("half", C.c_int32),
+                ("reserved", C.c_int32), ("positions", C.c_void_p)]
+
+
+class QvgPageCache(C.Structure):
+    _fields_ = [("type", C.c_int32), ("n_seqs", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("table_pages", C.c_int32),
+                ("reserved", C.c_int32), ("page_len", C.c_int64), ("pool_pages", C.c_int64), ("page_table", C.c_void_p), ("kv_len", C.c_void_p),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("stride_head", C.c_int64), ("stride_page", C.c_int64),
+                ("stride_token", C.c_int64)]
+
+
+class QvgPageStep(C.Structure):
+    _fields_ = [("group", C.c_int32), ("n_new", C.c_int32), ("n_live", C.c_void_p), ("q", C.c_void_p), ("q_stride_seq", C.c_int64),
+                ("q_stride_head", C.c_int64), ("q_stride_token", C.c_int64), ("causal", C.c_int32), ("window", C.c_int32), ("sink", C.c_int32),
+                ("reserved", C.c_int32), ("out", C.c_void_p), ("out_stride_seq", C.c_int64), ("out_stride_head", C.c_int64),
+                ("out_stride_token", C.c_int64), ("lse", C.c_void_p)]
 
 
 class QvgError(RuntimeError):
@@ -111,6 +133,17 @@ def lib():
         L.qvg_copy_pages.restype = C.c_int
         L.qvg_copy_pages.argtypes = [pp, i64, i64, C.POINTER(C.c_int32), C.POINTER(C.c_int32), i64, vp, u8p, u8p, vp,
                                      i64, vp, u8p, u8p, vp, vp]
+        L.qvg_rope_table.restype = C.c_int
+        L.qvg_rope_table.argtypes = [i64, C.c_int32, vp, i64, vp, C.c_int32, vp, C.c_float, C.c_int32, vp, vp]
+        pr, pc, ps = C.POINTER(QvgRotary), C.POINTER(QvgPageCache), C.POINTER(QvgPageStep)
+        L.qvg_rope.restype = C.c_int
+        L.qvg_rope.argtypes = [pr, C.c_int32, i64, C.c_int32, i64, C.c_int32, vp, i64, i64, i64, vp, C.c_int32, vp, i64, i64, i64, vp]
+        L.qvg_append_pages.restype = C.c_int
+        L.qvg_append_pages.argtypes = [pc, i64, vp, vp, i64, i64, i64, vp, pr, vp, vp]
+        L.qvg_attn_pages.restype = C.c_int
+        L.qvg_attn_pages.argtypes = [pc, ps, C.c_float, vp, C.c_size_t, vp]
+        L.qvg_attn_pages_scratch_bytes.restype = C.c_int
+        L.qvg_attn_pages_scratch_bytes.argtypes = [pc, ps, C.POINTER(C.c_size_t)]
         L.qvg_kmeans_assign.restype = C.c_int
         L.qvg_kmeans_assign.argtypes = [pp, i64, vp, i64, i64, vp, u8p, vp, C.c_size_t, vp]
         L.qvg_kmeans_update.restype = C.c_int
@@ -687,6 +720,217 @@ def copy_pages(cache: Encoded, src, dst, into: Encoded | None = None) -> Encoded
     if st != 0:
         raise QvgError(st, "qvg_copy_pages")
     return into
+
+
+def rope_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, trained=None, low=1.0, high=32.0, device="cuda"):
+    """Frequencies of a rotary embedding of `rotary_dim` channels and the amplitude that goes with them: (float64 [rotary_dim / 2],
+    float), base^(-2p / rotary_dim) radians a place.  For contexts `factor` times as long as those trained with:
+    scaling "linear": every frequency divided by factor (positions interpolated);
+    "base": the base raised to base * factor^(r / (r - 2)), r = rotary_dim: the slowest pair is divided by factor, the fastest one stays;
+    "bands": by the number of turns a pair makes in `trained` places: from `high` on as it is, below `low` divided by factor, between
+    them mixed in proportion; amplitude 0.1 ln(factor) + 1, which both sides of a score are multiplied by."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim: need an even number of channels")
+    if not (base > 0 and math.isfinite(base) and factor >= 1 and math.isfinite(factor)):
+        raise ValueError("base and factor: need finite numbers, base > 0 and factor >= 1")
+    n, amplitude = rotary_dim // 2, 1.0
+    if scaling == "base":
+        if n < 2:
+            raise ValueError("a single pair has no base to raise")
+        base *= factor ** (rotary_dim / (rotary_dim - 2))
+    f = [base ** (-p / n) for p in range(n)]
+    if scaling == "linear":
+        f = [x / factor for x in f]
+    elif scaling == "bands":
+        if trained is None or trained < 1 or not 0 <= low < high:
+            raise ValueError("bands: need the places trained with, and 0 <= low < high")
+        keep = [min(max((trained * x / (2 * math.pi) - low) / (high - low), 0.0), 1.0) for x in f]
+        f = [x * (k + (1 - k) / factor) for x, k in zip(f, keep)]
+        amplitude = 0.1 * math.log(factor) + 1.0
+    elif scaling not in (None, "base"):
+        raise ValueError(f"scaling: {scaling!r} is not one of None, 'linear', 'base', 'bands'")
+    return torch.tensor(f, dtype=torch.float64, device=device), amplitude
+
+
+def rope_table(n, frequencies, first=0, positions=None, axis=None, amplitude=1.0, dtype=torch.float16, out=None) -> torch.Tensor:
+    """qvg_rope_table -> [n, P, 2] (cos, sin), float16 (what the attention over compressed keys reads) or float32.  frequencies [P]
+    float64 (rope_frequencies), radians a place.  Row i is place first + i, or positions [n, A] int32 holds its place on each of A
+    axes (the frame, row and column of a video's token); axis: the axis of each pair, P Python integers (None: 0)."""
+    _check(frequencies, torch.float64, "frequencies")
+    if frequencies.dim() != 1 or not frequencies.is_contiguous():
+        raise ValueError("frequencies: need a contiguous [P] tensor")
+    if dtype not in (torch.float16, torch.float32):
+        raise TypeError("a table is float16 or float32")
+    P, A, pos, ax = frequencies.shape[0], 1, None, None
+    if positions is not None:
+        if positions.dim() != 2:
+            raise ValueError("positions: need [n, A]")
+        A = positions.shape[1]
+        pos = _ints(positions, (n, A), "positions")
+    if axis is not None:
+        if len(axis) != P:
+            raise ValueError(f"axis: need the axes of {P} pairs")
+        ax = (C.c_int32 * P).from_buffer(array("i", axis))               # (array: a number that does not fit 32 bits is an error)
+    if out is None:
+        out = torch.empty(n, P, 2, dtype=dtype, device=frequencies.device)
+    elif out.shape != (n, P, 2) or not out.is_contiguous():
+        raise ValueError(f"out: need a contiguous [{n}, {P}, 2] tensor")
+    else:
+        _check(out, dtype, "out")
+    _here(frequencies, positions, out)
+    st = lib().qvg_rope_table(n, P, frequencies.data_ptr(), first, pos, A, ax, amplitude, TYPES[dtype], out.data_ptr(), _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_rope_table")
+    return out
+
+
+def _rows_of(x, name, dtype=None, shape=None, written=False):
+    """[B, H, N, d] view with a contiguous last dim -> its three strides (of a dimension of one element 0, as in _rows4)."""
+    if x.dtype not in TYPES or not x.is_cuda or (dtype is not None and x.dtype is not dtype):
+        raise TypeError(f"{name}: expected a cuda tensor of {dtype or 'bfloat16, float16 or float32'}, got {x.dtype} on {x.device}")
+    if x.dim() != 4 or x.stride(3) != 1 or (shape is not None and x.shape != shape):
+        raise ValueError(f"{name}: need {'[B, H, N, d]' if shape is None else list(shape)} with unit stride along d")
+    a, b, c, _ = x.stride()
+    n = x.shape
+    if written and ((a == 0 and n[0] > 1) or (b == 0 and n[1] > 1) or (c == 0 and n[2] > 1)):
+        raise ValueError(f"{name}: rows that are written lie in places of their own")
+    return (0 if n[0] == 1 else a), (0 if n[1] == 1 else b), (0 if n[2] == 1 else c)
+
+
+def _rotary(table, half, positions, shape) -> QvgRotary:
+    if table.dtype is not torch.float16 and table.dtype is not torch.float32 or not table.is_cuda:
+        raise TypeError(f"a rotary table is a float16 or float32 cuda tensor, got {table.dtype} on {table.device}")
+    if table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous() or table.shape[0] < 1:
+        raise ValueError("a rotary table is a contiguous [n, P, 2] tensor")
+    return QvgRotary(table.data_ptr(), TYPES[table.dtype], table.shape[1], table.shape[0], 1 if half else 0, 0,
+                     None if positions is None else _ints(positions, shape, "positions"))
+
+
+def rope(x, table, positions=None, first=None, half=False, backward=False, out=None) -> torch.Tensor:
+    """qvg_rope: rows of x [B, H, N, d] (bf16, float16 or float32) turned by a table [n, P, 2] (rope_table): the first 2P of their channels
+    in pairs (2p, 2p + 1), or with half=True (p, p + P).  Token i of sequence b stands at positions[b, i] (int32 [B, N]), or at first[b] + i
+    (int32 [B]), or at i; beyond the table the nearest row counts.  backward: the gradient with respect to the rows of a gradient x
+    with respect to the turned rows.  out may be x."""
+    xs = _rows_of(x, "x")
+    n, H, m, d = x.shape
+    if positions is not None and first is not None:
+        raise ValueError("positions and first both say where tokens stand")
+    r = _rotary(table, half, positions, (n, m))
+    if out is None:
+        out = torch.empty(n, H, m, d, dtype=x.dtype, device=x.device)
+        os_ = (H * m * d, m * d, d)
+    else:
+        os_ = _rows_of(out, "out", x.dtype, x.shape, True)
+        if out is not x and out.data_ptr() == x.data_ptr() and os_ != xs:
+            raise ValueError("out: a view of x needs x's strides")
+    _here(x, table, positions, first, out)
+    st = lib().qvg_rope(C.byref(r), TYPES[x.dtype], n, H, m, d, x.data_ptr(), *xs, None if first is None else _ints(first, (n,), "first"),
+                        1 if backward else 0, out.data_ptr(), *os_, _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_rope")
+    return out
+
+
+def alloc_pages(heads, n_pages, page_len, head_dim=128, dtype=torch.bfloat16, device="cuda"):
+    """Uninitialised pages of a cache in 16 bits: (k_pages, v_pages), [heads, n_pages, page_len, head_dim] each."""
+    pool = torch.empty(2, heads, n_pages, page_len, head_dim, dtype=dtype, device=device)
+    return pool[0], pool[1]
+
+
+def _page_cache(k_pages, v_pages, page_table, kv_len, written=False) -> QvgPageCache:
+    if k_pages.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("k_pages: pages are bfloat16 or float16")
+    ks = _rows_of(k_pages, "k_pages", None, None, written)
+    if _rows_of(v_pages, "v_pages", k_pages.dtype, k_pages.shape) != ks:
+        raise ValueError("k_pages and v_pages must share their strides")
+    H, P, L, d = k_pages.shape
+    n, pages = page_table.shape if page_table.dim() == 2 else (-1, 0)
+    return QvgPageCache(TYPES[k_pages.dtype], n, H, d, pages, 0, L, P, _ints(page_table, (n, pages), "page_table"), _ints(kv_len, (n,), "kv_len"),
+                        k_pages.data_ptr(), v_pages.data_ptr(), *ks)
+
+
+def append_pages(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new=None, k_rope=None, positions=None, half=False,
+                 out_len=None) -> torch.Tensor:
+    """qvg_append_pages: the new tokens' K and V [B, H, N, d] go behind B sequences in pages k_pages, v_pages [H, P, L, d] (alloc_pages; any
+    views with unit stride along d that share their strides, a token's heads side by side among them).  page_table [B, M] int32: the
+    sequences' pages, kv_len [B] int32: their tokens so far, n_new [B] int32: how many of the N are there (None: all).
+    k_rope [n, P, 2]: K is turned on the way, by the row of its place in the sequence, or of positions [B, N] int32; half as in rope.
+    Returns the new lengths [B] int32 (out_len, which may be kv_len, or a new tensor).  Tokens beyond the table, and those of pages
+    outside the pool, are left out."""
+    c = _page_cache(k_pages, v_pages, page_table, kv_len, True)
+    ns = _rows_of(k_new, "k_new", k_pages.dtype)
+    n, H, m, d = k_new.shape
+    if n != c.n_seqs or H != c.n_heads or d != c.head_dim:
+        raise ValueError(f"k_new: need [{c.n_seqs}, {c.n_heads}, N, {c.head_dim}]")
+    if _rows_of(v_new, "v_new", k_pages.dtype, k_new.shape) != ns:
+        raise ValueError("k_new and v_new must share their strides")
+    r = None
+    if k_rope is not None:
+        r = _rotary(k_rope, half, positions, (n, m))
+    elif positions is not None:
+        raise ValueError("positions without k_rope: keys are not turned")
+    out_len = torch.empty_like(kv_len) if out_len is None else out_len
+    _here(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new, k_rope, positions, out_len)
+    st = lib().qvg_append_pages(C.byref(c), m, k_new.data_ptr(), v_new.data_ptr(), *ns, None if n_new is None else _ints(n_new, (n,), "n_new"),
+                                None if r is None else C.byref(r), _ints(out_len, (n,), "out_len"), _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_append_pages")
+    return out_len
+
+
+@functools.lru_cache(maxsize=256)
+def _pages_scratch_bytes(n_seqs, H, d, group, n_new, table_pages, page_len) -> int:
+    """Bytes of scratch of an attn_pages of these sizes (a function of its arguments alone)."""
+    need = C.c_size_t()
+    c = QvgPageCache(n_seqs=n_seqs, n_heads=H, head_dim=d, table_pages=table_pages, page_len=page_len, pool_pages=1)
+    st = lib().qvg_attn_pages_scratch_bytes(C.byref(c), C.byref(QvgPageStep(group=group, n_new=n_new)), C.byref(need))
+    if st != 0:
+        raise QvgError(st, "qvg_attn_pages_scratch_bytes")
+    return need.value
+
+
+def attn_pages_scratch(k_pages, n_seqs, group, n_new, table_pages) -> torch.Tensor:
+    """Scratch for an attn_pages of these sizes over the pages k_pages."""
+    H, _, L, d = k_pages.shape
+    return torch.empty(_pages_scratch_bytes(n_seqs, H, d, group, n_new, table_pages, L), dtype=torch.uint8, device=k_pages.device)
+
+
+def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True, window=None, sink=0, softmax_scale=None, want_lse=False,
+               out=None, scratch=None):
+    """qvg_attn_pages: attention of the new tokens' queries q [B, H * group, N, d] over their sequences' pages (append_pages; kv_len [B] counts
+    the new tokens) -> out like q (and lse fp32 [B, H * group, N]); query head h reads KV head h // group.
+    n_new [B] int32: how many of the N there are (None: all); row i of a sequence stands at place kv_len - n_new + i and sees the
+    tokens up to its place (causal), or all kv_len, and with a window only the newest `window` of its place and the first `sink` tokens.
+    Rows behind n_new, and those that see nothing, are zero with lse -inf.
+    scratch: uint8 tensor of attn_pages_scratch bytes for dividing the call over the chip; without one it is taken from torch's
+    allocator (where that has no memory left the call runs undivided, which differs by the order of fp32 sums)."""
+    c = _page_cache(k_pages, v_pages, page_table, kv_len)
+    qs = _rows_of(q, "q", k_pages.dtype)
+    n, hq, m, d = q.shape
+    H = c.n_heads
+    if n != c.n_seqs or d != c.head_dim or hq < H or hq % H:
+        raise ValueError(f"q: need [{c.n_seqs}, a multiple of {H} heads, N, {c.head_dim}]")
+    if window is not None and window < 1:
+        raise ValueError("window: a row sees its own place at least (None: no window)")
+    if out is None:
+        out = torch.empty(n, hq, m, d, dtype=q.dtype, device=q.device)
+        os_ = (hq * m * d, m * d, d)
+    else:
+        os_ = _rows_of(out, "out", q.dtype, q.shape, True)
+    lse = torch.empty(n, hq, m, dtype=torch.float32, device=q.device) if want_lse else None
+    if scratch is not None:
+        if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
+            raise ValueError("scratch: need a contiguous uint8 tensor")
+    else:
+        scratch = _scratch(_pages_scratch_bytes(n, H, d, hq // H, m, c.table_pages, c.page_len), q.device)
+    _here(q, k_pages, v_pages, page_table, kv_len, n_new, out, scratch)
+    t = QvgPageStep(hq // H, m, None if n_new is None else _ints(n_new, (n,), "n_new"), q.data_ptr(), *qs, 1 if causal else 0,
+                    0 if window is None else min(window, 0x7fffffff), min(sink, 0x7fffffff), 0, out.data_ptr(), *os_, _ptr(lse))
+    st = lib().qvg_attn_pages(C.byref(c), C.byref(t), 1.0 / (d ** 0.5) if softmax_scale is None else softmax_scale,
+                              _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
+    if st != 0:
+        raise QvgError(st, "qvg_attn_pages")
+    return (out, lse) if want_lse else out
 
 
 def kmeans_assign(x, centroids) -> torch.Tensor:

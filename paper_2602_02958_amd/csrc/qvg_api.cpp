@@ -8,6 +8,7 @@
 
 #include "qvg.h"
 #include "qvg_internal.hpp"
+#include "qvg_rows.hpp"
 #include "qvg_tree.hpp"
 
 using namespace qvg;
@@ -805,6 +806,170 @@ int qvg_copy_pages(const qvg_params *p, int64_t page_len, int64_t n_pairs, const
         arrays[k] = PageArray{from[k], to[k], bytes, bytes * src_pool_pages, bytes * dst_pool_pages};
     }
     return launch_copy_pages(arrays, p->n_heads, n_pairs, src, dst, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+}  // extern "C"
+
+// ---- rotary positions, caches of 16-bit pages -----------------------------------------------------
+namespace {
+
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// rows of elements of `size` bytes, strides in elements: every row starts at a multiple of 16 bytes
+bool rows_aligned(const void *base, int size, int64_t seq, int64_t head, int64_t row) {
+    return aligned16(base) && ((seq | head | row) & (16 / size - 1)) == 0;
+}
+constexpr int kMaxRow = 512;                       // channels of a row that is turned or put into pages
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // of a sequence's table of 16-bit pages
+
+int check_rotary(const qvg_rotary *r, int head_dim) {
+    if (r->type != QVG_F16 && r->type != QVG_F32) return QVG_ERR_BAD_PARAM;
+    if (r->n_pairs < 1 || r->n_pairs > head_dim / 2 || r->n_rows < 1 || r->n_rows > kMaxInt || (r->half != 0 && r->half != 1) || r->reserved != 0)
+        return QVG_ERR_BAD_PARAM;
+    return QVG_OK;
+}
+int check_rotary_pointers(const qvg_rotary *r) {
+    if (!r->table) return QVG_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(r->table) & (r->type == QVG_F32 ? 7u : 3u)) != 0 || !aligned4(r->positions)) return QVG_ERR_ALIGN;
+    return QVG_OK;
+}
+
+// the sizes of a cache of 16-bit pages (not its pointers)
+int check_cache(const qvg_page_cache *c) {
+    if (!c) return QVG_ERR_NULL;
+    if (c->type != QVG_BF16 && c->type != QVG_F16) return QVG_ERR_BAD_PARAM;
+    if (c->n_seqs < 0 || c->n_seqs > 65535 || c->n_heads < 1 || c->n_heads > 65535 || c->head_dim < 1 || c->table_pages < 0 || c->reserved != 0)
+        return QVG_ERR_BAD_PARAM;
+    if (c->page_len < 1 || c->page_len > kMaxInt || c->pool_pages < 1 || c->pool_pages > kMaxInt) return QVG_ERR_BAD_PARAM;
+    if (c->table_pages > 0 && c->page_len > kMaxTokens / c->table_pages) return QVG_ERR_BAD_PARAM;
+    if (c->stride_token < 0 || c->stride_token > (1 << 24)) return QVG_ERR_BAD_PARAM;
+    return QVG_OK;
+}
+int check_cache_pointers(const qvg_page_cache *c) {
+    if (!c->kv_len || (c->table_pages > 0 && (!c->page_table || !c->k_pages || !c->v_pages))) return QVG_ERR_NULL;
+    if (c->table_pages > 0 && (!rows_aligned(c->k_pages, 2, c->stride_head, c->stride_page, c->stride_token) || !aligned16(c->v_pages)))
+        return QVG_ERR_ALIGN;
+    return aligned4(c->page_table) && aligned4(c->kv_len) ? QVG_OK : QVG_ERR_ALIGN;
+}
+int check_page_step(const qvg_page_cache *c, const qvg_page_step *t) {
+    int st = check_cache(c);
+    if (st != QVG_OK) return st;
+    if (!t) return QVG_ERR_NULL;
+    if (t->group < 1 || t->n_new < 0 || (int64_t)t->group * t->n_new > (1 << 20) || (t->causal != 0 && t->causal != 1) || t->window < 0 ||
+        t->sink < 0 || t->reserved != 0)
+        return QVG_ERR_BAD_PARAM;
+    if (!page_attn_dim(c->head_dim)) return QVG_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)t->group * t->n_new;
+    if ((int64_t)c->n_seqs * c->n_heads * ((rows + 31) / 32) > (1 << 23)) return QVG_ERR_BAD_PARAM;
+    return QVG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qvg_rope_table(int64_t n_rows, int32_t n_pairs, const double *frequencies, int64_t first, const int32_t *positions, int32_t n_axes,
+                   const int32_t *axis, float amplitude, int32_t type, void *out, void *stream) {
+    if (n_rows < 0 || n_rows > kMaxInt || n_pairs < 1 || n_pairs > 256 || n_axes < 1 || n_axes > 8) return QVG_ERR_BAD_PARAM;
+    if ((type != QVG_F16 && type != QVG_F32) || amplitude - amplitude != 0.0f) return QVG_ERR_BAD_PARAM;
+    if (!positions && (n_axes != 1 || first < 0 || first > kMaxInt || first + n_rows > kMaxInt + 1)) return QVG_ERR_BAD_PARAM;
+    for (int p = 0; axis && p < n_pairs; ++p)
+        if (axis[p] < 0 || axis[p] >= n_axes) return QVG_ERR_BAD_PARAM;
+    if (n_rows == 0) return QVG_OK;
+    if (!frequencies || !out) return QVG_ERR_NULL;
+    if (!aligned16(out) || (reinterpret_cast<uintptr_t>(frequencies) & 7u) || !aligned4(positions)) return QVG_ERR_ALIGN;
+    RopeTableArgs a{n_rows, n_pairs, n_axes, first, frequencies, positions, amplitude, out, {}};
+    for (int p = 0; axis && p < n_pairs; ++p) a.axis[p] = (uint8_t)axis[p];
+    return launch_rope_table(a, type == QVG_F32, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+int qvg_rope(const qvg_rotary *r, int32_t type, int64_t n_seqs, int32_t n_heads, int64_t n_tokens, int32_t head_dim, const void *x,
+             int64_t x_stride_seq, int64_t x_stride_head, int64_t x_stride_token, const int32_t *first, int32_t backward, void *out,
+             int64_t out_stride_seq, int64_t out_stride_head, int64_t out_stride_token, void *stream) {
+    if (!r) return QVG_ERR_NULL;
+    if (type != QVG_BF16 && type != QVG_F16 && type != QVG_F32) return QVG_ERR_BAD_PARAM;
+    if (n_seqs < 0 || n_heads < 1 || n_heads > 65535 || n_tokens < 0 || n_seqs > kMaxInt || n_tokens > kMaxInt || n_seqs * n_tokens > kMaxInt)
+        return QVG_ERR_BAD_PARAM;
+    if (head_dim < 8 || head_dim > kMaxRow || head_dim % 8 || (backward != 0 && backward != 1)) return QVG_ERR_BAD_PARAM;
+    int st = check_rotary(r, head_dim);
+    if (st != QVG_OK) return st;
+    if (n_seqs == 0 || n_tokens == 0) return QVG_OK;
+    if (!x || !out) return QVG_ERR_NULL;
+    if ((st = check_rotary_pointers(r)) != QVG_OK) return st;
+    const int size = type == QVG_F32 ? 4 : 2;
+    if (!rows_aligned(x, size, x_stride_seq, x_stride_head, x_stride_token) ||
+        !rows_aligned(out, size, out_stride_seq, out_stride_head, out_stride_token) || !aligned4(first))
+        return QVG_ERR_ALIGN;
+    if (x == out && (x_stride_seq != out_stride_seq || x_stride_head != out_stride_head || x_stride_token != out_stride_token))
+        return QVG_ERR_BAD_PARAM;
+    TurnArgs a{};
+    a.x = x; a.out = out;
+    a.x_seq = x_stride_seq; a.x_head = x_stride_head; a.x_tok = x_stride_token;
+    a.o_seq = out_stride_seq; a.o_head = out_stride_head; a.o_tok = out_stride_token;
+    a.r = *r; a.first = first; a.backward = backward;
+    a.H = n_heads; a.d = head_dim; a.n_tokens = (int)n_tokens; a.tokens = n_seqs * n_tokens;
+    return launch_rope(a, type, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+int qvg_append_pages(const qvg_page_cache *c, int64_t n_new, const void *k_new, const void *v_new, int64_t new_stride_seq,
+                     int64_t new_stride_head, int64_t new_stride_token, const int32_t *n_live, const qvg_rotary *r, int32_t *len_out,
+                     void *stream) {
+    int st = check_cache(c);
+    if (st != QVG_OK) return st;
+    if (n_new < 0 || n_new > kMaxTokens || c->n_seqs * n_new > kMaxInt) return QVG_ERR_BAD_PARAM;
+    if (c->head_dim % 8 || c->head_dim > kMaxRow) return QVG_ERR_BAD_PARAM;
+    if (r && (st = check_rotary(r, c->head_dim)) != QVG_OK) return st;
+    if (c->n_seqs == 0) return QVG_OK;
+    if ((st = check_cache_pointers(c)) != QVG_OK) return st;
+    const bool rows = n_new > 0 && c->table_pages > 0;
+    if (rows && (!k_new || !v_new)) return QVG_ERR_NULL;
+    if (rows && r && (st = check_rotary_pointers(r)) != QVG_OK) return st;
+    if (rows && (!rows_aligned(k_new, 2, new_stride_seq, new_stride_head, new_stride_token) || !aligned16(v_new))) return QVG_ERR_ALIGN;
+    if (!aligned4(n_live) || !aligned4(len_out)) return QVG_ERR_ALIGN;
+    TurnArgs a{};
+    a.x = k_new; a.v = v_new;
+    a.x_seq = new_stride_seq; a.x_head = new_stride_head; a.x_tok = new_stride_token;
+    if (r) a.r = *r;
+    a.H = c->n_heads; a.d = c->head_dim; a.n_tokens = (int)n_new; a.tokens = rows ? c->n_seqs * n_new : 0;
+    a.k_pages = c->k_pages; a.v_pages = c->v_pages; a.head = c->stride_head; a.page = c->stride_page; a.tok = c->stride_token;
+    a.table = c->page_table; a.kv_len = c->kv_len; a.live = n_live; a.len_out = len_out;
+    a.table_pages = c->table_pages; a.capacity = (int)(c->table_pages * c->page_len); a.pool_pages = (uint32_t)c->pool_pages;
+    a.by_page = fast_div((uint32_t)c->page_len);
+    const uintptr_t was = reinterpret_cast<uintptr_t>(c->kv_len), live = reinterpret_cast<uintptr_t>(n_live), now = reinterpret_cast<uintptr_t>(len_out),
+                    size = (uintptr_t)c->n_seqs * sizeof(int32_t);
+    auto apart = [&](uintptr_t x) { return now >= x + size || x >= now + size; };
+    a.lengths_here = rows && len_out && apart(was) && (!n_live || apart(live));
+    return launch_append(a, c->n_seqs, c->type, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
+}
+
+int qvg_attn_pages_scratch_bytes(const qvg_page_cache *c, const qvg_page_step *t, size_t *out) {
+    const int st = check_page_step(c, t);
+    if (st != QVG_OK) return st;
+    if (!out) return QVG_ERR_NULL;
+    *out = page_plan(*c, *t).state_bytes;
+    return QVG_OK;
+}
+
+int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softmax_scale, void *scratch, size_t scratch_bytes, void *stream) {
+    int st = check_page_step(c, t);
+    if (st != QVG_OK) return st;
+    if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return QVG_ERR_BAD_PARAM;   // positive, finite
+    if (c->n_seqs == 0 || t->n_new == 0) return QVG_OK;
+    if ((st = check_cache_pointers(c)) != QVG_OK) return st;
+    if (!t->q || !t->out) return QVG_ERR_NULL;
+    if (!rows_aligned(t->q, 2, t->q_stride_seq, t->q_stride_head, t->q_stride_token) ||
+        !rows_aligned(t->out, 2, t->out_stride_seq, t->out_stride_head, t->out_stride_token) || !aligned4(t->n_live) || !aligned4(t->lse) ||
+        !aligned16(scratch))
+        return QVG_ERR_ALIGN;
+    const PagePlan plan = page_plan(*c, *t);
+    PageAttnArgs a{};
+    a.c = *c; a.t = *t; a.scale = softmax_scale * 1.4426950408889634f;
+    a.paged = plan.paged; a.rows = plan.rows; a.row_blocks = plan.row_blocks;
+    a.by_page = fast_div((uint32_t)c->page_len);
+    a.by_tiles = fast_div((uint32_t)page_tiles((int)c->page_len));
+    a.slots = scratch && scratch_bytes >= plan.state_bytes ? plan.slots : 0;
+    a.state = static_cast<float *>(scratch);
+    if (a.slots) a.places = reinterpret_cast<int2 *>(static_cast<char *>(scratch) + plan.state_bytes - (size_t)c->n_seqs * sizeof(int2));
+    return launch_attn_pages(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
 }
 
 }  // extern "C"

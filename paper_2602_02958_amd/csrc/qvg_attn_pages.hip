@@ -1,0 +1,554 @@
+// Attention of a step's tokens over a cache of 16-bit pages:
+//     o = sum_n w_n v_n / sum_n w_n,   w_n = exp(scale q.k_n),
+// in one pass over the tokens with the running maximum and sum of the soft-max.
+//
+// A workgroup takes a block of 16 or 32 query rows of one KV head (rows = group x new tokens) and a part of the sequence's tiles of
+// 32 tokens; each of its wavefronts walks tiles of its own, so a tile costs no barrier.  Both contractions run on
+// v_mfma_f32_16x16x32 with the operands where the loads put them, so keys and values pass through registers only:
+//   S^T = K Q^T:   lane (c, kb) reads channels 32 i + 8 kb .. + 7 of tokens c and 16 + c;
+//   O^T += V^T P:  lane (c, kb) reads an octet of channels (c, and 16 + c beyond 128) of tokens 4 kb + r and 16 + 4 kb + r, which
+//                  are the tokens whose scores S^T leaves in the lane: P needs no movement, and pairs of tokens are packed
+//                  channel by channel (v_perm_b32), which is the transposition.  MFMA j makes channels 8 c + j; the lane ends
+//                  up with octets 4 kb + r of query row c.
+// The weights enter as two numbers of the cache's type, w = hi + lo: the matrix cores have nothing else to do, and one number's
+// rounding (2^-8 of a bf16 weight) would be as large as the output's own.
+// A tile's keys are asked for when the one before has been contracted, and so are its values: a wavefront has 16 KB (of 128
+// channels) on their way all the time.  Memory bounds it.
+#include "qvg_rows.hpp"
+
+namespace qvg {
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
+
+constexpr int kPgThreads = 256, kPgWaves = kPgThreads / 64;
+constexpr float kPgNoScore = -3.402823466e38f;      // the running reference before any score
+// Weights are exp2(score - reference) x 2^kPgUp, and the reference moves when a score is kPgLag above it: they stay below 2^14, and
+// the small ones of a row keep their bits in binary16 for longer.
+constexpr float kPgUp = 7.0f, kPgLag = 7.0f;
+
+struct PgBf16 {
+    static __device__ __forceinline__ floatx4_t mfma(const uint4 &a, const uint4 &b, const floatx4_t &c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) { return pack_bf16x2(x, y); }
+    static __device__ __forceinline__ float lo(uint32_t w) { return bf16_lo(w); }
+    static __device__ __forceinline__ float hi(uint32_t w) { return bf16_hi(w); }
+};
+struct PgF16 {
+    static __device__ __forceinline__ floatx4_t mfma(const uint4 &a, const uint4 &b, const floatx4_t &c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8_t, a), __builtin_bit_cast(halfx8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) { return pack_f16x2_rne(x, y); }
+    static __device__ __forceinline__ float lo(uint32_t w) { return f16_bits_to_f32(w & 0xffffu); }
+    static __device__ __forceinline__ float hi(uint32_t w) { return f16_bits_to_f32(w >> 16); }
+};
+// How a head of D channels lies in the operands: CH channels to a lane and set, NS sets of 16 lanes
+template <int D> struct PgDim {
+    static constexpr int CH = D > 64 ? 8 : 4, NS = (D + 16 * CH - 1) / (16 * CH), KK = D / 32, W = CH / 2;
+    static constexpr int pitch = 16 * CH + 4;       // floats per row of a set where the wavefronts' results meet
+};
+
+// What a sequence's rows see, together: tokens 0 .. sink - 1 and lo .. kv - 1; and in tiles.
+struct Span { int kv, live, sink, lo, sink_tiles, main_tile, total; };
+__device__ __forceinline__ int tile_of(const PageAttnArgs &a, int n) {
+    if (!a.paged) return n / kPgTile;
+    const int pi = (int)quotient((uint32_t)n, a.by_page);
+    return pi * (int)a.by_tiles.d + (n - pi * (int)a.by_page.d) / kPgTile;
+}
+__device__ __forceinline__ Span span_of(const PageAttnArgs &a, int b) {
+    auto clamp = [](int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); };
+    Span s;
+    s.kv = a.c.table_pages ? clamp(a.c.kv_len[b], (int)(a.c.table_pages * a.c.page_len)) : 0;
+    s.live = a.t.n_live ? clamp(a.t.n_live[b], a.t.n_new) : a.t.n_new;
+    s.sink = s.lo = s.sink_tiles = s.main_tile = s.total = 0;
+    if (s.live == 0) s.kv = 0;                                           // no row: nothing to read
+    if (s.kv == 0) return s;
+    const int place = s.kv - s.live;                                     // of the first row
+    if (a.t.window > 0 && place >= a.t.window) {
+        s.lo = place - a.t.window + 1;
+        s.sink = a.t.sink < s.lo ? a.t.sink : s.lo;
+        if (s.sink == s.lo) s.sink = s.lo = 0;                           // no gap
+    }
+    s.sink_tiles = s.sink ? tile_of(a, s.sink - 1) + 1 : 0;
+    const int from = tile_of(a, s.lo), end = tile_of(a, s.kv - 1) + 1;
+    s.main_tile = from > s.sink_tiles ? from : s.sink_tiles;
+    s.total = s.sink_tiles + (end > s.main_tile ? end - s.main_tile : 0);
+    return s;
+}
+
+// How the slots of a divided call (a.slots of them, the same for every head and row block) are dealt to the sequences: a slot for every q
+// tiles or part of them, and one at least, with the smallest q for which the slots suffice, or nearly: it lies between total / slots
+// and total / (slots - n), since the sum of ceil(T / q) over n sequences is at most total / q + n, and is found in five halvings.
+// Every wavefront works that out for itself from the lengths, which only the device knows (n <= 256: a call of more sequences
+// is not divided).  Slots that are left over have nothing to do.
+struct Slot { int b, part, parts, first; };                              // first: the sequence's first slot; parts: 0, none
+__device__ __forceinline__ int parts_of(int total, int q) {
+    const int p = (int)(((uint32_t)total + (uint32_t)q - 1u) / (uint32_t)q);
+    return p < 1 ? 1 : p;
+}
+template <typename N>
+__device__ __forceinline__ N lanes_sum(N x) {
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) x += __shfl_xor(x, off, 64);
+    return x;
+}
+constexpr int kPgLeast = 2 * kPgWaves;              // tiles of a part: two to a wavefront
+__device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot) {
+    const int lane = threadIdx.x & 63, n = a.c.n_seqs;
+    int tiles[4];                                                        // of sequences lane, 64 + lane, ..
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        tiles[k] = 0;
+        if (64 * k < n && 64 * k + lane < n) tiles[k] = span_of(a, 64 * k + lane).total;
+    }
+    int q;
+    if (n == 1) q = (__builtin_amdgcn_readfirstlane(tiles[0]) + a.slots - 1) / a.slots;
+    else {
+        const int64_t total = lanes_sum((int64_t)tiles[0] + tiles[1] + tiles[2] + tiles[3]);
+        int lo = (int)((total + a.slots - 1) / a.slots);
+        q = (int)((total + a.slots - n - 1) / (a.slots - n));
+        for (int i = 0; i < 5 && lo < q; ++i) {                          // uniform
+            const int mid = lo + (q - lo) / 2;
+            int need = 0;
+            if (mid > 0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (64 * k < n) need += 64 * k + lane < n ? parts_of(tiles[k], mid) : 0;
+            if (mid > 0 && lanes_sum(need) <= a.slots) q = mid; else lo = mid + 1;
+        }
+    }
+    if (q < kPgLeast) q = kPgLeast;
+    Slot p{0, 0, 0, 0};
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int base = 64 * k, i = base + lane;
+        if (base >= n) break;                                            // uniform
+        const int mine = i < n ? parts_of(tiles[k], q) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const int x = __shfl_up(upto, off, 64);
+            if (lane >= off) upto += x;
+        }
+        upto += before;
+        const unsigned long long hit = __ballot(mine > 0 && slot >= upto - mine && slot < upto);
+        if (hit) {
+            const int at = __builtin_ctzll(hit);
+            p.b = base + at; p.parts = __shfl(mine, at, 64); p.first = __shfl(upto, at, 64) - p.parts;
+            p.part = slot - p.first;
+            break;
+        }
+        before = __shfl(upto, 63, 64);
+    }
+    p.b = __builtin_amdgcn_readfirstlane(p.b); p.part = __builtin_amdgcn_readfirstlane(p.part);
+    p.parts = __builtin_amdgcn_readfirstlane(p.parts); p.first = __builtin_amdgcn_readfirstlane(p.first);
+    return p;
+}
+// A part's partial result: [rows][D] sums, then the rows' references, then their sums of weights.
+static __host__ __device__ inline int64_t part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
+
+// Where a query row lies: head h * group + r / n_new, row r % n_new of the sequence.
+struct RowAt { int64_t head; int i; };
+__device__ __forceinline__ RowAt row_at(const PageAttnArgs &a, int h, int64_t r) {
+    RowAt p;
+    const int u = (int)((uint32_t)r / (uint32_t)a.t.n_new);
+    p.head = (int64_t)h * a.t.group + u; p.i = (int)r - u * a.t.n_new;
+    return p;
+}
+// Store CH channels of a row from `ch` on: unnormalised sums o, the row's reference m and sum l of weights.
+template <class T, int CH>
+__device__ __forceinline__ void store_part(const PageAttnArgs &a, int b, int h, int64_t r, int live, int ch, const float *o, float m, float l) {
+    const RowAt p = row_at(a, h, r);
+    const bool seen = p.i < live && l > 0.0f;
+    const float inv = seen ? 1.0f / l : 0.0f;
+    uint32_t w[CH / 2];
+#pragma unroll
+    for (int e = 0; e < CH / 2; ++e) w[e] = seen ? T::pack(o[2 * e] * inv, o[2 * e + 1] * inv) : 0u;
+    uint16_t *out = static_cast<uint16_t *>(a.t.out) + b * a.t.out_stride_seq + p.head * a.t.out_stride_head + p.i * a.t.out_stride_token + ch;
+    if constexpr (CH == 8) *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
+    if (a.t.lse && ch == 0)
+        a.t.lse[((int64_t)b * a.c.n_heads * a.t.group + p.head) * a.t.n_new + p.i] =
+            seen ? (m + (__builtin_log2f(l) - kPgUp)) * 0.6931471805599453f : -INFINITY;
+}
+
+// A tile: tokens first .. first + count - 1 of the sequence, of which those from `last` on are not there and those in sink .. lo - 1
+// are seen by no row.
+struct Tile { int first, last, page_index; int64_t page; };
+
+// A lane's tokens of a tile are places in its page (paged), or rows anywhere in the pool, which lanes 0 .. 31 look up and leave in LDS.
+template <class T, int D, int RB, bool PAGED>
+__global__ __launch_bounds__(kPgThreads, D > 192 || D * RB > 256 ? 1 : 2)
+void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
+    typedef PgDim<D> G;
+    constexpr int kRows = 16 * RB, KK = G::KK, NS = G::NS, CH = G::CH, W = G::W;
+    __shared__ __attribute__((aligned(16))) float meet[kPgWaves][16][G::pitch];
+    __shared__ float ms[kPgWaves][kRows], ls[kPgWaves][kRows];
+    __shared__ __attribute__((aligned(16))) int64_t rows_of[PAGED ? 1 : kPgWaves][2][kPgTile];
+    // workgroups are dealt to the 8 XCDs round-robin: a head's row blocks, which read the same tokens, run on one
+    const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
+    if (w >= blocks) return;                                             // uniform, before any barrier
+    const int units = a.c.n_heads * a.row_blocks, slot = w / units, unit = w - slot * units;
+    const int h = unit / a.row_blocks, rblk = unit - h * a.row_blocks;
+    int b = slot, part = 0, parts = 1;
+    if (a.slots) {
+        const Slot s = deal(a, slot);
+        if (s.parts == 0 || s.part >= s.parts) return;                   // uniform, before any barrier
+        b = s.b; part = s.part; parts = s.parts;
+        if (unit == 0 && part == 0 && threadIdx.x == 0) a.places[b] = make_int2(s.first, parts);
+    }
+    const Span sq = span_of(a, b);
+    const int lo_tile = (int)((int64_t)sq.total * part / parts), hi_tile = (int)((int64_t)sq.total * (part + 1) / parts);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, kb = lane >> 4;
+    const int64_t rows = (int64_t)a.t.group * a.t.n_new;
+    const uint16_t *kp = static_cast<const uint16_t *>(a.c.k_pages) + h * a.c.stride_head;
+    const uint16_t *vp = static_cast<const uint16_t *>(a.c.v_pages) + h * a.c.stride_head;
+    const uint32_t row_bytes = (uint32_t)a.c.stride_token * 2u;
+
+    // Q, and what each row sees: tokens below up[rb] that are at least low[rb], or below the sink.  Rows that are not there are
+    // zeros, whose results nobody stores.
+    uint4 q[RB][KK];
+    int up[RB], low[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int64_t r = (int64_t)rblk * kRows + rb * 16 + c;
+        up[rb] = low[rb] = 0;
+        const uint16_t *qp = nullptr;
+        if (r < rows) {
+            const RowAt p = row_at(a, h, r);
+            if (p.i < sq.live) {
+                const int place = sq.kv - sq.live + p.i;
+                up[rb] = a.t.causal ? place + 1 : sq.kv;
+                low[rb] = a.t.window > 0 && place >= a.t.window ? place - a.t.window + 1 : 0;
+                qp = static_cast<const uint16_t *>(a.t.q) + b * a.t.q_stride_seq + p.head * a.t.q_stride_head + p.i * a.t.q_stride_token;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KK; ++i) q[rb][i] = qp ? *reinterpret_cast<const uint4 *>(qp + 32 * i + 8 * kb) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    // tokens that every row of the sequence sees: all_low .. all_up - 1
+    const int all_up = a.t.causal ? sq.kv - sq.live + 1 : sq.kv;
+    const int all_low = a.t.window > 0 && sq.kv - 1 >= a.t.window ? sq.kv - a.t.window : 0;
+
+    // ---- where a tile's tokens lie ------------------------------------------------------------
+    auto tile_at = [&](int v) {                                          // the sequence's v-th tile
+        const int ti = v < sq.sink_tiles ? v : v - sq.sink_tiles + sq.main_tile;
+        Tile x;
+        if (PAGED) {
+            x.page_index = (int)quotient((uint32_t)ti, a.by_tiles);
+            x.first = x.page_index * (int)a.by_page.d + (ti - x.page_index * (int)a.by_tiles.d) * kPgTile;
+            x.last = min(min(x.first + kPgTile, (x.page_index + 1) * (int)a.by_page.d), sq.kv);
+        } else { x.page_index = 0; x.first = ti * kPgTile; x.last = min(x.first + kPgTile, sq.kv); }
+        x.page = 0;
+        return x;
+    };
+    auto in_pool = [&](int pg) -> int64_t { return pg < 0 ? 0 : (pg >= a.c.pool_pages ? a.c.pool_pages - 1 : pg); };
+    const int32_t *table = a.c.page_table + (int64_t)b * a.c.table_pages;
+    // token `off` of a tile, or one that some row sees instead of it
+    auto seen_token = [&](const Tile &x, int off) {
+        int n = min(x.first + off, x.last - 1);
+        if (n >= sq.sink && n < sq.lo) n = sq.lo < x.last ? sq.lo : sq.sink - 1;
+        return n;
+    };
+    // (not paged) the rows of a tile's tokens: their pages are asked for a tile ahead
+    struct Ahead { int n, in_page; int64_t page; };
+    auto ask = [&](const Tile &x) {
+        Ahead p;
+        p.n = seen_token(x, lane & 31);
+        const int pi = (int)quotient((uint32_t)p.n, a.by_page);
+        p.in_page = p.n - pi * (int)a.by_page.d;
+        p.page = in_pool(table[pi]);
+        return p;
+    };
+    auto park = [&](const Ahead &p, int par) {
+        if (lane < 32) rows_of[PAGED ? 0 : wave][par][lane] = p.page * a.c.stride_page + (int64_t)p.in_page * a.c.stride_token;
+        asm volatile("" ::: "memory");                                   // the wavefront's LDS operations stay in this order
+    };
+    auto row_ptr = [&](const uint16_t *pool, const Tile &x, int par, int off) {
+        if constexpr (PAGED) {
+            const int n = seen_token(x, off) - x.page_index * (int)a.by_page.d;
+            return reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(pool + x.page * a.c.stride_page) + (uint64_t)((uint32_t)n) * row_bytes);
+        } else return pool + rows_of[PAGED ? 0 : wave][par][off];
+    };
+    uint4 kr[2][KK];
+    uint32_t vr[NS][8][W];
+    auto load_k = [&](const Tile &x, int par) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint16_t *p = row_ptr(kp, x, par, 16 * hf + c) + 8 * kb;
+#pragma unroll
+            for (int i = 0; i < KK; ++i) kr[hf][i] = *reinterpret_cast<const uint4 *>(p + 32 * i);
+        }
+    };
+    auto load_v = [&](const Tile &x, int par) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint16_t *p = row_ptr(vp, x, par, 16 * (e >> 2) + 4 * kb + (e & 3));
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int oct = min(16 * s + c, D / CH - 1);             // (octets beyond the head: results that nobody stores)
+                if constexpr (CH == 8) __builtin_memcpy(vr[s][e], reinterpret_cast<const uint4 *>(p + oct * CH), 16);
+                else __builtin_memcpy(vr[s][e], reinterpret_cast<const uint2 *>(p + oct * CH), 8);
+            }
+        }
+    };
+
+    floatx4_t O[RB][NS][CH];
+    float m[RB], l[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = kPgNoScore; l[rb] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) O[rb][s][j] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    int v = lo_tile + wave, par = 0;
+    Tile x{}, nx{};
+    Ahead ahead{};
+    auto find = [&](int at) {                                            // tile `at`, or the part's last one
+        const Tile y0 = tile_at(min(at, hi_tile - 1));
+        if constexpr (PAGED) { Tile y = y0; y.page = in_pool(((const __attribute__((address_space(4))) int32_t *)table)[y.page_index]); return y; }
+        else { ahead = ask(y0); return y0; }
+    };
+    if (v < hi_tile) {
+        x = find(v);
+        if (!PAGED) park(ahead, 0);
+        load_k(x, 0);
+        nx = find(v + kPgWaves);
+        load_v(x, 0);
+    }
+    for (; v < hi_tile; v += kPgWaves) {
+        // ---- S^T = K Q^T -------------------------------------------------------------------
+        floatx4_t S[RB][2];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                S[rb][hf] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < KK; ++i) S[rb][hf] = T::mfma(kr[hf][i], q[rb][i], S[rb][hf]);
+            }
+        // (behind the last tile that one comes again: behind a branch around these loads the values' wait would be for all of them)
+        __builtin_amdgcn_sched_barrier(0);                               // (loads before their registers' last use would need others)
+        if (!PAGED) park(ahead, par ^ 1);
+        const Tile nnx = find(v + 2 * kPgWaves);                         // (its page is waited for behind these keys otherwise)
+        load_k(nx, par ^ 1);
+
+        // ---- soft-max: the lane has tokens 16 hf + 4 kb + r of row c ------------------------
+        const bool all = x.last - x.first == kPgTile && x.first >= all_low && x.last <= all_up;     // uniform
+        uint4 ph[RB], pl[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = S[rb][e >> 2][e & 3] * a.scale;
+            if (!all) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int n = x.first + 16 * (e >> 2) + 4 * kb + (e & 3);
+                    p[e] = n < x.last && n < up[rb] && (n >= low[rb] || n < a.t.sink) ? p[e] : -INFINITY;
+                }
+            }
+            float top = p[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, p[e]);
+            if (__ballot(top - m[rb] > kPgLag)) {                        // uniform: some row's reference moves
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float m_new = fmaxf(m[rb], top), alpha = __builtin_amdgcn_exp2f(m[rb] - m_new);
+                l[rb] *= alpha; m[rb] = m_new;
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int j = 0; j < CH; ++j) O[rb][s][j] *= alpha;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f((p[e] - m[rb]) + kPgUp); l[rb] += p[e]; }
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                hi[e] = T::pack(p[2 * e], p[2 * e + 1]);
+                lo[e] = T::pack(p[2 * e] - T::lo(hi[e]), p[2 * e + 1] - T::hi(hi[e]));
+            }
+            ph[rb] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            pl[rb] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+
+        // ---- O^T += V^T P ----------------------------------------------------------------------
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                uint32_t f[4];                                           // channel j: pairs of tokens
+#pragma unroll
+                for (int pr = 0; pr < 4; ++pr)
+                    f[pr] = __builtin_amdgcn_perm(vr[s][2 * pr + 1][j / 2], vr[s][2 * pr][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+                const uint4 vf = make_uint4(f[0], f[1], f[2], f[3]);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    O[rb][s][j] = T::mfma(vf, ph[rb], O[rb][s][j]);
+                    O[rb][s][j] = T::mfma(vf, pl[rb], O[rb][s][j]);
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(nx, par ^ 1);
+        x = nx; nx = nnx;
+        par ^= 1;
+    }
+
+    // ---- the wavefronts' results meet ------------------------------------------------------
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        l[rb] += __shfl_xor(l[rb], 16, 64);
+        l[rb] += __shfl_xor(l[rb], 32, 64);
+        if (kb == 0) { ms[wave][rb * 16 + c] = m[rb]; ls[wave][rb * 16 + c] = l[rb]; }
+    }
+    __syncthreads();
+    const int row = tid >> 4, oc = tid & 15;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        float mm = ms[0][rb * 16 + c];
+#pragma unroll
+        for (int i = 1; i < kPgWaves; ++i) mm = fmaxf(mm, ms[i][rb * 16 + c]);
+        const float f = __builtin_amdgcn_exp2f(m[rb] - mm);
+        const int64_t r = (int64_t)rblk * kRows + rb * 16 + row;
+        float mt = ms[0][rb * 16 + row], lt = 0.0f;
+#pragma unroll
+        for (int i = 1; i < kPgWaves; ++i) mt = fmaxf(mt, ms[i][rb * 16 + row]);
+#pragma unroll
+        for (int i = 0; i < kPgWaves; ++i) lt += ls[i][rb * 16 + row] * __builtin_amdgcn_exp2f(ms[i][rb * 16 + row] - mt);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            if (rb + s > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < CH; j += 4)
+                    *reinterpret_cast<float4 *>(&meet[wave][c][CH * (4 * kb + i) + j]) =
+                        make_float4(O[rb][s][j][i] * f, O[rb][s][j + 1][i] * f, O[rb][s][j + 2][i] * f, O[rb][s][j + 3][i] * f);
+            __syncthreads();
+            float o[CH];
+#pragma unroll
+            for (int e = 0; e < CH; ++e) o[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kPgWaves; ++i)
+#pragma unroll
+                for (int e = 0; e < CH; ++e) o[e] += meet[i][row][CH * oc + e];
+            const int ch = CH * (16 * s + oc);
+            if (ch >= D) continue;
+            if (a.slots) {
+                float *st = a.state + ((int64_t)unit * a.slots + slot) * part_floats(kRows, D), *op = st + (rb * 16 + row) * D + ch;
+#pragma unroll
+                for (int e = 0; e < CH; e += 4) *reinterpret_cast<float4 *>(op + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                if (ch == 0) { st[kRows * D + rb * 16 + row] = mt; st[kRows * (D + 1) + rb * 16 + row] = lt; }
+            } else if (r < rows) store_part<T, CH>(a, b, h, r, sq.live, ch, o, mt, lt);
+        }
+    }
+}
+
+// Joins a query row's parts: a workgroup to a row, D / 4 lanes (four channels each) to a part, as many parts at a time as fit.
+template <class T, int D>
+__global__ __launch_bounds__(256)
+void join_pages_kernel(PageAttnArgs a, int block_rows) {
+    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+    __shared__ __attribute__((aligned(16))) float sums[kGroups][D];
+    __shared__ float weights[kGroups];
+    const int64_t rows = (int64_t)a.t.group * a.t.n_new;
+    const int64_t bh = (int64_t)(blockIdx.x / (unsigned)rows), r = (int64_t)blockIdx.x - bh * rows;
+    const int b = (int)(bh / a.c.n_heads), h = (int)(bh - (int64_t)b * a.c.n_heads);
+    const int row = (int)(r % block_rows), grp = (int)threadIdx.x / kLanes, c4 = (int)threadIdx.x - grp * kLanes;
+    const int64_t step = part_floats(block_rows, D);
+    const int2 place = a.places[b];                                      // first slot, parts
+    const float *st = a.state + (((int64_t)h * a.row_blocks + r / block_rows) * a.slots + place.x) * step;
+    const float *mp = st + block_rows * D + row, *lp = mp + block_rows, *op = st + row * D + c4 * 4;
+    float m = kPgNoScore, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    // every lane finds the maximum over all parts: lane i of 64 looks at parts i, i + 64, ..
+    for (int p = threadIdx.x & 63; p < place.y; p += 64) m = fmaxf(m, mp[p * step]);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    if (grp < kGroups) {
+#pragma unroll 4
+        for (int p = grp; p < place.y; p += kGroups) {
+            const float f = __builtin_amdgcn_exp2f(mp[p * step] - m);
+            const float4 x = *reinterpret_cast<const float4 *>(op + p * step);
+            l += lp[p * step] * f;
+            o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+        }
+        *reinterpret_cast<float4 *>(&sums[grp][c4 * 4]) = o;
+        if (c4 == 0) weights[grp] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x >= D / 4) return;
+    l = 0.0f;
+    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const float4 x = *reinterpret_cast<const float4 *>(&sums[g][threadIdx.x * 4]);
+        l += weights[g];
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+    }
+    const float v[4] = {o.x, o.y, o.z, o.w};
+    store_part<T, 4>(a, b, h, r, a.t.n_live ? max(0, min(a.t.n_live[b], a.t.n_new)) : a.t.n_new, (int)threadIdx.x * 4, v, m, l);
+}
+
+bool page_attn_dim(int d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
+
+PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
+    PagePlan p{16, 1, 0, 0, 0};
+    // Tiles end where pages do, so that a tile's page is uniform, unless that would leave many of them short.
+    p.paged = c.page_len % kPgTile == 0 || c.page_len >= 8 * kPgTile;
+    const int64_t rows = (int64_t)t.group * t.n_new;
+    p.rows = rows <= 16 ? 16 : 32;
+    p.row_blocks = (int)((rows + p.rows - 1) / p.rows);
+    const int64_t units = (int64_t)c.n_heads * p.row_blocks;             // of a sequence
+    if (c.n_seqs < 1 || c.n_seqs > 256 || rows < 1) return p;
+    const int64_t tiles = p.paged ? (int64_t)c.table_pages * page_tiles((int)c.page_len) : page_tiles((int)(c.table_pages * c.page_len));
+    int64_t slots = 512 / units;
+    const int64_t most = c.n_seqs * (tiles / kPgLeast);
+    if (slots > most) slots = most;
+    if (slots >= 2 * (int64_t)c.n_seqs) {
+        p.slots = (int)slots;
+        p.state_bytes = (size_t)(units * slots * part_floats(p.rows, c.head_dim)) * sizeof(float) + (size_t)c.n_seqs * sizeof(int2);
+    }
+    return p;
+}
+
+template <class T, int D>
+static void launch_dim(const PageAttnArgs &a, int blocks, hipStream_t s) {
+    const int per_xcd = (blocks + 7) / 8;
+    const dim3 grid((unsigned)(per_xcd * 8)), threads(kPgThreads);
+    if (a.rows == 16) {
+        if (a.paged) attn_pages_kernel<T, D, 1, true><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
+        else attn_pages_kernel<T, D, 1, false><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
+    } else {
+        if (a.paged) attn_pages_kernel<T, D, 2, true><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
+        else attn_pages_kernel<T, D, 2, false><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
+    }
+    if (a.slots) {
+        const int64_t n = (int64_t)a.c.n_seqs * a.c.n_heads * a.t.group * a.t.n_new;
+        join_pages_kernel<T, D><<<dim3((unsigned)n), dim3(256), 0, s>>>(a, a.rows);
+    }
+}
+template <class T>
+static void launch_type(const PageAttnArgs &a, int blocks, hipStream_t s) {
+    switch (a.c.head_dim) {
+        case 64: launch_dim<T, 64>(a, blocks, s); break;
+        case 96: launch_dim<T, 96>(a, blocks, s); break;
+        case 128: launch_dim<T, 128>(a, blocks, s); break;
+        case 192: launch_dim<T, 192>(a, blocks, s); break;
+        default: launch_dim<T, 256>(a, blocks, s); break;
+    }
+}
+hipError_t launch_attn_pages(const PageAttnArgs &a, hipStream_t s) {
+    const int blocks = (int)((int64_t)(a.slots ? a.slots : a.c.n_seqs) * a.c.n_heads * a.row_blocks);
+    if (a.c.type == QVG_BF16) launch_type<PgBf16>(a, blocks, s);
+    else launch_type<PgF16>(a, blocks, s);
+    return hipGetLastError();
+}
+
+}  // namespace qvg

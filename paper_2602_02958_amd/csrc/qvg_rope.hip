@@ -1,0 +1,313 @@
+// Rotary positions: tables of (cos, sin), rows turned by them, and the new tokens' way into a cache of 16-bit pages, their keys turned
+// on the way.
+#include "qvg_rows.hpp"
+
+namespace qvg {
+
+// ---- tables -------------------------------------------------------------------------------------------------
+// A pair to a thread.  The angle is taken in turns: place x frequency / 2 pi in 64 bits, less its nearest whole number, leaves at most half a
+// turn, which 32 bits hold to 2^-26 of a turn (2^-23 rad, a quarter of binary16's step at 1 and of the size of a rounding of the
+// 32-bit result); its sine and cosine are then 32-bit functions.
+template <typename TAB>
+__global__ __launch_bounds__(256)
+void rope_table_kernel(RopeTableArgs a, FastDiv by_pairs, int rows_per_block) {
+    const int sub = (int)quotient(threadIdx.x, by_pairs), p = (int)threadIdx.x - sub * a.n_pairs;
+    if (sub >= rows_per_block) return;
+    const double turns = a.freq[p] * 0.15915494309189535;
+    // (where the arguments lie: as a value, indexed at run time, every thread would keep the axes in scratch memory)
+    const int ax = ((const RopeTableArgs *)__builtin_amdgcn_kernarg_segment_ptr())->axis[p];
+    for (int64_t i = (int64_t)blockIdx.x * rows_per_block + sub; i < a.n_rows; i += (int64_t)gridDim.x * rows_per_block) {
+        const int64_t at = a.positions ? a.positions[i * a.n_axes + ax] : a.first + i;
+        const double x = (double)at * turns;
+        const float f = 2.0f * (float)(x - __builtin_rint(x));
+        float s, c;
+        sincospif(f, &s, &c);
+        s *= a.amplitude; c *= a.amplitude;
+        const int64_t to = i * a.n_pairs + p;
+        if constexpr (sizeof(TAB) == 4) reinterpret_cast<float2 *>(a.out)[to] = make_float2(c, s);
+        else reinterpret_cast<uint32_t *>(a.out)[to] = pack_f16x2_rne(c, s);
+    }
+}
+hipError_t launch_rope_table(const RopeTableArgs &a, bool f32, hipStream_t s) {
+    const int per = 256 / a.n_pairs;
+    int64_t blocks = (a.n_rows + per - 1) / per;
+    if (blocks > 8192) blocks = 8192;
+    const FastDiv by = fast_div((uint32_t)a.n_pairs);
+    if (f32) rope_table_kernel<float><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
+    else rope_table_kernel<f16_t><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
+    return hipGetLastError();
+}
+
+// ---- rows -----------------------------------------------------------------------------------------------------
+struct Bf16 { typedef bf16_t raw; };
+struct F16 { typedef f16_t raw; };
+struct F32 { typedef float raw; };
+template <class T> struct Octet { uint4 w[sizeof(typename T::raw) / 2]; };      // eight elements as stored
+
+template <class T>
+__device__ __forceinline__ Octet<T> load_octet(const typename T::raw *p) {
+    Octet<T> o;
+#pragma unroll
+    for (size_t i = 0; i < sizeof(o.w) / 16; ++i) o.w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    return o;
+}
+template <class T>
+__device__ __forceinline__ void store_octet(typename T::raw *p, const Octet<T> &o) {
+#pragma unroll
+    for (size_t i = 0; i < sizeof(o.w) / 16; ++i) reinterpret_cast<uint4 *>(p)[i] = o.w[i];
+}
+__device__ __forceinline__ void octet_values(const Octet<Bf16> &o, float *v) { unpack_bf16x8(o.w[0], v); }
+__device__ __forceinline__ void octet_values(const Octet<F16> &o, float *v) {
+    const uint32_t w[4] = {o.w[0].x, o.w[0].y, o.w[0].z, o.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = f16_bits_to_f32(w[i] & 0xffffu); v[2 * i + 1] = f16_bits_to_f32(w[i] >> 16); }
+}
+__device__ __forceinline__ void octet_values(const Octet<F32> &o, float *v) { __builtin_memcpy(v, o.w, 32); }
+__device__ __forceinline__ void octet_of(const float *v, Octet<Bf16> &o) { o.w[0] = pack_bf16x8(v); }
+__device__ __forceinline__ void octet_of(const float *v, Octet<F16> &o) {
+    o.w[0] = make_uint4(pack_f16x2_rne(v[0], v[1]), pack_f16x2_rne(v[2], v[3]), pack_f16x2_rne(v[4], v[5]), pack_f16x2_rne(v[6], v[7]));
+}
+__device__ __forceinline__ void octet_of(const float *v, Octet<F32> &o) { __builtin_memcpy(o.w, v, 32); }
+__device__ __forceinline__ float value_of(bf16_t x, Bf16) { return bf16_lo(x); }
+__device__ __forceinline__ float value_of(f16_t x, F16) { return f16_bits_to_f32(x); }
+__device__ __forceinline__ float value_of(float x, F32) { return x; }
+__device__ __forceinline__ bf16_t raw_of(float x, Bf16) { return (bf16_t)pack_bf16x2(x, 0.0f); }
+__device__ __forceinline__ f16_t raw_of(float x, F16) { return (f16_t)f32_to_f16_bits(x); }
+__device__ __forceinline__ float raw_of(float x, F32) { return x; }
+
+__device__ __forceinline__ void turn(float &x0, float &x1, float2 cs) {
+    const float t0 = x1 * cs.y, t1 = x1 * cs.x, y0 = __builtin_fmaf(x0, cs.x, -t0);
+    x1 = __builtin_fmaf(x0, cs.y, t1);
+    x0 = y0;
+}
+template <typename TAB>
+__device__ __forceinline__ float2 table_pair(const TAB *row, int p) {
+    if constexpr (sizeof(TAB) == 4) return reinterpret_cast<const float2 *>(row)[p];
+    else {
+        const uint32_t w = reinterpret_cast<const uint32_t *>(row)[p];
+        return make_float2(f16_bits_to_f32(w & 0xffffu), f16_bits_to_f32(w >> 16));
+    }
+}
+// Pairs p0 .. p0 + N - 1 (N a multiple of 4) of a row; `whole`: rows are 16-byte aligned and have all of them
+template <typename TAB, int N>
+__device__ __forceinline__ void table_pairs(const TAB *row, int p0, int n_pairs, bool whole, float2 *cs) {
+    if (whole) {
+        constexpr int kWords = N * (int)sizeof(TAB) / 8;
+        uint4 w[kWords];
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4 *>(row + 2 * p0)[i];
+        if constexpr (sizeof(TAB) == 4) __builtin_memcpy(cs, w, sizeof(w));
+        else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t x = (&w[i / 4].x)[i % 4];
+                cs[i] = make_float2(f16_bits_to_f32(x & 0xffffu), f16_bits_to_f32(x >> 16));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) cs[i] = p0 + i < n_pairs ? table_pair(row, p0 + i) : make_float2(1.0f, 0.0f);
+    }
+}
+
+// What is done with a row: pairs (2p, 2p + 1), an octet of channels to a thread; pairs (p, p + n), eight of them (two octets) to a
+// thread, or one where they do not start at multiples of eight; nothing.  Channels behind the pairs are copied.
+enum { kTurnNext, kTurnHalf, kTurnPair, kTurnNone };
+constexpr int kTurnHeads = 4;      // heads that a thread takes at once, where there are many rows: they share the table's row
+
+// A thread takes a piece of a token's rows in `HP` heads: it reads the table's row once for all of them, and all rows before it
+// writes any.  Memory bounds it: the rows both ways.
+template <class T, typename TAB, int MODE, bool APPEND, int HP>
+__global__ __launch_bounds__(256)
+void turn_kernel(TurnArgs a, int per_block, int whole) {
+    typedef typename T::raw raw;
+    const int sub = per_block == 1 ? 0 : (int)quotient(threadIdx.x, a.by_units);
+    const int64_t t = (a.first_block + blockIdx.x) * per_block + sub;
+    if (sub >= per_block || t >= a.tokens) return;
+    int u = (int)threadIdx.x - sub * a.units;
+    const int b = (int)quotient((uint32_t)t, a.by_tokens), i = (int)t - b * a.n_tokens;
+    const raw *src = static_cast<const raw *>(a.x) + b * a.x_seq + i * a.x_tok, *vsrc = nullptr;
+    raw *dst, *vdst = nullptr;
+    int64_t dst_head;
+    int place;
+    if constexpr (APPEND) {
+        int len = a.kv_len[b], n = a.n_tokens;
+        len = len < 0 ? 0 : (len > a.capacity ? a.capacity : len);
+        if (a.live) { n = a.live[b]; n = n < 0 ? 0 : (n > a.n_tokens ? a.n_tokens : n); }
+        const int room = a.capacity - len;                               // (len + n may pass 31 bits)
+        // (where the new lengths have a place of their own; else they wait for the rows to be done with the old ones)
+        if (a.lengths_here && i == 0 && u == 0 && blockIdx.y == 0) a.len_out[b] = len + (n < room ? n : room);
+        if (i >= n || i >= room) return;
+        place = len + i;
+        const int pi = (int)quotient((uint32_t)place, a.by_page);
+        const uint32_t pg = (uint32_t)a.table[(int64_t)b * a.table_pages + pi];
+        if (pg >= a.pool_pages) return;
+        const int64_t to = (int64_t)pg * a.page + (int64_t)(place - pi * (int)a.by_page.d) * a.tok;
+        dst = static_cast<raw *>(a.k_pages) + to; vdst = static_cast<raw *>(a.v_pages) + to;
+        vsrc = static_cast<const raw *>(a.v) + b * a.x_seq + i * a.x_tok;
+        dst_head = a.head;
+    } else {
+        dst = static_cast<raw *>(a.out) + b * a.o_seq + i * a.o_tok;
+        dst_head = a.o_head;
+        place = 0;
+    }
+    const TAB *row = nullptr;
+    if constexpr (MODE != kTurnNone) {
+        int64_t at = a.r.positions ? a.r.positions[t] : APPEND ? place : (a.first ? (int64_t)a.first[b] : 0) + i;
+        at = at < 0 ? 0 : (at >= a.r.n_rows ? a.r.n_rows - 1 : at);
+        row = static_cast<const TAB *>(a.r.table) + at * (2 * a.r.n_pairs);
+    }
+    const int P = a.r.n_pairs, heads = (int)gridDim.y;
+    const float sign = a.backward ? -1.0f : 1.0f;
+
+    if constexpr (MODE == kTurnPair) {
+        for (; u < a.units; u += 256) {                                  // (one piece, but of rows of more than 256)
+            const bool pair = u < P;
+            const int c0 = pair ? u : u + P;
+            float2 cs = make_float2(1.0f, 0.0f);
+            if (pair) { cs = table_pair(row, u); cs.y *= sign; }
+            for (int h = blockIdx.y; h < a.H; h += heads) {
+                const raw *x = src + h * a.x_head;
+                raw *y = dst + h * dst_head;
+                if (pair) {
+                    float x0 = value_of(x[c0], T{}), x1 = value_of(x[c0 + P], T{});
+                    turn(x0, x1, cs);
+                    y[c0] = raw_of(x0, T{}); y[c0 + P] = raw_of(x1, T{});
+                } else y[c0] = x[c0];
+                if constexpr (APPEND) {
+                    const raw *vx = vsrc + h * a.x_head;
+                    raw *vy = vdst + h * dst_head;
+                    vy[c0] = vx[c0];
+                    if (pair) vy[c0 + P] = vx[c0 + P];
+                }
+            }
+        }
+        return;
+    }
+
+    constexpr int kOct = MODE == kTurnHalf ? 2 : 1;                      // octets of a piece
+    int c[2];                                                            // their first channels
+    bool turned;
+    if constexpr (MODE == kTurnHalf) {
+        turned = u * 8 < P;
+        c[0] = turned ? u * 8 : P + u * 8; c[1] = c[0] + (turned ? P : 0);    // (pieces behind the pairs have one octet)
+    } else {
+        c[0] = c[1] = u * 8;
+        turned = MODE == kTurnNext && u * 4 < P;
+    }
+    float2 cs[4 * kOct];
+    if (MODE != kTurnNone && turned) {
+        table_pairs<TAB, 4 * kOct>(row, MODE == kTurnHalf ? u * 8 : u * 4, P, whole && (MODE == kTurnHalf || u * 4 + 4 <= P), cs);
+#pragma unroll
+        for (int p = 0; p < 4 * kOct; ++p) cs[p].y *= sign;
+    }
+    for (int h0 = blockIdx.y; h0 < a.H; h0 += heads * HP) {
+        Octet<T> x[HP][kOct], v[HP][APPEND ? kOct : 1];
+#pragma unroll
+        for (int k = 0; k < HP; ++k) {
+            const int h = h0 + k * heads;
+            if (h < a.H) {
+#pragma unroll
+                for (int o = 0; o < kOct; ++o)
+                    if (o == 0 || turned) {
+                        x[k][o] = load_octet<T>(src + h * a.x_head + c[o]);
+                        if constexpr (APPEND) v[k][o] = load_octet<T>(vsrc + h * a.x_head + c[o]);
+                    }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < HP; ++k) {
+            const int h = h0 + k * heads;
+            if (h < a.H) {
+                if (MODE != kTurnNone && turned) {
+                    float f[kOct][8];
+#pragma unroll
+                    for (int o = 0; o < kOct; ++o) octet_values(x[k][o], f[o]);
+                    if constexpr (MODE == kTurnHalf) {
+#pragma unroll
+                        for (int p = 0; p < 8; ++p) turn(f[0][p], f[1][p], cs[p]);
+                    } else {
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+                            if (u * 4 + p < P) turn(f[0][2 * p], f[0][2 * p + 1], cs[p]);
+                    }
+#pragma unroll
+                    for (int o = 0; o < kOct; ++o) octet_of(f[o], x[k][o]);
+                }
+#pragma unroll
+                for (int o = 0; o < kOct; ++o)
+                    if (o == 0 || turned) {
+                        store_octet<T>(dst + h * dst_head + c[o], x[k][o]);
+                        if constexpr (APPEND) store_octet<T>(vdst + h * dst_head + c[o], v[k][o]);
+                    }
+            }
+        }
+    }
+}
+// (in a launch of its own, behind the rows, when len_out may be kv_len)
+__global__ __launch_bounds__(256)
+void append_lengths_kernel(TurnArgs a, int n_seqs) {
+    const int b = blockIdx.x * 256 + threadIdx.x;
+    if (b >= n_seqs) return;
+    int len = a.kv_len[b], n = a.n_tokens;
+    len = len < 0 ? 0 : (len > a.capacity ? a.capacity : len);
+    if (a.live) { n = a.live[b]; n = n < 0 ? 0 : (n > a.n_tokens ? a.n_tokens : n); }
+    a.len_out[b] = len + (n < a.capacity - len ? n : a.capacity - len);
+}
+
+template <class T, typename TAB, int MODE, bool APPEND>
+static void launch_turn(TurnArgs &a, hipStream_t s) {
+    const int per = a.units < 256 ? 256 / a.units : 1;
+    const int64_t blocks = (a.tokens + per - 1) / per;
+    const int heads = (a.H + kTurnHeads - 1) / kTurnHeads;
+    const int whole = MODE != kTurnNone && a.r.n_pairs % 4 == 0 && (reinterpret_cast<uintptr_t>(a.r.table) & 15u) == 0;
+    a.by_units = fast_div((uint32_t)a.units);
+    a.by_tokens = fast_div((uint32_t)a.n_tokens);
+    const bool many = MODE != kTurnPair && blocks * a.H > 4 * 2048;
+    constexpr int64_t kMost = 1 << 23;                                   // (a launch has fewer than 2^32 threads along an axis)
+    for (a.first_block = 0; a.first_block < blocks; a.first_block += kMost) {
+        const unsigned n = (unsigned)(blocks - a.first_block < kMost ? blocks - a.first_block : kMost);
+        if constexpr (MODE != kTurnPair)
+            if (many) {
+                turn_kernel<T, TAB, MODE, APPEND, kTurnHeads><<<dim3(n, (unsigned)heads), dim3(256), 0, s>>>(a, per, whole);
+                continue;
+            }
+        turn_kernel<T, TAB, MODE, APPEND, 1><<<dim3(n, (unsigned)a.H), dim3(256), 0, s>>>(a, per, whole);
+    }
+}
+template <class T, bool APPEND>
+static void launch_typed(TurnArgs &a, bool turned_only, hipStream_t s) {
+    const int P = a.r.table ? a.r.n_pairs : 0;
+    const bool f32 = a.r.type == QVG_F32;
+    if (P == 0) {
+        a.units = a.d / 8;
+        if constexpr (APPEND) launch_turn<T, f16_t, kTurnNone, APPEND>(a, s);
+    } else if (!a.r.half) {
+        a.units = turned_only ? (P + 3) / 4 : a.d / 8;
+        f32 ? launch_turn<T, float, kTurnNext, APPEND>(a, s) : launch_turn<T, f16_t, kTurnNext, APPEND>(a, s);
+    } else if (P % 8 == 0) {
+        a.units = turned_only ? P / 8 : P / 8 + (a.d - 2 * P) / 8;
+        f32 ? launch_turn<T, float, kTurnHalf, APPEND>(a, s) : launch_turn<T, f16_t, kTurnHalf, APPEND>(a, s);
+    } else {
+        a.units = turned_only ? P : a.d - P;
+        f32 ? launch_turn<T, float, kTurnPair, APPEND>(a, s) : launch_turn<T, f16_t, kTurnPair, APPEND>(a, s);
+    }
+}
+hipError_t launch_rope(TurnArgs &a, int type, hipStream_t s) {
+    const bool turned_only = a.out == a.x;                               // (with x's strides: the other channels are there)
+    if (type == QVG_BF16) launch_typed<Bf16, false>(a, turned_only, s);
+    else if (type == QVG_F16) launch_typed<F16, false>(a, turned_only, s);
+    else launch_typed<F32, false>(a, turned_only, s);
+    return hipGetLastError();
+}
+// (both types are 16 bits: rows that are not turned are copied as either)
+hipError_t launch_append(TurnArgs &a, int n_seqs, int type, hipStream_t s) {
+    if (a.tokens > 0) {
+        if (type == QVG_BF16 || !a.r.table) launch_typed<Bf16, true>(a, false, s);
+        else launch_typed<F16, true>(a, false, s);
+    }
+    if (a.len_out && !a.lengths_here) append_lengths_kernel<<<dim3((unsigned)((n_seqs + 255) / 256)), dim3(256), 0, s>>>(a, n_seqs);
+    return hipGetLastError();
+}
+
+}  // namespace qvg
