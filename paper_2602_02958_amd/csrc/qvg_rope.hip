@@ -2,39 +2,75 @@
 // on the way.
 #include "qvg_rows.hpp"
 
+#include <type_traits>
+
 namespace qvg {
 
 // ---- tables -------------------------------------------------------------------------------------------------
-// A pair to a thread.  The angle is taken in turns: place x frequency / 2 pi in 64 bits, less its nearest whole number, leaves at most half a
-// turn, which 32 bits hold to 2^-26 of a turn (2^-23 rad, a quarter of binary16's step at 1 and of the size of a rounding of the
-// 32-bit result); its sine and cosine are then 32-bit functions.
-template <typename TAB>
+// A pair to a thread.  The angle is taken in quarter turns: place x frequency x 4 / 2 pi in 64 bits, less its nearest whole number (adding
+// 1.5 x 2^52 rounds to it, and leaves it in the sum's low bits), is half a quarter or less, which 32 bits hold to 2^-27 of a
+// turn.  Sine and cosine of that are Taylor's polynomials in 32 bits (their next terms are below 2^-29 at pi / 4), and the quarter says which
+// is which and its sign.
+__device__ __forceinline__ float2 cos_sin_of(double place, double quarters) {
+    const double x = place * quarters, sum = x + 6755399441055744.0;
+    const float r = (float)(x - (sum - 6755399441055744.0));
+    const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, sum);
+    const float z = __builtin_amdgcn_fmed3f(r, -0.5f, 0.5f) * 1.57079637f, w = z * z;
+    auto fma = [](float x, float y, float t) { return __builtin_fmaf(x, y, t); };
+    const float s = fma(z * w, fma(w, fma(w, fma(w, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), z);
+    const float c = fma(w, fma(w, fma(w, fma(w, fma(w, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
+    const uint32_t cb = __float_as_uint(k & 1u ? s : c) ^ ((k + 1u & 2u) << 30), sb = __float_as_uint(k & 1u ? c : s) ^ ((k & 2u) << 30);
+    return make_float2(__uint_as_float(cb), __uint_as_float(sb));
+}
+template <typename TAB, int ROWS, bool GIVEN>
 __global__ __launch_bounds__(256)
 void rope_table_kernel(RopeTableArgs a, FastDiv by_pairs, int rows_per_block) {
+    typedef uint32_t two __attribute__((ext_vector_type(2)));
+    typedef typename std::conditional<sizeof(TAB) == 4, two, uint32_t>::type pair;
     const int sub = (int)quotient(threadIdx.x, by_pairs), p = (int)threadIdx.x - sub * a.n_pairs;
-    if (sub >= rows_per_block) return;
-    const double turns = a.freq[p] * 0.15915494309189535;
-    // (where the arguments lie: as a value, indexed at run time, every thread would keep the axes in scratch memory)
-    const int ax = ((const RopeTableArgs *)__builtin_amdgcn_kernarg_segment_ptr())->axis[p];
-    for (int64_t i = (int64_t)blockIdx.x * rows_per_block + sub; i < a.n_rows; i += (int64_t)gridDim.x * rows_per_block) {
-        const int64_t at = a.positions ? a.positions[i * a.n_axes + ax] : a.first + i;
-        const double x = (double)at * turns;
-        const float f = 2.0f * (float)(x - __builtin_rint(x));
-        float s, c;
-        sincospif(f, &s, &c);
-        s *= a.amplitude; c *= a.amplitude;
-        const int64_t to = i * a.n_pairs + p;
-        if constexpr (sizeof(TAB) == 4) reinterpret_cast<float2 *>(a.out)[to] = make_float2(c, s);
-        else reinterpret_cast<uint32_t *>(a.out)[to] = pack_f16x2_rne(c, s);
+    const int64_t i0 = (int64_t)blockIdx.x * (rows_per_block * ROWS) + sub, left = a.n_rows - i0;
+    if (sub >= rows_per_block || left <= 0) return;
+    const double quarters = a.freq[p] * 0.6366197723675814;
+    // (rows, and pairs, are a fixed way apart: addresses are sums)
+    const int rows = (int)(left < ROWS * 256 ? left : ROWS * 256);       // (of which every rows_per_block-th is this thread's)
+    int at[ROWS];
+    if constexpr (GIVEN) {
+        // (where the arguments lie: as a value, indexed at run time, every thread would keep the axes in scratch memory)
+        const int ax = ((const RopeTableArgs *)__builtin_amdgcn_kernarg_segment_ptr())->axis[p];
+        const int32_t *from = a.positions + (i0 * a.n_axes + ax);
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) at[j] = from[(uint32_t)(min(j * rows_per_block, rows - 1) * a.n_axes)];
+    } else {
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) at[j] = (int)(a.first + i0) + j * rows_per_block;
+    }
+    pair *to = reinterpret_cast<pair *>(a.out) + (i0 * a.n_pairs + p);
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        if (j * rows_per_block >= rows) return;
+        float2 cs = cos_sin_of((double)at[j], quarters);
+        cs.x *= a.amplitude; cs.y *= a.amplitude;
+        pair v;
+        if constexpr (sizeof(TAB) == 4) v = two{__float_as_uint(cs.x), __float_as_uint(cs.y)};
+        else v = pack_f16x2_rne(cs.x, cs.y);
+        pair *row = to + (uint32_t)(j * rows_per_block * a.n_pairs);
+        // (a large table is read long after: past the caches it takes 66 us instead of 80, 383 MB)
+        if constexpr (ROWS > 1) __builtin_nontemporal_store(v, row);
+        else *row = v;
     }
 }
+template <typename TAB, int ROWS>
+static void launch_table(const RopeTableArgs &a, int64_t blocks, int per, hipStream_t s) {
+    const FastDiv by = fast_div((uint32_t)a.n_pairs);
+    if (a.positions) rope_table_kernel<TAB, ROWS, true><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
+    else rope_table_kernel<TAB, ROWS, false><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
+}
+constexpr int kTableRows = 16;     // of a thread, whose places it asks for together, where there are many
 hipError_t launch_rope_table(const RopeTableArgs &a, bool f32, hipStream_t s) {
     const int per = 256 / a.n_pairs;
-    int64_t blocks = (a.n_rows + per - 1) / per;
-    if (blocks > 8192) blocks = 8192;
-    const FastDiv by = fast_div((uint32_t)a.n_pairs);
-    if (f32) rope_table_kernel<float><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
-    else rope_table_kernel<f16_t><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
+    const int64_t blocks = (a.n_rows + per - 1) / per, fewer = (blocks + kTableRows - 1) / kTableRows;
+    if (blocks > 8192) f32 ? launch_table<float, kTableRows>(a, fewer, per, s) : launch_table<f16_t, kTableRows>(a, fewer, per, s);
+    else f32 ? launch_table<float, 1>(a, blocks, per, s) : launch_table<f16_t, 1>(a, blocks, per, s);
     return hipGetLastError();
 }
 
@@ -51,10 +87,15 @@ __device__ __forceinline__ Octet<T> load_octet(const typename T::raw *p) {
     for (size_t i = 0; i < sizeof(o.w) / 16; ++i) o.w[i] = reinterpret_cast<const uint4 *>(p)[i];
     return o;
 }
-template <class T>
+// FAR: nobody reads them soon
+template <class T, bool FAR>
 __device__ __forceinline__ void store_octet(typename T::raw *p, const Octet<T> &o) {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (size_t i = 0; i < sizeof(o.w) / 16; ++i) reinterpret_cast<uint4 *>(p)[i] = o.w[i];
+    for (size_t i = 0; i < sizeof(o.w) / 16; ++i) {
+        if constexpr (FAR) __builtin_nontemporal_store(__builtin_bit_cast(words, o.w[i]), reinterpret_cast<words *>(p) + i);
+        else reinterpret_cast<uint4 *>(p)[i] = o.w[i];
+    }
 }
 __device__ __forceinline__ void octet_values(const Octet<Bf16> &o, float *v) { unpack_bf16x8(o.w[0], v); }
 __device__ __forceinline__ void octet_values(const Octet<F16> &o, float *v) {
@@ -237,8 +278,8 @@ void turn_kernel(TurnArgs a, int per_block, int whole) {
 #pragma unroll
                 for (int o = 0; o < kOct; ++o)
                     if (o == 0 || turned) {
-                        store_octet<T>(dst + h * dst_head + c[o], x[k][o]);
-                        if constexpr (APPEND) store_octet<T>(vdst + h * dst_head + c[o], v[k][o]);
+                        store_octet<T, APPEND>(dst + h * dst_head + c[o], x[k][o]);
+                        if constexpr (APPEND) store_octet<T, APPEND>(vdst + h * dst_head + c[o], v[k][o]);
                     }
             }
         }
@@ -263,7 +304,7 @@ static void launch_turn(TurnArgs &a, hipStream_t s) {
     const int whole = MODE != kTurnNone && a.r.n_pairs % 4 == 0 && (reinterpret_cast<uintptr_t>(a.r.table) & 15u) == 0;
     a.by_units = fast_div((uint32_t)a.units);
     a.by_tokens = fast_div((uint32_t)a.n_tokens);
-    const bool many = MODE != kTurnPair && blocks * a.H > 4 * 2048;
+    const bool many = MODE != kTurnPair && blocks * a.H > 1024;
     constexpr int64_t kMost = 1 << 23;                                   // (a launch has fewer than 2^32 threads along an axis)
     for (a.first_block = 0; a.first_block < blocks; a.first_block += kMost) {
         const unsigned n = (unsigned)(blocks - a.first_block < kMost ? blocks - a.first_block : kMost);
