@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqvg.so")
 SOURCES = ["qvg_api.cpp", "qvg_decode.hip", "qvg_encode.hip", "qvg_lloyd.hip", "qvg_kmeans.hip", "qvg_quant.hip", "qvg_attn.hip", "qvg_attn_slab.hip",
            "qvg_tree.hip", "qvg_tree_packed.hip", "qvg_tree_wide.hip", "qvg_pages.hip", "qvg_rope.hip", "qvg_attn_pages.hip"]
-HEADERS = [os.path.join(CSRC, "qvg_internal.hpp"), os.path.join(CSRC, "qvg_attn_tiles.hpp"), os.path.join(CSRC, "qvg_tree.hpp"), os.path.join(CSRC, "qvg_rows.hpp"), os.path.join(CSRC, "qvg_tree_lane.hpp"), os.path.join(CSRC, "qvg_kmeans.hpp"), os.path.join(CSRC, "qvg_assign.hpp"),
+HEADERS = [os.path.join(CSRC, "qvg_internal.hpp"), os.path.join(CSRC, "qvg_attn_tiles.hpp"), os.path.join(CSRC, "qvg_tree.hpp"), os.path.join(CSRC, "qvg_rows.hpp"), os.path.join(CSRC, "qvg_attn_pages.hpp"), os.path.join(CSRC, "qvg_tree_lane.hpp"), os.path.join(CSRC, "qvg_kmeans.hpp"), os.path.join(CSRC, "qvg_assign.hpp"),
            os.path.join(ROOT, "include", "qvg.h")]
 
 FLAGS = [

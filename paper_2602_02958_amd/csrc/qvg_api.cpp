@@ -967,6 +967,7 @@ int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softma
     a.by_page = fast_div((uint32_t)c->page_len);
     a.by_tiles = fast_div((uint32_t)page_tiles((int)c->page_len));
     a.slots = scratch && scratch_bytes >= plan.state_bytes ? plan.slots : 0;
+    a.extra = plan.extra; a.kept = plan.kept;
     a.state = static_cast<float *>(scratch);
     if (a.slots) a.places = reinterpret_cast<int2 *>(static_cast<char *>(scratch) + plan.state_bytes - (size_t)c->n_seqs * sizeof(int2));
     return launch_attn_pages(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;

@@ -12,18 +12,19 @@
 //                  up with octets 4 kb + r of query row c.
 // The weights enter as two numbers of the cache's type, w = hi + lo: the matrix cores have nothing else to do, and one number's
 // rounding (2^-8 of a bf16 weight) would be as large as the output's own.
-// A tile's keys are asked for when the one before has been contracted, and so are its values: a wavefront has 16 KB (of 128
-// channels) on their way all the time.  Memory bounds it.
-#include "qvg_rows.hpp"
+// A tile's keys are asked for when one before has been contracted, and so are its values: a wavefront has 16 KB (of 128 channels)
+// on their way all the time; twice as much changes nothing (one head over 32000 tokens 41 us so and so).  Memory bounds it.
+#include "qvg_attn_pages.hpp"
 
 namespace qvg {
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
 
 constexpr int kPgThreads = 256, kPgWaves = kPgThreads / 64;
-constexpr float kPgNoScore = -3.402823466e38f;      // the running reference before any score
-// Weights are exp2(score - reference) x 2^kPgUp, and the reference moves when a score is kPgLag above it: they stay below 2^14, and
-// the small ones of a row keep their bits in binary16 for longer.
+constexpr float kPgNoScore = -3.402823466e38f;      // the running reference before any product
+// References are products q.k, before the scale: a weight is exp2((product - reference) x scale + kPgUp), whose difference is exact where it
+// matters, however large the products are.  A reference moves when a weight would pass 2^(kPgUp + kPgLag): they stay below 2^14,
+// and the small ones of a row keep their bits in binary16 for longer.
 constexpr float kPgUp = 7.0f, kPgLag = 7.0f;
 
 struct PgBf16 {
@@ -48,101 +49,83 @@ template <int D> struct PgDim {
     static constexpr int pitch = 16 * CH + 4;       // floats per row of a set where the wavefronts' results meet
 };
 
-// What a sequence's rows see, together: tokens 0 .. sink - 1 and lo .. kv - 1; and in tiles.
-struct Span { int kv, live, sink, lo, sink_tiles, main_tile, total; };
-__device__ __forceinline__ int tile_of(const PageAttnArgs &a, int n) {
-    if (!a.paged) return n / kPgTile;
-    const int pi = (int)quotient((uint32_t)n, a.by_page);
-    return pi * (int)a.by_tiles.d + (n - pi * (int)a.by_page.d) / kPgTile;
-}
-__device__ __forceinline__ Span span_of(const PageAttnArgs &a, int b) {
-    auto clamp = [](int v, int hi) { return v < 0 ? 0 : (v > hi ? hi : v); };
-    Span s;
-    s.kv = a.c.table_pages ? clamp(a.c.kv_len[b], (int)(a.c.table_pages * a.c.page_len)) : 0;
-    s.live = a.t.n_live ? clamp(a.t.n_live[b], a.t.n_new) : a.t.n_new;
-    s.sink = s.lo = s.sink_tiles = s.main_tile = s.total = 0;
-    if (s.live == 0) s.kv = 0;                                           // no row: nothing to read
-    if (s.kv == 0) return s;
-    const int place = s.kv - s.live;                                     // of the first row
-    if (a.t.window > 0 && place >= a.t.window) {
-        s.lo = place - a.t.window + 1;
-        s.sink = a.t.sink < s.lo ? a.t.sink : s.lo;
-        if (s.sink == s.lo) s.sink = s.lo = 0;                           // no gap
-    }
-    s.sink_tiles = s.sink ? tile_of(a, s.sink - 1) + 1 : 0;
-    const int from = tile_of(a, s.lo), end = tile_of(a, s.kv - 1) + 1;
-    s.main_tile = from > s.sink_tiles ? from : s.sink_tiles;
-    s.total = s.sink_tiles + (end > s.main_tile ? end - s.main_tile : 0);
-    return s;
+__device__ __forceinline__ PgLens lens_of(const PageAttnArgs &a, int b) {
+    return {a.c.table_pages ? a.c.kv_len[b] : 0, a.t.n_live ? a.t.n_live[b] : a.t.n_new};
 }
 
 // How the slots of a divided call (a.slots of them, the same for every head and row block) are dealt to the sequences: a slot for every q
-// tiles or part of them, and one at least, with the smallest q for which the slots suffice, or nearly: it lies between total / slots
-// and total / (slots - n), since the sum of ceil(T / q) over n sequences is at most total / q + n, and is found in five halvings.
+// tiles or part of them, and one at least.  With n sequences and a.extra = slots - n the sum of ceil(T / q) is at most total / q + n, so that
+// q = total / extra suffices.  Where there are few sequences it is the smallest that does, or nearly: it lies between total / slots and
+// that, and is found in five halvings.  Where there are many it stays: the usual ones are taken whole, and those of more than q
+// tiles, fewer than `extra`, have 2 extra parts at most, which are all that leave partial results.
 // Every wavefront works that out for itself from the lengths, which only the device knows (n <= 256: a call of more sequences
 // is not divided).  Slots that are left over have nothing to do.
-struct Slot { int b, part, parts, first; };                              // first: the sequence's first slot; parts: 0, none
+struct Slot { int b, part, parts, first; PgLens n; };                    // first: of the sequence's partial results; part >= parts: none
 __device__ __forceinline__ int parts_of(int total, int q) {
     const int p = (int)(((uint32_t)total + (uint32_t)q - 1u) / (uint32_t)q);
     return p < 1 ? 1 : p;
 }
-template <typename N>
-__device__ __forceinline__ N lanes_sum(N x) {
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) x += __shfl_xor(x, off, 64);
+// Sums of lanes 0 .. i, and of all, between lanes of a row and then rows (no LDS, which five halvings of six exchanges would wait for)
+__device__ __forceinline__ int lanes_upto(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
-constexpr int kPgLeast = 2 * kPgWaves;              // tiles of a part: two to a wavefront
+__device__ __forceinline__ int lanes_sum(int x) { return __builtin_amdgcn_readlane(lanes_upto(x), 63); }
 __device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot) {
     const int lane = threadIdx.x & 63, n = a.c.n_seqs;
+    Slot p{0, 0, 0, 0, {0, 0}};
+    if (n == 1) {
+        p.n = lens_of(a, 0);
+        const int total = pg_span_of(a, p.n).total, q = max((total + a.slots - 1) / a.slots, kPgWaves);
+        p.parts = parts_of(total, q);
+        p.part = slot;
+        return p;
+    }
     int tiles[4];                                                        // of sequences lane, 64 + lane, ..
+    PgLens lens[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        tiles[k] = 0;
-        if (64 * k < n && 64 * k + lane < n) tiles[k] = span_of(a, 64 * k + lane).total;
+        lens[k] = PgLens{0, 0};
+        if (64 * k < n) lens[k] = lens_of(a, min(64 * k + lane, n - 1));
+        tiles[k] = 64 * k + lane < n ? pg_span_of(a, lens[k]).total : 0;
     }
-    int q;
-    if (n == 1) q = (__builtin_amdgcn_readfirstlane(tiles[0]) + a.slots - 1) / a.slots;
-    else {
-        const int64_t total = lanes_sum((int64_t)tiles[0] + tiles[1] + tiles[2] + tiles[3]);
-        int lo = (int)((total + a.slots - 1) / a.slots);
-        q = (int)((total + a.slots - n - 1) / (a.slots - n));
-        for (int i = 0; i < 5 && lo < q; ++i) {                          // uniform
-            const int mid = lo + (q - lo) / 2;
-            int need = 0;
-            if (mid > 0)
+    int few = 0, many = 0;                                               // the total's two halves: it may pass 31 bits
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (64 * k < n) need += 64 * k + lane < n ? parts_of(tiles[k], mid) : 0;
-            if (mid > 0 && lanes_sum(need) <= a.slots) q = mid; else lo = mid + 1;
-        }
+    for (int k = 0; k < 4; ++k) { few += tiles[k] & 0xffff; many += tiles[k] >> 16; }
+    const int64_t total = lanes_sum(few) + ((int64_t)lanes_sum(many) << 16);
+    // (2^26: more tiles than a sequence has)
+    int q = max((int)min((total + a.extra - 1) / a.extra, (int64_t)1 << 26), kPgWaves), lo = n <= a.extra ? max((int)((total + a.slots - 1) / a.slots), kPgWaves) : q;
+    for (int i = 0; i < 5 && lo < q; ++i) {                              // uniform
+        const int mid = lo + (q - lo) / 2;
+        int need = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (64 * k < n) need += 64 * k + lane < n ? parts_of(tiles[k], mid) : 0;
+        if (lanes_sum(need) <= a.slots) q = mid; else lo = mid + 1;
     }
-    if (q < kPgLeast) q = kPgLeast;
-    Slot p{0, 0, 0, 0};
-    int before = 0;
+    int before = 0, divided = 0;                                         // slots, and partial results, of the sequences before
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const int base = 64 * k, i = base + lane;
-        if (base >= n) break;                                            // uniform
-        const int mine = i < n ? parts_of(tiles[k], q) : 0;
-        int upto = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off *= 2) {
-            const int x = __shfl_up(upto, off, 64);
-            if (lane >= off) upto += x;
-        }
-        upto += before;
-        const unsigned long long hit = __ballot(mine > 0 && slot >= upto - mine && slot < upto);
+        if (64 * k >= n) break;                                          // uniform
+        const int mine = 64 * k + lane < n ? parts_of(tiles[k], q) : 0, kept = mine > 1 ? mine : 0;
+        const int upto = before + lanes_upto(mine), kept_upto = divided + lanes_upto(kept);
+        const unsigned long long hit = __ballot(slot >= upto - mine && slot < upto);
         if (hit) {
             const int at = __builtin_ctzll(hit);
-            p.b = base + at; p.parts = __shfl(mine, at, 64); p.first = __shfl(upto, at, 64) - p.parts;
-            p.part = slot - p.first;
+            p.b = 64 * k + at; p.parts = __builtin_amdgcn_readlane(mine, at);
+            p.part = slot - (__builtin_amdgcn_readlane(upto, at) - p.parts);
+            p.first = __builtin_amdgcn_readlane(kept_upto - kept, at);
+            p.n = PgLens{__builtin_amdgcn_readlane(lens[k].kv, at), __builtin_amdgcn_readlane(lens[k].live, at)};
             break;
         }
-        before = __shfl(upto, 63, 64);
+        before = __builtin_amdgcn_readlane(upto, 63);
+        divided = __builtin_amdgcn_readlane(kept_upto, 63);
     }
-    p.b = __builtin_amdgcn_readfirstlane(p.b); p.part = __builtin_amdgcn_readfirstlane(p.part);
-    p.parts = __builtin_amdgcn_readfirstlane(p.parts); p.first = __builtin_amdgcn_readfirstlane(p.first);
     return p;
 }
 // A part's partial result: [rows][D] sums, then the rows' references, then their sums of weights.
@@ -170,35 +153,35 @@ __device__ __forceinline__ void store_part(const PageAttnArgs &a, int b, int h, 
     else *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
     if (a.t.lse && ch == 0)
         a.t.lse[((int64_t)b * a.c.n_heads * a.t.group + p.head) * a.t.n_new + p.i] =
-            seen ? (m + (__builtin_log2f(l) - kPgUp)) * 0.6931471805599453f : -INFINITY;
+            seen ? (m * a.scale + (__builtin_log2f(l) - kPgUp)) * 0.6931471805599453f : -INFINITY;
 }
 
-// A tile: tokens first .. first + count - 1 of the sequence, of which those from `last` on are not there and those in sink .. lo - 1
-// are seen by no row.
-struct Tile { int first, last, page_index; int64_t page; };
-
 // A lane's tokens of a tile are places in its page (paged), or rows anywhere in the pool, which lanes 0 .. 31 look up and leave in LDS.
-template <class T, int D, int RB, bool PAGED>
+// ONCE: no other workgroup reads the values again: they are loaded past the caches' usual order of eviction, which takes 4.6 GB at 6.75 TB/s
+// instead of 6.06 (keys too: the same, but half as fast where a few workgroups read alone, since a row's keys come by halves
+// of a line).
+template <class T, int D, int RB, bool PAGED, bool ONCE>
 __global__ __launch_bounds__(kPgThreads, D > 192 || D * RB > 256 ? 1 : 2)
 void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
     typedef PgDim<D> G;
     constexpr int kRows = 16 * RB, KK = G::KK, NS = G::NS, CH = G::CH, W = G::W;
     __shared__ __attribute__((aligned(16))) float meet[kPgWaves][16][G::pitch];
     __shared__ float ms[kPgWaves][kRows], ls[kPgWaves][kRows];
-    __shared__ __attribute__((aligned(16))) int64_t rows_of[PAGED ? 1 : kPgWaves][2][kPgTile];
+    __shared__ __attribute__((aligned(16))) int64_t rows_of[PAGED ? 1 : kPgWaves][kPgTile];
     // workgroups are dealt to the 8 XCDs round-robin: a head's row blocks, which read the same tokens, run on one
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
     const int units = a.c.n_heads * a.row_blocks, slot = w / units, unit = w - slot * units;
     const int h = unit / a.row_blocks, rblk = unit - h * a.row_blocks;
-    int b = slot, part = 0, parts = 1;
+    int b = slot, part = 0, parts = 1, first = 0;
+    PgLens lens;
     if (a.slots) {
         const Slot s = deal(a, slot);
-        if (s.parts == 0 || s.part >= s.parts) return;                   // uniform, before any barrier
-        b = s.b; part = s.part; parts = s.parts;
-        if (unit == 0 && part == 0 && threadIdx.x == 0) a.places[b] = make_int2(s.first, parts);
-    }
-    const Span sq = span_of(a, b);
+        if (s.part >= s.parts) return;                                   // uniform, before any barrier
+        b = s.b; part = s.part; parts = s.parts; first = s.first; lens = s.n;
+        if (unit == 0 && part == 0 && threadIdx.x == 0) a.places[b] = make_int2(first, parts);
+    } else lens = lens_of(a, b);
+    const PgSpan sq = pg_span_of(a, lens);
     const int lo_tile = (int)((int64_t)sq.total * part / parts), hi_tile = (int)((int64_t)sq.total * (part + 1) / parts);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
@@ -233,70 +216,56 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
     const int all_low = a.t.window > 0 && sq.kv - 1 >= a.t.window ? sq.kv - a.t.window : 0;
 
     // ---- where a tile's tokens lie ------------------------------------------------------------
-    auto tile_at = [&](int v) {                                          // the sequence's v-th tile
-        const int ti = v < sq.sink_tiles ? v : v - sq.sink_tiles + sq.main_tile;
-        Tile x;
-        if (PAGED) {
-            x.page_index = (int)quotient((uint32_t)ti, a.by_tiles);
-            x.first = x.page_index * (int)a.by_page.d + (ti - x.page_index * (int)a.by_tiles.d) * kPgTile;
-            x.last = min(min(x.first + kPgTile, (x.page_index + 1) * (int)a.by_page.d), sq.kv);
-        } else { x.page_index = 0; x.first = ti * kPgTile; x.last = min(x.first + kPgTile, sq.kv); }
-        x.page = 0;
-        return x;
-    };
     auto in_pool = [&](int pg) -> int64_t { return pg < 0 ? 0 : (pg >= a.c.pool_pages ? a.c.pool_pages - 1 : pg); };
     const int32_t *table = a.c.page_table + (int64_t)b * a.c.table_pages;
-    // token `off` of a tile, or one that some row sees instead of it
-    auto seen_token = [&](const Tile &x, int off) {
-        int n = min(x.first + off, x.last - 1);
-        if (n >= sq.sink && n < sq.lo) n = sq.lo < x.last ? sq.lo : sq.sink - 1;
-        return n;
-    };
     // (not paged) the rows of a tile's tokens: their pages are asked for a tile ahead
-    struct Ahead { int n, in_page; int64_t page; };
-    auto ask = [&](const Tile &x) {
+    struct Ahead { int n, in_page, page; };
+    auto ask = [&](const PgTile &x) {
         Ahead p;
-        p.n = seen_token(x, lane & 31);
+        p.n = pg_seen_token(sq, x, lane & 31);
         const int pi = (int)quotient((uint32_t)p.n, a.by_page);
         p.in_page = p.n - pi * (int)a.by_page.d;
-        p.page = in_pool(table[pi]);
+        p.page = table[pi];
         return p;
     };
-    auto park = [&](const Ahead &p, int par) {
-        if (lane < 32) rows_of[PAGED ? 0 : wave][par][lane] = p.page * a.c.stride_page + (int64_t)p.in_page * a.c.stride_token;
+    auto park = [&](const Ahead &p) {
+        if (lane < 32) rows_of[PAGED ? 0 : wave][lane] = in_pool(p.page) * a.c.stride_page + (int64_t)p.in_page * a.c.stride_token;
         asm volatile("" ::: "memory");                                   // the wavefront's LDS operations stay in this order
     };
-    auto row_ptr = [&](const uint16_t *pool, const Tile &x, int par, int off) {
+    auto row_ptr = [&](const uint16_t *pool, const PgTile &x, int off) {
         if constexpr (PAGED) {
-            const int n = seen_token(x, off) - x.page_index * (int)a.by_page.d;
+            const int n = pg_seen_token(sq, x, off) - x.page_index * (int)a.by_page.d;
             return reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(pool + x.page * a.c.stride_page) + (uint64_t)((uint32_t)n) * row_bytes);
-        } else return pool + rows_of[PAGED ? 0 : wave][par][off];
+        } else return pool + rows_of[PAGED ? 0 : wave][off];
     };
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
     uint4 kr[2][KK];
     uint32_t vr[NS][8][W];
-    auto load_k = [&](const Tile &x, int par) {
+    auto load_k = [&](const PgTile &x) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            const uint16_t *p = row_ptr(kp, x, par, 16 * hf + c) + 8 * kb;
+            const uint16_t *p = row_ptr(kp, x, 16 * hf + c) + 8 * kb;
 #pragma unroll
             for (int i = 0; i < KK; ++i) kr[hf][i] = *reinterpret_cast<const uint4 *>(p + 32 * i);
         }
     };
-    auto load_v = [&](const Tile &x, int par) {
+    auto load_v = [&](const PgTile &x) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint16_t *p = row_ptr(vp, x, par, 16 * (e >> 2) + 4 * kb + (e & 3));
+            const uint16_t *p = row_ptr(vp, x, 16 * (e >> 2) + 4 * kb + (e & 3));
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const int oct = min(16 * s + c, D / CH - 1);             // (octets beyond the head: results that nobody stores)
-                if constexpr (CH == 8) __builtin_memcpy(vr[s][e], reinterpret_cast<const uint4 *>(p + oct * CH), 16);
-                else __builtin_memcpy(vr[s][e], reinterpret_cast<const uint2 *>(p + oct * CH), 8);
+                const words *from = reinterpret_cast<const words *>(p + oct * CH);
+                const words got = ONCE ? __builtin_nontemporal_load(from) : *from;
+                __builtin_memcpy(vr[s][e], &got, sizeof(words));
             }
         }
     };
 
     floatx4_t O[RB][NS][CH];
     float m[RB], l[RB];
+    const float lag = kPgLag / a.scale;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         m[rb] = kPgNoScore; l[rb] = 0.0f;
@@ -306,20 +275,23 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
             for (int j = 0; j < CH; ++j) O[rb][s][j] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    int v = lo_tile + wave, par = 0;
-    Tile x{}, nx{};
-    Ahead ahead{};
-    auto find = [&](int at) {                                            // tile `at`, or the part's last one
-        const Tile y0 = tile_at(min(at, hi_tile - 1));
-        if constexpr (PAGED) { Tile y = y0; y.page = in_pool(((const __attribute__((address_space(4))) int32_t *)table)[y.page_index]); return y; }
-        else { ahead = ask(y0); return y0; }
+    // x is in registers, or on its way there; the one that follows it there is next, whose page is known or asked for.  (A wavefront asks for
+    // tiles behind its last one too: behind a branch around the loads the waits for those before would be for all of them.)
+    int v = lo_tile + wave;
+    PgTile x, next;
+    Ahead ahead;
+    auto find = [&](int at) {
+        PgTile y = pg_tile_at(a, sq, at, hi_tile);
+        if constexpr (PAGED) y.page = in_pool(((const __attribute__((address_space(4))) int32_t *)table)[y.page_index]);
+        else ahead = ask(y);
+        return y;
     };
     if (v < hi_tile) {
         x = find(v);
-        if (!PAGED) park(ahead, 0);
-        load_k(x, 0);
-        nx = find(v + kPgWaves);
-        load_v(x, 0);
+        if (!PAGED) park(ahead);
+        load_k(x);
+        next = find(v + kPgWaves);
+        load_v(x);
     }
     for (; v < hi_tile; v += kPgWaves) {
         // ---- S^T = K Q^T -------------------------------------------------------------------
@@ -332,34 +304,35 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
 #pragma unroll
                 for (int i = 0; i < KK; ++i) S[rb][hf] = T::mfma(kr[hf][i], q[rb][i], S[rb][hf]);
             }
-        // (behind the last tile that one comes again: behind a branch around these loads the values' wait would be for all of them)
         __builtin_amdgcn_sched_barrier(0);                               // (loads before their registers' last use would need others)
-        if (!PAGED) park(ahead, par ^ 1);
-        const Tile nnx = find(v + 2 * kPgWaves);                         // (its page is waited for behind these keys otherwise)
-        load_k(nx, par ^ 1);
+        const PgTile now = x;
+        x = next;
+        if (!PAGED) park(ahead);
+        next = find(v + 2 * kPgWaves);                                   // (behind these keys its page would be waited for with them)
+        load_k(x);
 
         // ---- soft-max: the lane has tokens 16 hf + 4 kb + r of row c ------------------------
-        const bool all = x.last - x.first == kPgTile && x.first >= all_low && x.last <= all_up;     // uniform
+        const bool all = now.last - now.first == kPgTile && now.first >= all_low && now.last <= all_up;     // uniform
         uint4 ph[RB], pl[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = S[rb][e >> 2][e & 3] * a.scale;
+            for (int e = 0; e < 8; ++e) p[e] = S[rb][e >> 2][e & 3];
             if (!all) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int n = x.first + 16 * (e >> 2) + 4 * kb + (e & 3);
-                    p[e] = n < x.last && n < up[rb] && (n >= low[rb] || n < a.t.sink) ? p[e] : -INFINITY;
+                    const int n = now.first + 16 * (e >> 2) + 4 * kb + (e & 3);
+                    p[e] = n < now.last && n < up[rb] && (n >= low[rb] || n < a.t.sink) ? p[e] : -INFINITY;
                 }
             }
             float top = p[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, p[e]);
-            if (__ballot(top - m[rb] > kPgLag)) {                        // uniform: some row's reference moves
+            if (__ballot(top - m[rb] > lag)) {                        // uniform: some row's reference moves
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float m_new = fmaxf(m[rb], top), alpha = __builtin_amdgcn_exp2f(m[rb] - m_new);
+                const float m_new = fmaxf(m[rb], top), alpha = __builtin_amdgcn_exp2f((m[rb] - m_new) * a.scale);
                 l[rb] *= alpha; m[rb] = m_new;
 #pragma unroll
                 for (int s = 0; s < NS; ++s)
@@ -367,12 +340,12 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
                     for (int j = 0; j < CH; ++j) O[rb][s][j] *= alpha;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f((p[e] - m[rb]) + kPgUp); l[rb] += p[e]; }
+            for (int e = 0; e < 8; ++e) { p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e] - m[rb], a.scale, kPgUp)); l[rb] += p[e]; }
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 hi[e] = T::pack(p[2 * e], p[2 * e + 1]);
-                lo[e] = T::pack(p[2 * e] - T::lo(hi[e]), p[2 * e + 1] - T::hi(hi[e]));
+                lo[e] = T::pack(__builtin_fmaf(T::lo(hi[e]), -1.0f, p[2 * e]), __builtin_fmaf(T::hi(hi[e]), -1.0f, p[2 * e + 1]));
             }
             ph[rb] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             pl[rb] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -395,9 +368,7 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
                 }
             }
         __builtin_amdgcn_sched_barrier(0);
-        load_v(nx, par ^ 1);
-        x = nx; nx = nnx;
-        par ^= 1;
+        load_v(x);
     }
 
     // ---- the wavefronts' results meet ------------------------------------------------------
@@ -414,13 +385,13 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
         float mm = ms[0][rb * 16 + c];
 #pragma unroll
         for (int i = 1; i < kPgWaves; ++i) mm = fmaxf(mm, ms[i][rb * 16 + c]);
-        const float f = __builtin_amdgcn_exp2f(m[rb] - mm);
+        const float f = __builtin_amdgcn_exp2f((m[rb] - mm) * a.scale);
         const int64_t r = (int64_t)rblk * kRows + rb * 16 + row;
         float mt = ms[0][rb * 16 + row], lt = 0.0f;
 #pragma unroll
         for (int i = 1; i < kPgWaves; ++i) mt = fmaxf(mt, ms[i][rb * 16 + row]);
 #pragma unroll
-        for (int i = 0; i < kPgWaves; ++i) lt += ls[i][rb * 16 + row] * __builtin_amdgcn_exp2f(ms[i][rb * 16 + row] - mt);
+        for (int i = 0; i < kPgWaves; ++i) lt += ls[i][rb * 16 + row] * __builtin_amdgcn_exp2f((ms[i][rb * 16 + row] - mt) * a.scale);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             if (rb + s > 0) __syncthreads();
@@ -440,8 +411,8 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
                 for (int e = 0; e < CH; ++e) o[e] += meet[i][row][CH * oc + e];
             const int ch = CH * (16 * s + oc);
             if (ch >= D) continue;
-            if (a.slots) {
-                float *st = a.state + ((int64_t)unit * a.slots + slot) * part_floats(kRows, D), *op = st + (rb * 16 + row) * D + ch;
+            if (parts > 1) {
+                float *st = a.state + ((int64_t)unit * a.kept + first + part) * part_floats(kRows, D), *op = st + (rb * 16 + row) * D + ch;
 #pragma unroll
                 for (int e = 0; e < CH; e += 4) *reinterpret_cast<float4 *>(op + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 if (ch == 0) { st[kRows * D + rb * 16 + row] = mt; st[kRows * (D + 1) + rb * 16 + row] = lt; }
@@ -450,56 +421,72 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
     }
 }
 
-// Joins a query row's parts: a workgroup to a row, D / 4 lanes (four channels each) to a part, as many parts at a time as fit.
-template <class T, int D>
+// Joins query rows' parts: D / 4 lanes (four channels each) to a part, PER parts of a row at a time, as many rows to a workgroup as fit.
+template <class T, int D, int PER>
 __global__ __launch_bounds__(256)
-void join_pages_kernel(PageAttnArgs a, int block_rows) {
-    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+void join_pages_kernel(PageAttnArgs a, int64_t n_rows) {
+    constexpr int kLanes = D / 4, kRows = 256 / (kLanes * PER), kGroups = kRows * PER;
     __shared__ __attribute__((aligned(16))) float sums[kGroups][D];
-    __shared__ float weights[kGroups];
+    __shared__ float weights[kGroups], tops[kGroups];
     const int64_t rows = (int64_t)a.t.group * a.t.n_new;
-    const int64_t bh = (int64_t)(blockIdx.x / (unsigned)rows), r = (int64_t)blockIdx.x - bh * rows;
+    const int grp = (int)threadIdx.x / kLanes, c4 = (int)threadIdx.x - grp * kLanes, j = grp / PER;
+    const int64_t at = (int64_t)blockIdx.x * kRows + j;
+    const bool there = j < kRows && at < n_rows;
+    const int64_t bh = (int64_t)((uint32_t)at / (uint32_t)rows), r = at - bh * rows;
     const int b = (int)(bh / a.c.n_heads), h = (int)(bh - (int64_t)b * a.c.n_heads);
-    const int row = (int)(r % block_rows), grp = (int)threadIdx.x / kLanes, c4 = (int)threadIdx.x - grp * kLanes;
-    const int64_t step = part_floats(block_rows, D);
-    const int2 place = a.places[b];                                      // first slot, parts
-    const float *st = a.state + (((int64_t)h * a.row_blocks + r / block_rows) * a.slots + place.x) * step;
-    const float *mp = st + block_rows * D + row, *lp = mp + block_rows, *op = st + row * D + c4 * 4;
+    // a group's parts one after the other, their sums against the largest reference so far
     float m = kPgNoScore, l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    // every lane finds the maximum over all parts: lane i of 64 looks at parts i, i + 64, ..
-    for (int p = threadIdx.x & 63; p < place.y; p += 64) m = fmaxf(m, mp[p * step]);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-    if (grp < kGroups) {
+    int parts = 0;
+    if (there) {
+        const int2 place = a.places[b];                                  // first partial result, parts
+        const int row = (int)(r % a.rows);
+        const int64_t step = part_floats(a.rows, D);
+        const float *st = a.state + (((int64_t)h * a.row_blocks + r / a.rows) * a.kept + place.x) * step;
+        const float *mp = st + a.rows * D + row, *lp = mp + a.rows, *op = st + row * D + c4 * 4;
+        parts = place.y > 1 ? place.y : 0;                               // (one: its workgroup has stored the row)
 #pragma unroll 4
-        for (int p = grp; p < place.y; p += kGroups) {
-            const float f = __builtin_amdgcn_exp2f(mp[p * step] - m);
+        for (int p = grp - j * PER; p < parts; p += PER) {
+            const float mx = mp[p * step], lx = lp[p * step];
             const float4 x = *reinterpret_cast<const float4 *>(op + p * step);
-            l += lp[p * step] * f;
+            const float m_new = fmaxf(m, mx), f = __builtin_amdgcn_exp2f((mx - m_new) * a.scale), g = __builtin_amdgcn_exp2f((m - m_new) * a.scale);
+            m = m_new;
+            l = l * g + lx * f;
+            o.x = o.x * g + x.x * f; o.y = o.y * g + x.y * f; o.z = o.z * g + x.z * f; o.w = o.w * g + x.w * f;
+        }
+    }
+    if constexpr (PER > 1) {
+        if (there) {
+            *reinterpret_cast<float4 *>(&sums[grp][c4 * 4]) = o;
+            if (c4 == 0) { weights[grp] = l; tops[grp] = m; }
+        }
+        __syncthreads();
+        if (!parts || grp != j * PER) return;
+#pragma unroll
+        for (int g = 0; g < PER; ++g) m = fmaxf(m, tops[grp + g]);
+        l = 0.0f;
+        o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int g = 0; g < PER; ++g) {
+            const float4 x = *reinterpret_cast<const float4 *>(&sums[grp + g][c4 * 4]);
+            const float f = __builtin_amdgcn_exp2f((tops[grp + g] - m) * a.scale);
+            l += weights[grp + g] * f;
             o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
         }
-        *reinterpret_cast<float4 *>(&sums[grp][c4 * 4]) = o;
-        if (c4 == 0) weights[grp] = l;
-    }
-    __syncthreads();
-    if (threadIdx.x >= D / 4) return;
-    l = 0.0f;
-    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        const float4 x = *reinterpret_cast<const float4 *>(&sums[g][threadIdx.x * 4]);
-        l += weights[g];
-        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
-    }
+    } else if (!parts) return;
     const float v[4] = {o.x, o.y, o.z, o.w};
-    store_part<T, 4>(a, b, h, r, a.t.n_live ? max(0, min(a.t.n_live[b], a.t.n_new)) : a.t.n_new, (int)threadIdx.x * 4, v, m, l);
+    store_part<T, 4>(a, b, h, r, a.t.n_live ? max(0, min(a.t.n_live[b], a.t.n_new)) : a.t.n_new, c4 * 4, v, m, l);
+}
+template <class T, int D, int PER>
+static void launch_join(const PageAttnArgs &a, int64_t n, hipStream_t s) {
+    constexpr int kRows = 256 / (D / 4 * PER);
+    join_pages_kernel<T, D, PER><<<dim3((unsigned)((n + kRows - 1) / kRows)), dim3(256), 0, s>>>(a, n);
 }
 
 bool page_attn_dim(int d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
 
 PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
-    PagePlan p{16, 1, 0, 0, 0};
+    PagePlan p{16, 1, 0, 0, 0, 0, 0};
     // Tiles end where pages do, so that a tile's page is uniform, unless that would leave many of them short.
     p.paged = c.page_len % kPgTile == 0 || c.page_len >= 8 * kPgTile;
     const int64_t rows = (int64_t)t.group * t.n_new;
@@ -508,13 +495,29 @@ PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
     const int64_t units = (int64_t)c.n_heads * p.row_blocks;             // of a sequence
     if (c.n_seqs < 1 || c.n_seqs > 256 || rows < 1) return p;
     const int64_t tiles = p.paged ? (int64_t)c.table_pages * page_tiles((int)c.page_len) : page_tiles((int)(c.table_pages * c.page_len));
-    int64_t slots = 512 / units;
-    const int64_t most = c.n_seqs * (tiles / kPgLeast);
-    if (slots > most) slots = most;
+    // Two workgroups to a CU, which lengths that differ are dealt to best, or one where no two fit a CU, and for a sequence alone, whose
+    // parts are all alike (4 heads x 64 rows over 32768 tokens 27 -> 23 us, 256 channels 176 -> 168; a ragged batch of 16: 182 -> 176 us
+    // with two; three or four lose 1 to 10 % of a long cache's rate); a tile to a wavefront at least.  With more sequences than
+    // that a call is divided only for those that are much longer than the others (extra).
+    // Not divided below 28 tiles, which cost less than the second launch (16 sequences of 500 tokens, 8 heads: 9.6 us, 13.4
+    // divided; 8 of 700: 10.8 and 13.0; but one of 1000: 12.6 and 8.2).
+    const int chip = c.n_seqs == 1 || c.head_dim > 192 || c.head_dim * p.rows > 16 * 256 ? 256 : 512;
+    if (tiles < 28 || (c.n_seqs == 1 && units > 128)) return p;          // (1024 rows of 8 heads over 8192: 79 us, 94 divided)
+    const int64_t full = (chip + units - 1) / units;
+    int64_t slots = chip / units;
     if (slots >= 2 * (int64_t)c.n_seqs) {
-        p.slots = (int)slots;
-        p.state_bytes = (size_t)(units * slots * part_floats(p.rows, c.head_dim)) * sizeof(float) + (size_t)c.n_seqs * sizeof(int2);
+        const int64_t most = c.n_seqs * (tiles / kPgWaves);
+        if (slots > most) slots = most;
+        p.extra = (int)(slots - c.n_seqs);
+        p.kept = (int)slots;
+    } else {
+        if (tiles < 256 || c.n_seqs * c.n_heads * rows > (1 << 22)) return p;                                       // (128 of 2000 tokens: 178 us, 215 so)
+        slots = c.n_seqs + full;
+        p.extra = (int)full;
+        p.kept = (int)(2 * full < slots ? 2 * full : slots);
     }
+    p.slots = (int)slots;
+    p.state_bytes = (size_t)(units * p.kept * part_floats(p.rows, c.head_dim)) * sizeof(float) + (size_t)c.n_seqs * sizeof(int2);
     return p;
 }
 
@@ -522,16 +525,15 @@ template <class T, int D>
 static void launch_dim(const PageAttnArgs &a, int blocks, hipStream_t s) {
     const int per_xcd = (blocks + 7) / 8;
     const dim3 grid((unsigned)(per_xcd * 8)), threads(kPgThreads);
-    if (a.rows == 16) {
-        if (a.paged) attn_pages_kernel<T, D, 1, true><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
-        else attn_pages_kernel<T, D, 1, false><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
-    } else {
-        if (a.paged) attn_pages_kernel<T, D, 2, true><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
-        else attn_pages_kernel<T, D, 2, false><<<grid, threads, 0, s>>>(a, blocks, per_xcd);
-    }
+    auto launch = [&](auto kernel) { kernel<<<grid, threads, 0, s>>>(a, blocks, per_xcd); };
+    if (a.rows == 16) launch(a.paged ? attn_pages_kernel<T, D, 1, true, true> : attn_pages_kernel<T, D, 1, false, true>);
+    else if (a.row_blocks == 1) launch(a.paged ? attn_pages_kernel<T, D, 2, true, true> : attn_pages_kernel<T, D, 2, false, true>);
+    else launch(a.paged ? attn_pages_kernel<T, D, 2, true, false> : attn_pages_kernel<T, D, 2, false, false>);
     if (a.slots) {
         const int64_t n = (int64_t)a.c.n_seqs * a.c.n_heads * a.t.group * a.t.n_new;
-        join_pages_kernel<T, D><<<dim3((unsigned)n), dim3(256), 0, s>>>(a, a.rows);
+        // (many rows have few parts)
+        if (n > 512) launch_join<T, D, 1024 / D < 4 ? 1 : 2>(a, n, s);
+        else launch_join<T, D, 1024 / D>(a, n, s);
     }
 }
 template <class T>

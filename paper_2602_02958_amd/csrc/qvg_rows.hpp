@@ -53,10 +53,11 @@ struct PageAttnArgs {
     FastDiv by_page, by_tiles;                    // tokens of a page, tiles of one
     int rows, row_blocks;                         // rows of a block of a KV head's query rows, and the blocks
     int slots;                                    // workgroups of a block of all sequences, dealt to them by their lengths; 0: one to each
-    float *state;                                 // partial results of the slots
-    int2 *places;                                 // [n_seqs] a sequence's first slot and its parts, for the joining launch
+    int extra, kept;                              // slots beyond one to a sequence; partial results of a block, at most
+    float *state;                                 // [blocks of all sequences][kept] partial results
+    int2 *places;                                 // [n_seqs] a sequence's first partial result and its parts, for the joining launch
 };
-struct PagePlan { int rows, row_blocks, slots, paged; size_t state_bytes; };
+struct PagePlan { int rows, row_blocks, slots, extra, kept, paged; size_t state_bytes; };      // (as in PageAttnArgs)
 PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t);
 bool page_attn_dim(int d);
 hipError_t launch_attn_pages(const PageAttnArgs &a, hipStream_t s);

@@ -172,6 +172,10 @@ def test_one_sequence_many_parts_and_many_sequences():
     kv = [(i * 37) % 90 for i in range(300)]              # (more than are divided)
     kv[7] = 900
     Case(kv, None, H=1, g=1, d=64, L=16, seed=21).check()
+    # many workgroups: only sequences much longer than the others are divided
+    Case([5000 if i == 13 else 40 + i for i in range(70)], None, H=8, g=1, d=64, L=32, seed=36).check()
+    Case([2600 if i in (0, 63) else 0 for i in range(64)], None, H=16, g=2, d=64, L=32, seed=37).check()
+    Case([900] * 40, None, H=8, g=1, d=64, L=64, seed=38).check()
     kv = [600 if i % 50 == 0 else i % 4 for i in range(200)]
     Case(kv, None, H=1, g=1, d=64, L=64, seed=22).check()
 
