@@ -785,16 +785,26 @@ def rope_table(n, frequencies, first=0, positions=None, axis=None, amplitude=1.0
 
 
 def _rows_of(x, name, dtype=None, shape=None, written=False):
-    """[B, H, N, d] view with a contiguous last dim -> its three strides (of a dimension of one element 0, as in _rows4)."""
-    if x.dtype not in TYPES or not x.is_cuda or (dtype is not None and x.dtype is not dtype):
+    """[B, H, N, d] view with a contiguous last dim -> its three strides (of a dimension of one element 0 where they break the alignment
+    rule, as in _rows4)."""
+    have = x.shape
+    if not x.is_cuda or (x.dtype is not dtype if dtype is not None else x.dtype not in TYPES):
         raise TypeError(f"{name}: expected a cuda tensor of {dtype or 'bfloat16, float16 or float32'}, got {x.dtype} on {x.device}")
-    if x.dim() != 4 or x.stride(3) != 1 or (shape is not None and x.shape != shape):
+    if len(have) != 4 or (shape is not None and have != shape):
         raise ValueError(f"{name}: need {'[B, H, N, d]' if shape is None else list(shape)} with unit stride along d")
-    a, b, c, _ = x.stride()
-    n = x.shape
-    if written and ((a == 0 and n[0] > 1) or (b == 0 and n[1] > 1) or (c == 0 and n[2] > 1)):
+    a, b, c, unit = x.stride()
+    if unit != 1 and have[3] != 1:
+        raise ValueError(f"{name}: need unit stride along d")
+    if written and not (a and b and c) and any(s == 0 and n > 1 for s, n in zip((a, b, c), have)):
         raise ValueError(f"{name}: rows that are written lie in places of their own")
-    return (0 if n[0] == 1 else a), (0 if n[1] == 1 else b), (0 if n[2] == 1 else c)
+    if (a | b | c) & 7:
+        return tuple(0 if n == 1 else s for n, s in zip(have, (a, b, c)))
+    return a, b, c
+
+
+def _same_strides(sx, sy, shape, names):
+    if sx != sy and any(a != b and n != 1 for a, b, n in zip(sx, sy, shape)):
+        raise ValueError(f"{names[0]} and {names[1]} must share their strides")
 
 
 def _rotary(table, half, positions, shape) -> QvgRotary:
@@ -821,8 +831,9 @@ def rope(x, table, positions=None, first=None, half=False, backward=False, out=N
         os_ = (H * m * d, m * d, d)
     else:
         os_ = _rows_of(out, "out", x.dtype, x.shape, True)
-        if out is not x and out.data_ptr() == x.data_ptr() and os_ != xs:
-            raise ValueError("out: a view of x needs x's strides")
+        if out.data_ptr() == x.data_ptr():
+            _same_strides(xs, os_, x.shape, ("x", "out"))
+            os_ = xs
     _here(x, table, positions, first, out)
     st = lib().qvg_rope(C.byref(r), TYPES[x.dtype], n, H, m, d, x.data_ptr(), *xs, None if first is None else _ints(first, (n,), "first"),
                         1 if backward else 0, out.data_ptr(), *os_, _stream())
@@ -838,15 +849,21 @@ def alloc_pages(heads, n_pages, page_len, head_dim=128, dtype=torch.bfloat16, de
 
 
 def _page_cache(k_pages, v_pages, page_table, kv_len, written=False) -> QvgPageCache:
-    if k_pages.dtype not in (torch.bfloat16, torch.float16):
+    shape, dtype, ks, table = k_pages.shape, k_pages.dtype, k_pages.stride(), page_table.shape
+    # (all in order at a glance: asking one by one costs more than the smallest call's launches)
+    if not (v_pages.stride() == ks and v_pages.shape == shape and v_pages.dtype is dtype and len(shape) == 4 and ks[3] == 1 and
+            not (ks[0] | ks[1] | ks[2]) & 7 and ks[0] and ks[1] and ks[2] and k_pages.is_cuda and v_pages.is_cuda):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("k_pages: pages are bfloat16 or float16")
+        ks = _rows_of(k_pages, "k_pages", None, None, written)
+        _same_strides(ks, _rows_of(v_pages, "v_pages", dtype, shape, written), shape, ("k_pages", "v_pages"))
+    if dtype is torch.float32 or dtype not in TYPES:
         raise TypeError("k_pages: pages are bfloat16 or float16")
-    ks = _rows_of(k_pages, "k_pages", None, None, written)
-    if _rows_of(v_pages, "v_pages", k_pages.dtype, k_pages.shape) != ks:
-        raise ValueError("k_pages and v_pages must share their strides")
-    H, P, L, d = k_pages.shape
-    n, pages = page_table.shape if page_table.dim() == 2 else (-1, 0)
-    return QvgPageCache(TYPES[k_pages.dtype], n, H, d, pages, 0, L, P, _ints(page_table, (n, pages), "page_table"), _ints(kv_len, (n,), "kv_len"),
-                        k_pages.data_ptr(), v_pages.data_ptr(), *ks)
+    if len(table) != 2:
+        raise ValueError("page_table: need [B, M]")
+    n, pages = table
+    return QvgPageCache(TYPES[dtype], n, shape[0], shape[3], pages, 0, shape[2], shape[1], _ints(page_table, table, "page_table"),
+                        _ints(kv_len, (n,), "kv_len"), k_pages.data_ptr(), v_pages.data_ptr(), ks[0], ks[1], ks[2])
 
 
 def append_pages(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new=None, k_rope=None, positions=None, half=False,
@@ -862,14 +879,14 @@ def append_pages(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new=None,
     n, H, m, d = k_new.shape
     if n != c.n_seqs or H != c.n_heads or d != c.head_dim:
         raise ValueError(f"k_new: need [{c.n_seqs}, {c.n_heads}, N, {c.head_dim}]")
-    if _rows_of(v_new, "v_new", k_pages.dtype, k_new.shape) != ns:
-        raise ValueError("k_new and v_new must share their strides")
+    _same_strides(ns, _rows_of(v_new, "v_new", k_pages.dtype, k_new.shape), k_new.shape, ("k_new", "v_new"))
     r = None
     if k_rope is not None:
         r = _rotary(k_rope, half, positions, (n, m))
     elif positions is not None:
         raise ValueError("positions without k_rope: keys are not turned")
-    out_len = torch.empty_like(kv_len) if out_len is None else out_len
+    if out_len is None:
+        out_len = torch.empty(n, dtype=torch.int32, device=kv_len.device)
     _here(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new, k_rope, positions, out_len)
     st = lib().qvg_append_pages(C.byref(c), m, k_new.data_ptr(), v_new.data_ptr(), *ns, None if n_new is None else _ints(n_new, (n,), "n_new"),
                                 None if r is None else C.byref(r), _ints(out_len, (n,), "out_len"), _stream())
@@ -907,8 +924,9 @@ def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True,
     c = _page_cache(k_pages, v_pages, page_table, kv_len)
     qs = _rows_of(q, "q", k_pages.dtype)
     n, hq, m, d = q.shape
-    H = c.n_heads
-    if n != c.n_seqs or d != c.head_dim or hq < H or hq % H:
+    H, L, pages = c.n_heads, c.page_len, c.table_pages
+    group = hq // H
+    if n != c.n_seqs or d != c.head_dim or hq < H or group * H != hq:
         raise ValueError(f"q: need [{c.n_seqs}, a multiple of {H} heads, N, {c.head_dim}]")
     if window is not None and window < 1:
         raise ValueError("window: a row sees its own place at least (None: no window)")
@@ -922,9 +940,9 @@ def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True,
         if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
             raise ValueError("scratch: need a contiguous uint8 tensor")
     else:
-        scratch = _scratch(_pages_scratch_bytes(n, H, d, hq // H, m, c.table_pages, c.page_len), q.device)
+        scratch = _scratch(_pages_scratch_bytes(n, H, d, group, m, pages, L), q.device)
     _here(q, k_pages, v_pages, page_table, kv_len, n_new, out, scratch)
-    t = QvgPageStep(hq // H, m, None if n_new is None else _ints(n_new, (n,), "n_new"), q.data_ptr(), *qs, 1 if causal else 0,
+    t = QvgPageStep(group, m, None if n_new is None else _ints(n_new, (n,), "n_new"), q.data_ptr(), *qs, 1 if causal else 0,
                     0 if window is None else min(window, 0x7fffffff), min(sink, 0x7fffffff), 0, out.data_ptr(), *os_, _ptr(lse))
     st = lib().qvg_attn_pages(C.byref(c), C.byref(t), 1.0 / (d ** 0.5) if softmax_scale is None else softmax_scale,
                               _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
