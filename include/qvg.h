@@ -540,7 +540,8 @@ typedef struct qvg_page_cache {    /* a HOST structure; its pointers are device 
  *   n_live        [n_seqs] int32, device, clamped to 0 .. n_new; NULL: n_new
  *   len_out       [n_seqs] int32 or NULL: kv_len[b] + n_live[b], at most table_pages * page_len; may be kv_len
  * A token beyond the table, or whose page is outside 0 .. pool_pages - 1, is not written; nothing else of the pool is touched.
- * Sequences that share a page must not write to the same places of it.  head_dim a multiple of 8 up to 512; n_seqs * n_new below 2^31.
+ * No two tokens may go to the same place (of a page that sequences share, or that a table names twice), and the pool must not overlap
+ * k_new or v_new.  head_dim a multiple of 8 up to 512; n_seqs * n_new below 2^31.
  */
 int qvg_append_pages(const qvg_page_cache *c, int64_t n_new, const void *k_new, const void *v_new, int64_t new_stride_seq,
                      int64_t new_stride_head, int64_t new_stride_token, const int32_t *n_live, const qvg_rotary *r, int32_t *len_out,
@@ -569,7 +570,7 @@ typedef struct qvg_page_step {
  * Rows i >= n_live[b], and rows that see no token, get a zero row and lse = -infinity.  What no row of a sequence sees may hold anything (also
  * what is no number): tokens behind kv_len, tokens between the first `sink` and the first row's window, whose pages may be
  * gone.  A page of a token that is seen, outside 0 .. pool_pages - 1, reads the nearest page of the pool.  All else must be
- * finite, and so must the scaled scores.
+ * finite, and so must the scores, before and after they are scaled.
  *   head_dim 64, 96, 128, 192 or 256; n_seqs times n_heads times blocks of 32 of a KV head's query rows at most 2^23
  *   out      may be q with q's strides; it overlaps no other input
  *   scratch  optional, 16-byte aligned: with qvg_attn_pages_scratch_bytes bytes the sequences' tokens are dealt to several workgroups

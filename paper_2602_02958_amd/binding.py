@@ -1204,13 +1204,23 @@ class PagedCache:
                 self.tails[seq] = n - full
                 self._tell(seq)
 
-    def append(self, seq, kv, k_rotated=None):
+    def append(self, seq, kv, k_rotated=None, k_rope=None):
         """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence.  pre_rope: kv
-        holds the keys before the rotary embedding, k_rotated [heads, n, d] bf16 the same ones rotated by their places."""
+        holds the keys before the rotary embedding, k_rotated [heads, n, d] bf16 the same ones rotated by their places; or k_rope
+        [n, d/2, 2] is the table that attend is given, and they are rotated here (rope)."""
         units, d = 2 * self.heads, self.tail.shape[3]
         if kv.dim() != 3 or kv.shape[0] != units or kv.shape[2] != d:
             raise ValueError(f"kv: need [{units}, n, {d}]")
         _check(kv, torch.bfloat16, "kv")
+        if k_rope is not None:
+            if k_rotated is not None:
+                raise ValueError("k_rotated and k_rope both give the rotated keys")
+            if not self.pre_rope:
+                raise ValueError("k_rope: needed by a cache of pre_rope keys, and by no other")
+            if k_rope.dim() != 3 or k_rope.shape[1] != d // 2:
+                raise ValueError(f"k_rope: need [n, {d // 2}, 2]")
+            self._open(seq)
+            k_rotated = rope(kv[None, :self.heads], k_rope, first=self.kv_len[seq:seq + 1] + self.tail_len[seq:seq + 1])[0]
         self._check_rotated(k_rotated)
         if k_rotated is not None:
             if k_rotated.shape != (self.heads, kv.shape[1], d):

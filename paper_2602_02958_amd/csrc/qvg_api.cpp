@@ -877,7 +877,7 @@ int qvg_rope_table(int64_t n_rows, int32_t n_pairs, const double *frequencies, i
     if (n_rows == 0) return QVG_OK;
     if (!frequencies || !out) return QVG_ERR_NULL;
     if (!aligned16(out) || (reinterpret_cast<uintptr_t>(frequencies) & 7u) || !aligned4(positions)) return QVG_ERR_ALIGN;
-    RopeTableArgs a{n_rows, n_pairs, n_axes, first, frequencies, positions, amplitude, out, {}};
+    RopeTableArgs a{n_rows, n_pairs, n_axes, first, frequencies, positions, amplitude, out, {}, 0};
     for (int p = 0; axis && p < n_pairs; ++p) a.axis[p] = (uint8_t)axis[p];
     return launch_rope_table(a, type == QVG_F32, static_cast<hipStream_t>(stream)) == hipSuccess ? QVG_OK : QVG_ERR_LAUNCH;
 }
@@ -952,7 +952,8 @@ int qvg_attn_pages_scratch_bytes(const qvg_page_cache *c, const qvg_page_step *t
 int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softmax_scale, void *scratch, size_t scratch_bytes, void *stream) {
     int st = check_page_step(c, t);
     if (st != QVG_OK) return st;
-    if (!(softmax_scale > 0.0f) || softmax_scale - softmax_scale != 0.0f) return QVG_ERR_BAD_PARAM;   // positive, finite
+    const float scale = softmax_scale * 1.4426950408889634f;
+    if (!(softmax_scale > 0.0f) || scale - scale != 0.0f) return QVG_ERR_BAD_PARAM;       // positive, finite, also to base 2
     if (c->n_seqs == 0 || t->n_new == 0) return QVG_OK;
     if ((st = check_cache_pointers(c)) != QVG_OK) return st;
     if (!t->q || !t->out) return QVG_ERR_NULL;
@@ -962,7 +963,7 @@ int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softma
         return QVG_ERR_ALIGN;
     const PagePlan plan = page_plan(*c, *t);
     PageAttnArgs a{};
-    a.c = *c; a.t = *t; a.scale = softmax_scale * 1.4426950408889634f;
+    a.c = *c; a.t = *t; a.scale = scale;
     a.paged = plan.paged; a.rows = plan.rows; a.row_blocks = plan.row_blocks;
     a.by_page = fast_div((uint32_t)c->page_len);
     a.by_tiles = fast_div((uint32_t)page_tiles((int)c->page_len));

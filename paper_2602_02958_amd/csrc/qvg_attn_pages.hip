@@ -265,7 +265,7 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
 
     floatx4_t O[RB][NS][CH];
     float m[RB], l[RB];
-    const float lag = kPgLag / a.scale;
+    const float lag = fminf(kPgLag / a.scale, 1e38f);                    // (any product is further than that above none)
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         m[rb] = kPgNoScore; l[rb] = 0.0f;

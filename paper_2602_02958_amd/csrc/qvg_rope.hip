@@ -28,7 +28,7 @@ void rope_table_kernel(RopeTableArgs a, FastDiv by_pairs, int rows_per_block) {
     typedef uint32_t two __attribute__((ext_vector_type(2)));
     typedef typename std::conditional<sizeof(TAB) == 4, two, uint32_t>::type pair;
     const int sub = (int)quotient(threadIdx.x, by_pairs), p = (int)threadIdx.x - sub * a.n_pairs;
-    const int64_t i0 = (int64_t)blockIdx.x * (rows_per_block * ROWS) + sub, left = a.n_rows - i0;
+    const int64_t i0 = (a.first_block + blockIdx.x) * (rows_per_block * ROWS) + sub, left = a.n_rows - i0;
     if (sub >= rows_per_block || left <= 0) return;
     const double quarters = a.freq[p] * 0.6366197723675814;
     // (rows, and pairs, are a fixed way apart: addresses are sums)
@@ -59,11 +59,15 @@ void rope_table_kernel(RopeTableArgs a, FastDiv by_pairs, int rows_per_block) {
         else *row = v;
     }
 }
+constexpr int64_t kMostBlocks = 1 << 23;        // of a launch: it has fewer than 2^32 threads along an axis
 template <typename TAB, int ROWS>
-static void launch_table(const RopeTableArgs &a, int64_t blocks, int per, hipStream_t s) {
+static void launch_table(RopeTableArgs a, int64_t blocks, int per, hipStream_t s) {
     const FastDiv by = fast_div((uint32_t)a.n_pairs);
-    if (a.positions) rope_table_kernel<TAB, ROWS, true><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
-    else rope_table_kernel<TAB, ROWS, false><<<dim3((unsigned)blocks), dim3(256), 0, s>>>(a, by, per);
+    for (a.first_block = 0; a.first_block < blocks; a.first_block += kMostBlocks) {
+        const dim3 n((unsigned)(blocks - a.first_block < kMostBlocks ? blocks - a.first_block : kMostBlocks));
+        if (a.positions) rope_table_kernel<TAB, ROWS, true><<<n, dim3(256), 0, s>>>(a, by, per);
+        else rope_table_kernel<TAB, ROWS, false><<<n, dim3(256), 0, s>>>(a, by, per);
+    }
 }
 constexpr int kTableRows = 16;     // of a thread, whose places it asks for together, where there are many
 hipError_t launch_rope_table(const RopeTableArgs &a, bool f32, hipStream_t s) {
@@ -305,9 +309,8 @@ static void launch_turn(TurnArgs &a, hipStream_t s) {
     a.by_units = fast_div((uint32_t)a.units);
     a.by_tokens = fast_div((uint32_t)a.n_tokens);
     const bool many = MODE != kTurnPair && blocks * a.H > 1024;
-    constexpr int64_t kMost = 1 << 23;                                   // (a launch has fewer than 2^32 threads along an axis)
-    for (a.first_block = 0; a.first_block < blocks; a.first_block += kMost) {
-        const unsigned n = (unsigned)(blocks - a.first_block < kMost ? blocks - a.first_block : kMost);
+    for (a.first_block = 0; a.first_block < blocks; a.first_block += kMostBlocks) {
+        const unsigned n = (unsigned)(blocks - a.first_block < kMostBlocks ? blocks - a.first_block : kMostBlocks);
         if constexpr (MODE != kTurnPair)
             if (many) {
                 turn_kernel<T, TAB, MODE, APPEND, kTurnHeads><<<dim3(n, (unsigned)heads), dim3(256), 0, s>>>(a, per, whole);

@@ -20,6 +20,7 @@ struct RopeTableArgs {
     int64_t n_rows; int n_pairs, n_axes; int64_t first;
     const double *freq; const int32_t *positions; float amplitude; void *out;
     uint8_t axis[256];
+    int64_t first_block;                          // of a launch
 };
 hipError_t launch_rope_table(const RopeTableArgs &a, bool f32, hipStream_t s);
 

@@ -164,6 +164,37 @@ def test_scales():
         Case([90, 513], None, H=1, g=4, L=64, seed=17).check(scale)
 
 
+def test_small_numbers_keep_their_bits():
+    """Subnormal values of binary16, and products that far below 1."""
+    c = Case([300, 40], None, H=1, g=2, L=16, dtype=F16, seed=40, poison=False)
+    c.v.mul_(2.0 ** -16)
+    c.k.mul_(2.0 ** -14)
+    c.check()
+    c.check(scale=2.0 ** 12)
+    c = Case([300, 40], None, H=1, g=2, L=16, dtype=BF, seed=41, poison=False)
+    c.v.mul_(2.0 ** -100)
+    c.q.mul_(2.0 ** -60), c.k.mul_(2.0 ** -60)
+    c.check()
+
+
+def test_large_scales_and_small_ones():
+    c = Case([200, 30], None, H=1, g=2, L=16, seed=42)
+    c.check(scale=1e-44)
+    c.check(scale=1e-38)
+    # products of at most 1 / 128, of which one is a power of two above the others
+    c = Case([200], None, H=1, g=1, L=32, seed=43, poison=False)
+    c.q.zero_(), c.k.zero_()
+    c.q[..., 0] = 2.0 ** -10
+    flat = c.table[0].long()
+    k = c.k[0, flat].flatten(0, 1)
+    k[:, 0] = 2.0 ** -11
+    k[77, 0] = 2.0 ** -10
+    c.k[0, flat] = k.view(flat.shape[0], 32, 128)
+    for scratch in (None, torch.empty(0, dtype=torch.uint8, device=DEV)):
+        out = B.attn_pages(**c.device(), softmax_scale=2.0 ** 100, scratch=scratch)
+        assert torch.equal(out[0, 0, 0].cpu(), c.v[0, flat].flatten(0, 1)[77])
+
+
 def test_one_sequence_many_parts_and_many_sequences():
     Case([5000], None, H=1, g=1, L=48, seed=18).check()
     Case([4000, 3, 2500], None, H=1, g=2, L=512, d=64, seed=19).check()
