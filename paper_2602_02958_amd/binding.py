@@ -896,20 +896,20 @@ def append_pages(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new=None,
 
 
 @functools.lru_cache(maxsize=256)
-def _pages_scratch_bytes(n_seqs, H, d, group, n_new, table_pages, page_len) -> int:
+def _pages_scratch_bytes(n_seqs, H, d, group, n_new, table_pages, page_len, window, sink) -> int:
     """Bytes of scratch of an attn_pages of these sizes (a function of its arguments alone)."""
     need = C.c_size_t()
     c = QvgPageCache(n_seqs=n_seqs, n_heads=H, head_dim=d, table_pages=table_pages, page_len=page_len, pool_pages=1)
-    st = lib().qvg_attn_pages_scratch_bytes(C.byref(c), C.byref(QvgPageStep(group=group, n_new=n_new)), C.byref(need))
+    st = lib().qvg_attn_pages_scratch_bytes(C.byref(c), C.byref(QvgPageStep(group=group, n_new=n_new, window=window, sink=sink)), C.byref(need))
     if st != 0:
         raise QvgError(st, "qvg_attn_pages_scratch_bytes")
     return need.value
 
 
 def attn_pages_scratch(k_pages, n_seqs, group, n_new, table_pages) -> torch.Tensor:
-    """Scratch for an attn_pages of these sizes over the pages k_pages."""
+    """Scratch for an attn_pages of these sizes over the pages k_pages, with a window or without."""
     H, _, L, d = k_pages.shape
-    return torch.empty(_pages_scratch_bytes(n_seqs, H, d, group, n_new, table_pages, L), dtype=torch.uint8, device=k_pages.device)
+    return torch.empty(_pages_scratch_bytes(n_seqs, H, d, group, n_new, table_pages, L, 0, 0), dtype=torch.uint8, device=k_pages.device)
 
 
 def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True, window=None, sink=0, softmax_scale=None, want_lse=False,
@@ -936,14 +936,15 @@ def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True,
     else:
         os_ = _rows_of(out, "out", q.dtype, q.shape, True)
     lse = torch.empty(n, hq, m, dtype=torch.float32, device=q.device) if want_lse else None
+    window, sink = 0 if window is None else min(window, 0x7fffffff), min(sink, 0x7fffffff)
     if scratch is not None:
         if scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
             raise ValueError("scratch: need a contiguous uint8 tensor")
     else:
-        scratch = _scratch(_pages_scratch_bytes(n, H, d, group, m, pages, L), q.device)
+        scratch = _scratch(_pages_scratch_bytes(n, H, d, group, m, pages, L, window, sink), q.device)
     _here(q, k_pages, v_pages, page_table, kv_len, n_new, out, scratch)
     t = QvgPageStep(group, m, None if n_new is None else _ints(n_new, (n,), "n_new"), q.data_ptr(), *qs, 1 if causal else 0,
-                    0 if window is None else min(window, 0x7fffffff), min(sink, 0x7fffffff), 0, out.data_ptr(), *os_, _ptr(lse))
+                    window, sink, 0, out.data_ptr(), *os_, _ptr(lse))
     st = lib().qvg_attn_pages(C.byref(c), C.byref(t), 1.0 / (d ** 0.5) if softmax_scale is None else softmax_scale,
                               _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream())
     if st != 0:

@@ -489,12 +489,17 @@ PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
     PagePlan p{16, 1, 0, 0, 0, 0, 0};
     // Tiles end where pages do, so that a tile's page is uniform, unless that would leave many of them short.
     p.paged = c.page_len % kPgTile == 0 || c.page_len >= 8 * kPgTile;
+    // tiles that a sequence's rows see, at most
+    int64_t tiles = p.paged ? (int64_t)c.table_pages * page_tiles((int)c.page_len) : page_tiles((int)(c.table_pages * c.page_len));
+    if (t.window > 0) {
+        const int64_t seen = (int64_t)t.window + t.n_new + t.sink, most = seen / kPgTile + 4 + (p.paged ? seen / c.page_len : 0);
+        if (most < tiles) tiles = most;
+    }
     const int64_t rows = (int64_t)t.group * t.n_new;
     p.rows = rows <= 16 ? 16 : 32;
     p.row_blocks = (int)((rows + p.rows - 1) / p.rows);
     const int64_t units = (int64_t)c.n_heads * p.row_blocks;             // of a sequence
     if (c.n_seqs < 1 || c.n_seqs > 256 || rows < 1) return p;
-    const int64_t tiles = p.paged ? (int64_t)c.table_pages * page_tiles((int)c.page_len) : page_tiles((int)(c.table_pages * c.page_len));
     // Two workgroups to a CU, which lengths that differ are dealt to best, or one where no two fit a CU, and for a sequence alone, whose
     // parts are all alike (4 heads x 64 rows over 32768 tokens 27 -> 23 us, 256 channels 176 -> 168; a ragged batch of 16: 182 -> 176 us
     // with two; three or four lose 1 to 10 % of a long cache's rate); a tile to a wavefront at least.  With more sequences than
@@ -511,7 +516,7 @@ PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
         p.extra = (int)(slots - c.n_seqs);
         p.kept = (int)slots;
     } else {
-        if (tiles < 256 || c.n_seqs * c.n_heads * rows > (1 << 22)) return p;                                       // (128 of 2000 tokens: 178 us, 215 so)
+        if (tiles < 256 || units >= chip || c.n_seqs * c.n_heads * rows > (1 << 22)) return p;       // (128 of 2000 tokens: 178 us, 215 so)
         slots = c.n_seqs + full;
         p.extra = (int)full;
         p.kept = (int)(2 * full < slots ? 2 * full : slots);

@@ -81,6 +81,14 @@ def test_row_counts(g, m, d):
     Case([130, 600], [m, 1], H=1, g=g, m=m, d=d, L=320, dtype=F16, causal=False, order="token", seed=3).check()
 
 
+@pytest.mark.parametrize("d,dtype", [(64, BF), (96, F16), (128, BF), (192, F16), (256, BF)])
+def test_many_rows(d, dtype):
+    """Rows of wavefronts' own, blocks of them that are not full, divided and not; pages of both kinds."""
+    Case([700, 350, 0, 33], [20, 20, 20, 7], H=2, g=16, m=20, d=d, L=24, dtype=dtype, seed=44).check()
+    Case([1500], [65], H=1, g=1, m=65, d=d, L=300, dtype=dtype, order="token", seed=45).check()
+    Case([1500, 2], [100, 3], H=1, g=3, m=100, d=d, L=32, dtype=dtype, window=300, sink=50, seed=46).check()
+
+
 @pytest.mark.parametrize("kv", [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1023, 1025, 2049])
 @pytest.mark.parametrize("L", [16, 64, 300])
 def test_lengths(kv, L):
