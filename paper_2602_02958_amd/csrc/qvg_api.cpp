@@ -967,6 +967,7 @@ int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softma
     a.paged = plan.paged; a.rows = plan.rows; a.row_blocks = plan.row_blocks;
     a.by_page = fast_div((uint32_t)c->page_len);
     a.by_tiles = fast_div((uint32_t)page_tiles((int)c->page_len));
+    a.by_units = fast_div((uint32_t)(c->n_heads * plan.row_blocks)); a.by_blocks = fast_div((uint32_t)plan.row_blocks); a.by_new = fast_div((uint32_t)t->n_new);
     a.slots = scratch && scratch_bytes >= plan.state_bytes ? plan.slots : 0;
     a.extra = plan.extra; a.kept = plan.kept;
     a.state = static_cast<float *>(scratch);

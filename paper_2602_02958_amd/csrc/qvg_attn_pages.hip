@@ -16,6 +16,8 @@
 // on their way all the time; twice as much changes nothing (one head over 32000 tokens 41 us so and so).  Memory bounds it.
 #include "qvg_attn_pages.hpp"
 
+#include <type_traits>
+
 namespace qvg {
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
@@ -66,61 +68,73 @@ __device__ __forceinline__ int parts_of(int total, int q) {
     return p < 1 ? 1 : p;
 }
 // Sums of lanes 0 .. i, and of all, between lanes of a row and then rows (no LDS, which five halvings of six exchanges would wait for)
-__device__ __forceinline__ int lanes_upto(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+template <typename N>
+__device__ __forceinline__ N lanes_upto(N x) {
+    auto from = [&](auto ctrl, auto rows) {
+        return __builtin_bit_cast(N, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    typedef std::integral_constant<int, 0xf> all;
+    x += from(std::integral_constant<int, 0x111>{}, all{});              // row_shr 1, 2, 4, 8
+    x += from(std::integral_constant<int, 0x112>{}, all{});
+    x += from(std::integral_constant<int, 0x114>{}, all{});
+    x += from(std::integral_constant<int, 0x118>{}, all{});
+    x += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});      // row_bcast 15, 31
+    x += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
     return x;
 }
-__device__ __forceinline__ int lanes_sum(int x) { return __builtin_amdgcn_readlane(lanes_upto(x), 63); }
-__device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot) {
+template <typename N>
+__device__ __forceinline__ N lanes_sum(N x) {
+    return __builtin_bit_cast(N, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lanes_upto(x)), 63));
+}
+// What a wavefront keeps of the sequences while it deals.  (Its loops are not unrolled: instructions that run once are waited for as they
+// are fetched, and 2600 before the first tile cost every call 0.6 us more than these 1100.)
+struct DealPlace { int2 lens[256]; int tiles[256]; };
+template <bool PAGED>
+__device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot, DealPlace &keep) {
     const int lane = threadIdx.x & 63, n = a.c.n_seqs;
     Slot p{0, 0, 0, 0, {0, 0}};
     if (n == 1) {
         p.n = lens_of(a, 0);
-        const int total = pg_span_of(a, p.n).total, q = max((total + a.slots - 1) / a.slots, kPgWaves);
+        const int total = pg_span_of<PAGED>(a, p.n).total, q = max(parts_of(total, a.slots), kPgWaves);
         p.parts = parts_of(total, q);
         p.part = slot;
         return p;
     }
-    int tiles[4];                                                        // of sequences lane, 64 + lane, ..
-    PgLens lens[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        lens[k] = PgLens{0, 0};
-        if (64 * k < n) lens[k] = lens_of(a, min(64 * k + lane, n - 1));
-        tiles[k] = 64 * k + lane < n ? pg_span_of(a, lens[k]).total : 0;
+    float total = 0.0f;
+#pragma unroll 1
+    for (int k = 0; k < n; k += 64) {
+        const int i = k + lane;
+        const PgLens l = lens_of(a, min(i, n - 1));
+        const int t = i < n ? pg_span_of<PAGED>(a, l).total : 0;
+        keep.lens[i] = make_int2(l.kv, l.live); keep.tiles[i] = t;
+        total += (float)t;
     }
-    int few = 0, many = 0;                                               // the total's two halves: it may pass 31 bits
-#pragma unroll
-    for (int k = 0; k < 4; ++k) { few += tiles[k] & 0xffff; many += tiles[k] >> 16; }
-    const int64_t total = lanes_sum(few) + ((int64_t)lanes_sum(many) << 16);
-    // (2^26: more tiles than a sequence has)
-    int q = max((int)min((total + a.extra - 1) / a.extra, (int64_t)1 << 26), kPgWaves), lo = n <= a.extra ? max((int)((total + a.slots - 1) / a.slots), kPgWaves) : q;
-    for (int i = 0; i < 5 && lo < q; ++i) {                              // uniform
+    total = lanes_sum(total);
+    // (rounded up, and down, by more than the sum is off; 2^26: more tiles than a sequence has)
+    int q = max((int)fminf(total * (1.0001f * __builtin_amdgcn_rcpf((float)a.extra)), 67108863.0f) + 1, kPgWaves);
+    int lo = n <= a.extra ? max((int)(total * (0.9999f * __builtin_amdgcn_rcpf((float)a.slots))), kPgWaves) : q;
+#pragma unroll 1
+    for (int h = 0; h < 5 && lo < q; ++h) {                              // uniform
         const int mid = lo + (q - lo) / 2;
         int need = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (64 * k < n) need += 64 * k + lane < n ? parts_of(tiles[k], mid) : 0;
+#pragma unroll 1
+        for (int k = 0; k < n; k += 64) need += k + lane < n ? parts_of(keep.tiles[k + lane], mid) : 0;
         if (lanes_sum(need) <= a.slots) q = mid; else lo = mid + 1;
     }
     int before = 0, divided = 0;                                         // slots, and partial results, of the sequences before
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (64 * k >= n) break;                                          // uniform
-        const int mine = 64 * k + lane < n ? parts_of(tiles[k], q) : 0, kept = mine > 1 ? mine : 0;
+#pragma unroll 1
+    for (int k = 0; k < n; k += 64) {
+        const int i = k + lane, mine = i < n ? parts_of(keep.tiles[i], q) : 0, kept = mine > 1 ? mine : 0;
         const int upto = before + lanes_upto(mine), kept_upto = divided + lanes_upto(kept);
         const unsigned long long hit = __ballot(slot >= upto - mine && slot < upto);
         if (hit) {
             const int at = __builtin_ctzll(hit);
-            p.b = 64 * k + at; p.parts = __builtin_amdgcn_readlane(mine, at);
+            p.b = k + at; p.parts = __builtin_amdgcn_readlane(mine, at);
             p.part = slot - (__builtin_amdgcn_readlane(upto, at) - p.parts);
             p.first = __builtin_amdgcn_readlane(kept_upto - kept, at);
-            p.n = PgLens{__builtin_amdgcn_readlane(lens[k].kv, at), __builtin_amdgcn_readlane(lens[k].live, at)};
+            asm volatile("" ::: "memory");                               // the wavefront's LDS operations stay in this order
+            const int2 l = keep.lens[p.b];
+            p.n = PgLens{__builtin_amdgcn_readfirstlane(l.x), __builtin_amdgcn_readfirstlane(l.y)};
             break;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
@@ -135,7 +149,7 @@ static __host__ __device__ inline int64_t part_floats(int rows, int d) { return 
 struct RowAt { int64_t head; int i; };
 __device__ __forceinline__ RowAt row_at(const PageAttnArgs &a, int h, int64_t r) {
     RowAt p;
-    const int u = (int)((uint32_t)r / (uint32_t)a.t.n_new);
+    const int u = (int)quotient((uint32_t)r, a.by_new);
     p.head = (int64_t)h * a.t.group + u; p.i = (int)r - u * a.t.n_new;
     return p;
 }
@@ -171,18 +185,20 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
     // workgroups are dealt to the 8 XCDs round-robin: a head's row blocks, which read the same tokens, run on one
     const int w = (int)(blockIdx.x % 8u) * per_xcd + (int)(blockIdx.x / 8u);
     if (w >= blocks) return;                                             // uniform, before any barrier
-    const int units = a.c.n_heads * a.row_blocks, slot = w / units, unit = w - slot * units;
-    const int h = unit / a.row_blocks, rblk = unit - h * a.row_blocks;
+    const int slot = (int)quotient((uint32_t)w, a.by_units), unit = w - slot * (int)a.by_units.d;
+    const int h = (int)quotient((uint32_t)unit, a.by_blocks), rblk = unit - h * a.row_blocks;
     int b = slot, part = 0, parts = 1, first = 0;
     PgLens lens;
     if (a.slots) {
-        const Slot s = deal(a, slot);
+        __shared__ DealPlace keep[kPgWaves];
+        const Slot s = deal<PAGED>(a, slot, keep[threadIdx.x >> 6]);
         if (s.part >= s.parts) return;                                   // uniform, before any barrier
         b = s.b; part = s.part; parts = s.parts; first = s.first; lens = s.n;
         if (unit == 0 && part == 0 && threadIdx.x == 0) a.places[b] = make_int2(first, parts);
     } else lens = lens_of(a, b);
-    const PgSpan sq = pg_span_of(a, lens);
-    const int lo_tile = (int)((int64_t)sq.total * part / parts), hi_tile = (int)((int64_t)sq.total * (part + 1) / parts);
+    const PgSpan sq = pg_span_of<PAGED>(a, lens);
+    int lo_tile, hi_tile;
+    pg_part(sq.total, part, parts, lo_tile, hi_tile);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, kb = lane >> 4;
     const int64_t rows = (int64_t)a.t.group * a.t.n_new;
@@ -281,7 +297,7 @@ void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
     PgTile x, next;
     Ahead ahead;
     auto find = [&](int at) {
-        PgTile y = pg_tile_at(a, sq, at, hi_tile);
+        PgTile y = pg_tile_at<PAGED>(a, sq, at, hi_tile);
         if constexpr (PAGED) y.page = in_pool(((const __attribute__((address_space(4))) int32_t *)table)[y.page_index]);
         else ahead = ask(y);
         return y;

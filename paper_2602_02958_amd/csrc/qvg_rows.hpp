@@ -51,7 +51,7 @@ struct PageAttnArgs {
     qvg_page_step t;
     float scale;                                  // times log2(e)
     int paged;                                    // tiles end where pages do (else they run on over them)
-    FastDiv by_page, by_tiles;                    // tokens of a page, tiles of one
+    FastDiv by_page, by_tiles, by_units, by_blocks, by_new;      // tokens of a page, tiles of one; heads x row blocks, row blocks, new tokens
     int rows, row_blocks;                         // rows of a block of a KV head's query rows, and the blocks
     int slots;                                    // workgroups of a block of all sequences, dealt to them by their lengths; 0: one to each
     int extra, kept;                              // slots beyond one to a sequence; partial results of a block, at most

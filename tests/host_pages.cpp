@@ -15,19 +15,23 @@ static PageAttnArgs args(int64_t table_pages, int64_t L, bool paged, int n_new, 
     return a;
 }
 
+static PgSpan span_of(const PageAttnArgs &a, PgLens n) { return a.paged ? pg_span_of<true>(a, n) : pg_span_of<false>(a, n); }
+static PgTile tile_at(const PageAttnArgs &a, const PgSpan &s, int v, int end) { return a.paged ? pg_tile_at<true>(a, s, v, end) : pg_tile_at<false>(a, s, v, end); }
+
 // Every token that some row sees lies in one tile of one part; every address that a wavefront forms, behind its last tile too, is one
 // of such a token, in the tile's page.
 static const char *walk(const PageAttnArgs &a, PgLens lens, int parts) {
-    const PgSpan s = pg_span_of(a, lens);
+    const PgSpan s = span_of(a, lens);
     const int L = (int)a.c.page_len;
     if (s.kv > a.c.table_pages * L || s.kv < 0 || (s.sink >= s.lo && s.lo)) return "span";
     auto seen = [&](int n) { return n >= 0 && n < s.kv && (n < s.sink || n >= s.lo); };
     std::vector<char> met(s.kv, 0);
     for (int part = 0; part < parts; ++part) {
-        const int lo = (int)((int64_t)s.total * part / parts), hi = (int)((int64_t)s.total * (part + 1) / parts);
+        int lo, hi;
+        pg_part(s.total, part, parts, lo, hi);
         if (lo >= hi) continue;
         for (int v = lo; v < hi + 24; ++v) {
-            const PgTile x = pg_tile_at(a, s, v, hi);
+            const PgTile x = tile_at(a, s, v, hi);
             for (int off = 0; off < kPgTile; ++off) {
                 const int n = pg_seen_token(s, x, off);
                 if (!seen(n)) return "token";
@@ -75,14 +79,16 @@ static const char *large(bool paged) {
                 for (int n_new : {1, 1000}) {
                     const int64_t pages = (1ll << 30) / L;
                     const PageAttnArgs a = args(pages, L, paged, n_new, w, sink);
-                    const PgSpan s = pg_span_of(a, PgLens{0x7fffffff, 0x7fffffff});
+                    const PgSpan s = span_of(a, PgLens{0x7fffffff, 0x7fffffff});
                     if (s.kv != pages * L || s.live != n_new || s.total < 1) return "span";
                     for (int parts : {1, 7, 512})
                         for (int part : {0, parts / 2, parts - 1}) {
-                            const int lo = (int)((int64_t)s.total * part / parts), hi = (int)((int64_t)s.total * (part + 1) / parts);
+                            int lo, hi;
+                            pg_part(s.total, part, parts, lo, hi);
+                            if (part == parts - 1 && hi != s.total) return "end";
                             for (int v : {lo, lo + 1, lo + 3, (lo + hi) / 2, hi - 2, hi - 1, hi, hi + 15}) {
                                 if (v < lo || lo >= hi) continue;
-                                const PgTile x = pg_tile_at(a, s, v, hi);
+                                const PgTile x = tile_at(a, s, v, hi);
                                 if (x.first < 0 || x.last <= x.first || x.last > s.kv || x.last - x.first > kPgTile) return "tile";
                                 for (int off = 0; off < kPgTile; ++off) {
                                     const int n = pg_seen_token(s, x, off);
