@@ -13,7 +13,10 @@
 // The weights enter as two numbers of the cache's type, w = hi + lo: the matrix cores have nothing else to do, and one number's
 // rounding (2^-8 of a bf16 weight) would be as large as the output's own.
 // A tile's keys are asked for when one before has been contracted, and so are its values: a wavefront has 16 KB (of 128 channels)
-// on their way all the time; twice as much changes nothing (one head over 32000 tokens 41 us so and so).  Memory bounds it.
+// on their way all the time; twice as much changes nothing (12 heads over 37440 tokens 41 us so and so).  Memory bounds it: 12 heads
+// over 748800 tokens of 128 bf16, 4.6 GB, 675 us (6.8 TB/s; a large copy moves 4.9); a ragged batch of 16, 8 heads x 4, 1.08 GB,
+// 175 us (6.1).  A call over few tokens is its launches, the walk to the first tile and 1 us a tile: 4.7 us for 100 tokens, 8 us for
+// 1000 (one head).
 #include "qvg_attn_pages.hpp"
 
 #include <type_traits>
@@ -172,8 +175,7 @@ __device__ __forceinline__ void store_part(const PageAttnArgs &a, int b, int h, 
 
 // A lane's tokens of a tile are places in its page (paged), or rows anywhere in the pool, which lanes 0 .. 31 look up and leave in LDS.
 // ONCE: no other workgroup reads the values again: they are loaded past the caches' usual order of eviction, which takes 4.6 GB at 6.75 TB/s
-// instead of 6.06 (keys too: the same, but half as fast where a few workgroups read alone, since a row's keys come by halves
-// of a line).
+// instead of 6.06 (keys too: no faster, and a fifth slower where few workgroups read, since a token's keys come by halves of a line).
 template <class T, int D, int RB, bool PAGED, bool ONCE>
 __global__ __launch_bounds__(kPgThreads, D > 192 || D * RB > 256 ? 1 : 2)
 void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {

@@ -10,7 +10,8 @@ namespace qvg {
 // A pair to a thread.  The angle is taken in quarter turns: place x frequency x 4 / 2 pi in 64 bits, less its nearest whole number (adding
 // 1.5 x 2^52 rounds to it, and leaves it in the sum's low bits), is half a quarter or less, which 32 bits hold to 2^-27 of a
 // turn.  Sine and cosine of that are Taylor's polynomials in 32 bits (their next terms are below 2^-29 at pi / 4), and the quarter says which
-// is which and its sign.
+// is which and its sign.  Memory bounds a large table of 32 bits: 748800 x 64 pairs and three axes, 392 MB, 66 us (5.9 TB/s); of 16 bits the
+// 35 instructions of a pair do, 51 us for 191 MB.
 __device__ __forceinline__ float2 cos_sin_of(double place, double quarters) {
     const double x = place * quarters, sum = x + 6755399441055744.0;
     const float r = (float)(x - (sum - 6755399441055744.0));
@@ -113,6 +114,17 @@ __device__ __forceinline__ void octet_of(const float *v, Octet<F16> &o) {
     o.w[0] = make_uint4(pack_f16x2_rne(v[0], v[1]), pack_f16x2_rne(v[2], v[3]), pack_f16x2_rne(v[4], v[5]), pack_f16x2_rne(v[6], v[7]));
 }
 __device__ __forceinline__ void octet_of(const float *v, Octet<F32> &o) { __builtin_memcpy(o.w, v, 32); }
+// the pairs of an octet from `from` on, as they were
+template <class T>
+__device__ __forceinline__ void keep_pairs(Octet<T> &o, const Octet<T> &was, int from) {
+    constexpr int kWords = sizeof(typename T::raw) / 2;                  // 32-bit words of a pair
+    uint32_t now[4 * kWords], old[4 * kWords];
+    __builtin_memcpy(now, o.w, sizeof(now));
+    __builtin_memcpy(old, was.w, sizeof(old));
+#pragma unroll
+    for (int i = 0; i < 4 * kWords; ++i) now[i] = i / kWords < from ? now[i] : old[i];
+    __builtin_memcpy(o.w, now, sizeof(now));
+}
 __device__ __forceinline__ float value_of(bf16_t x, Bf16) { return bf16_lo(x); }
 __device__ __forceinline__ float value_of(f16_t x, F16) { return f16_bits_to_f32(x); }
 __device__ __forceinline__ float value_of(float x, F32) { return x; }
@@ -161,7 +173,9 @@ enum { kTurnNext, kTurnHalf, kTurnPair, kTurnNone };
 constexpr int kTurnHeads = 4;      // heads that a thread takes at once, where there are many rows: they share the table's row
 
 // A thread takes a piece of a token's rows in `HP` heads: it reads the table's row once for all of them, and all rows before it
-// writes any.  Memory bounds it: the rows both ways.
+// writes any.  Memory bounds it, the rows both ways: 40 heads x 10800 rows of 128 bf16, 224 MB with the table, 40.7 us (5.5 TB/s); 12
+// heads x 4680 keys and values into pages, 59 MB, 11.6 us (5.1 TB/s; 14.2 with a head to a thread, written through the
+// caches); a token's 12 heads 2.4 us, a launch.
 template <class T, typename TAB, int MODE, bool APPEND, int HP>
 __global__ __launch_bounds__(256)
 void turn_kernel(TurnArgs a, int per_block, int whole) {
@@ -276,8 +290,11 @@ void turn_kernel(TurnArgs a, int per_block, int whole) {
                         for (int p = 0; p < 4; ++p)
                             if (u * 4 + p < P) turn(f[0][2 * p], f[0][2 * p + 1], cs[p]);
                     }
+                    const Octet<T> was = x[k][0];
 #pragma unroll
                     for (int o = 0; o < kOct; ++o) octet_of(f[o], x[k][o]);
+                    if constexpr (MODE == kTurnNext)
+                        if (u * 4 + 4 > P) keep_pairs(x[k][0], was, P - u * 4);      // (what is not turned stays bit for bit)
                 }
 #pragma unroll
                 for (int o = 0; o < kOct; ++o)

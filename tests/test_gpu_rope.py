@@ -131,14 +131,21 @@ def test_a_table_that_starts_between_16_byte_places_and_strided_outputs():
     assert (out[..., 128:] == 7).all()                       # nothing behind the rows
 
 
-def test_channels_behind_the_pairs_stay_bit_for_bit_even_no_numbers():
-    x = rows((1, 2, 3, 128), BF, 12)
-    x[..., 64:] = math.nan
+@pytest.mark.parametrize("pairs", [32, 30, 29, 1])
+@pytest.mark.parametrize("dtype", [BF, F16, F32])
+def test_channels_behind_the_pairs_stay_bit_for_bit_even_no_numbers(dtype, pairs):
+    x = rows((1, 2, 3, 128), dtype, 12)
+    whole = {2: torch.int16, 4: torch.int32}[x.element_size()]
+    bits = x.view(whole)
+    top = -1 if whole is torch.int16 else -(1 << 20)
+    bits[..., 2 * pairs:] = torch.arange(128 - 2 * pairs, dtype=whole) + (top - 200)            # no numbers, of many kinds
     x[..., 100] = math.inf
     for half in (False, True):
-        got = B.rope(x.to(DEV), table(3, 32, F16, 13).to(DEV), half=half).cpu()
-        assert torch.equal(got[..., 64:].view(torch.int16), x[..., 64:].contiguous().view(torch.int16))
-        assert torch.isfinite(got[..., :64].float()).all()
+        for out in (None, x.to(DEV)):
+            xd = x.to(DEV) if out is None else out
+            got = B.rope(xd, table(3, pairs, F16, 13).to(DEV), half=half, out=out).cpu()
+            assert torch.equal(got.view(whole)[..., 2 * pairs:], bits[..., 2 * pairs:])
+            assert torch.isfinite(got[..., :2 * pairs].float()).all()
 
 
 def test_gradient_against_differences():
