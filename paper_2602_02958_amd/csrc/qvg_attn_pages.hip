@@ -175,7 +175,8 @@ __device__ __forceinline__ void store_part(const PageAttnArgs &a, int b, int h, 
 
 // A lane's tokens of a tile are places in its page (paged), or rows anywhere in the pool, which lanes 0 .. 31 look up and leave in LDS.
 // ONCE: no other workgroup reads the values again: they are loaded past the caches' usual order of eviction, which takes 4.6 GB at 6.75 TB/s
-// instead of 6.06 (keys too: no faster, and a fifth slower where few workgroups read, since a token's keys come by halves of a line).
+// instead of 6.06 (keys too: divided calls no faster than so, undivided ones slower, a ragged batch of 16 211 -> 246 us: a token's keys
+// come by halves of a line).
 template <class T, int D, int RB, bool PAGED, bool ONCE>
 __global__ __launch_bounds__(kPgThreads, D > 192 || D * RB > 256 ? 1 : 2)
 void attn_pages_kernel(PageAttnArgs a, int blocks, int per_xcd) {
@@ -520,8 +521,8 @@ PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
     if (c.n_seqs < 1 || c.n_seqs > 256 || rows < 1) return p;
     // Two workgroups to a CU, which lengths that differ are dealt to best, or one where no two fit a CU, and for a sequence alone, whose
     // parts are all alike (4 heads x 64 rows over 32768 tokens 27 -> 23 us, 256 channels 176 -> 168; a ragged batch of 16: 182 -> 176 us
-    // with two; three or four lose 1 to 10 % of a long cache's rate); a tile to a wavefront at least.  With more sequences than
-    // that a call is divided only for those that are much longer than the others (extra).
+    // with two; three take up to 20 % longer, four up to 41 %); a tile to a wavefront at least.  With more sequences than that a call
+    // is divided only for those that are much longer than the others (extra).
     // Not divided below 28 tiles, which cost less than the second launch (16 sequences of 500 tokens, 8 heads: 9.6 us, 13.4
     // divided; 8 of 700: 10.8 and 13.0; but one of 1000: 12.6 and 8.2).
     const int chip = c.n_seqs == 1 || c.head_dim > 192 || c.head_dim * p.rows > 16 * 256 ? 256 : 512;
