@@ -1236,7 +1236,8 @@ class PagedCache:
     def append(self, seq, kv, k_rotated=None, k_rope=None):
         """Tokens that are there already (a prompt), kv [2 * heads, n, d] bf16 (K heads first), behind the sequence.  pre_rope: kv
         holds the keys before the rotary embedding, k_rotated [heads, n, d] bf16 the same ones rotated by their places; or k_rope
-        [n, d/2, 2] is the table that attend is given, and they are rotated here (rope)."""
+        [n, d/2, 2] is the table that attend is given, with a row for every place of the sequence and the new tokens, and they are
+        rotated here (rope)."""
         units, d = 2 * self.heads, self.tail.shape[3]
         if kv.dim() != 3 or kv.shape[0] != units or kv.shape[2] != d:
             raise ValueError(f"kv: need [{units}, n, {d}]")
@@ -1248,7 +1249,10 @@ class PagedCache:
                 raise ValueError("k_rope: needed by a cache of pre_rope keys, and by no other")
             if k_rope.dim() != 3 or k_rope.shape[1] != d // 2:
                 raise ValueError(f"k_rope: need [n, {d // 2}, 2]")
-            self._open(seq)
+            end = self.length(seq) + kv.shape[1]
+            if k_rope.shape[0] < end:                  # (beyond a table its last row would count: keys of another place)
+                raise ValueError(f"k_rope: need the rows of {end} places, got {k_rope.shape[0]}")
+            self._need({seq: kv.shape[1]})
             k_rotated = rope(kv[None, :self.heads], k_rope, first=self.kv_len[seq:seq + 1] + self.tail_len[seq:seq + 1])[0]
         self._check_rotated(k_rotated)
         if k_rotated is not None:
