@@ -777,6 +777,7 @@ def rope_table(n, frequencies, first=0, positions=None, axis=None, amplitude=1.0
         raise ValueError(f"out: need a contiguous [{n}, {P}, 2] tensor")
     else:
         _check(out, dtype, "out")
+        torch.autograd.graph.increment_version(out)                      # (a gradient of rope that has kept it is an error then)
     _here(frequencies, positions, out)
     st = lib().qvg_rope_table(n, P, frequencies.data_ptr(), first, pos, A, ax, amplitude, TYPES[dtype], out.data_ptr(), _stream())
     if st != 0:
@@ -855,7 +856,35 @@ def rope(x, table, positions=None, first=None, half=False, backward=False, out=N
     """qvg_rope: rows of x [B, H, N, d] (bf16, float16 or float32) turned by a table [n, P, 2] (rope_table): the first 2P of their channels
     in pairs (2p, 2p + 1), or with half=True (p, p + P).  Token i of sequence b stands at positions[b, i] (int32 [B, N]), or at first[b] + i
     (int32 [B]), or at i; beyond the table the nearest row counts.  backward: the gradient with respect to the rows of a gradient x
-    with respect to the turned rows.  out may be x."""
+    with respect to the turned rows; that of a call on an x that requires a gradient is recorded, and made so (out is for calls without
+    one; table, positions and first have none).  out may be x."""
+    if (x.requires_grad or table.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
+        if out is not None:
+            raise ValueError("out: not for a call that a gradient is recorded of")
+        if table.requires_grad:
+            raise ValueError("table: a gradient with respect to it is not made (detach it)")
+        return _Turn.apply(x, table, positions, first, half, backward)
+    return _rope(x, table, positions, first, half, backward, out)
+
+
+class _Turn(torch.autograd.Function):
+    """rope with its gradient, which is the turn back by the same rows."""
+
+    @staticmethod
+    def forward(ctx, x, table, positions, first, half, backward):
+        # (copies: a step's lengths, which first often is, move on before its gradient comes)
+        ctx.save_for_backward(table, *(None if t is None else t.clone() for t in (positions, first)))
+        ctx.half, ctx.back = half, not backward
+        return _rope(x, table, positions, first, half, backward, None)
+
+    @staticmethod
+    def backward(ctx, g):
+        if g.stride(3) != 1 or g.data_ptr() % 16 or any(s * g.element_size() % 16 for s in g.stride()[:3]):
+            g = g.contiguous()
+        return rope(g, *ctx.saved_tensors, ctx.half, ctx.back), None, None, None, None, None
+
+
+def _rope(x, table, positions, first, half, backward, out):
     _all_here(x, table, positions, first, out)
     xs = _rows_of(x, "x")
     n, H, m, d = x.shape

@@ -1,0 +1,134 @@
+"""The gradient that torch records of rope: against the formula in 64 bits and differences, of shared rows, strided ones, lengths that moved on,
+captured."""
+import pytest
+import torch
+
+from paper_2602_02958_amd import binding as B
+from rows_util import turned, within
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(shape, dtype, seed):
+    return torch.randn(shape, generator=gen(seed)).to(dtype)
+
+
+def table(n, pairs, dtype, seed):
+    ang = torch.rand(n, pairs, generator=gen(seed), dtype=torch.float64) * 50 - 25
+    return torch.stack([ang.cos(), ang.sin()], -1).to(dtype)
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("dtype,tdtype,d,pairs", [(BF, F16, 128, 64), (F16, F32, 96, 20), (F32, F32, 64, 13), (F32, F16, 256, 128)])
+def test_against_the_formula(dtype, tdtype, d, pairs, half):
+    x, t, g = randn((2, 3, 7, d), dtype, 1), table(40, pairs, tdtype, 2), randn((2, 7, 3, d), dtype, 3).transpose(1, 2)
+    pos = torch.randint(0, 40, (2, 7), generator=gen(4), dtype=torch.int32)
+    xd = x.to(DEV).requires_grad_()
+    y = B.rope(xd, t.to(DEV), positions=pos.to(DEV), half=half)
+    assert torch.equal(y.detach(), B.rope(xd.detach(), t.to(DEV), positions=pos.to(DEV), half=half))
+    (got,) = torch.autograd.grad(y, xd, g.to(DEV))
+    want, tol = turned(g, t[pos.long()][:, None], half, backward=True)
+    within(got, want, tol)
+    # the gradient of the backward form is the turn itself
+    (got,) = torch.autograd.grad(B.rope(xd, t.to(DEV), positions=pos.to(DEV), half=half, backward=True), xd, g.to(DEV))
+    want, tol = turned(g, t[pos.long()][:, None], half)
+    within(got, want, tol)
+
+
+def test_against_differences():
+    """d/dx of sum w y^2 / 2 by central differences of the definition in 64 bits."""
+    x, t, w = randn((1, 2, 3, 16), F32, 5), table(3, 6, F32, 6), randn((1, 2, 3, 16), F32, 7)
+    xd = x.to(DEV).requires_grad_()
+    (got,) = torch.autograd.grad((B.rope(xd, t.to(DEV)).square() * w.to(DEV)).sum() / 2, xd)
+    step, bound = 1e-5, 0.0
+    for i in range(x.numel()):
+        e = torch.zeros(x.numel(), dtype=torch.float64)
+        e[i] = step
+        up, down = ((turned(x.double() + s * e.view(x.shape), t[None, None])[0].square() * w.double()).sum() / 2 for s in (1, -1))
+        # quadratic: the difference is exact but for 64-bit roundings of sums below 500 over the step.  y, w y and the turn back: a product
+        # and an fma of numbers below 5 x 4 each, 2^-24 of them a rounding, at most eight on the way
+        bound = 500 * 2.0 ** -50 / step + 8 * 20 * 2 * 2.0 ** -24
+        assert abs(float(up - down) / (2 * step) - float(got.flatten()[i])) <= bound
+
+
+def test_shared_rows_and_gradients_without_strides():
+    """A head's row that several heads share sums their gradients; a sum's gradient has no strides at all."""
+    x, t = randn((2, 1, 5, 64), F32, 8), table(5, 32, F32, 9)
+    xd = x.to(DEV).requires_grad_()
+    B.rope(xd.expand(2, 6, 5, 64), t.to(DEV)).sum().backward()
+    want, tol = turned(torch.ones(2, 1, 5, 64), t[None, None], backward=True)
+    # six equal gradients, five fp32 sums of them
+    within(xd.grad, 6 * want, 6 * tol + 5 * 2.0 ** -24 * 6 * want.abs())
+    # rows that do not start at 16 bytes
+    g = randn((2, 6, 5, 65), F32, 10)
+    (got,) = torch.autograd.grad(B.rope(xd.expand(2, 6, 5, 64), t.to(DEV)), xd, g.to(DEV)[..., 1:])
+    back, tol = turned(g[..., 1:], t[None, None], backward=True)
+    within(got, back.sum(1, keepdim=True), tol.sum(1, keepdim=True) + 5 * 2.0 ** -24 * back.abs().sum(1, keepdim=True))
+
+
+def test_lengths_that_move_on_before_the_gradient_comes():
+    x, t = randn((2, 2, 1, 128), BF, 11), table(60, 64, F16, 12)
+    k, v = B.alloc_pages(2, 8, 16, 128, BF, DEV)
+    pages = torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4)
+    lens = torch.tensor([3, 40], dtype=torch.int32, device=DEV)
+    xd, new = x.to(DEV).requires_grad_(), randn((2, 2, 1, 128), BF, 13).to(DEV)
+    y = B.rope(xd, t.to(DEV), first=lens)
+    B.append_pages(new, new, k, v, pages, lens, out_len=lens)
+    assert lens.tolist() == [4, 41]
+    (got,) = torch.autograd.grad(y, xd, new)
+    want, tol = turned(new.cpu(), t[[3, 40]][:, None, None], backward=True)
+    within(got, want, tol)
+
+
+def test_a_table_written_by_the_library_since_is_an_error():
+    f, _ = B.rope_frequencies(64, device=DEV)
+    t = B.rope_table(5, f)
+    y = B.rope(randn((1, 1, 5, 64), BF, 14).to(DEV).requires_grad_(), t)
+    B.rope_table(5, f, first=7, out=t)
+    with pytest.raises(RuntimeError, match="modified"):
+        y.sum().backward()
+
+
+def test_captured_with_its_gradient():
+    x, t = randn((2, 3, 9, 128), F32, 15).to(DEV), table(30, 64, F32, 16).to(DEV)
+    first, w = torch.tensor([2, 11], dtype=torch.int32, device=DEV), randn((2, 3, 9, 128), F32, 17).to(DEV)
+
+    def step(leaf):
+        return torch.autograd.grad(B.rope(leaf, t, first=first), leaf, w)[0]
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(x.clone().requires_grad_())
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    leaf = x.clone().requires_grad_()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step(leaf)
+    for i in range(4):
+        first.fill_(3 * i)
+        w.copy_(randn((2, 3, 9, 128), F32, 20 + i))
+        out.zero_()
+        g.replay()
+        assert torch.equal(out, step(x.clone().requires_grad_()))
+        torch.cuda.synchronize()
+
+
+def test_on_another_stream():
+    x, t, w = randn((1, 2, 50, 128), BF, 18).to(DEV), table(50, 64, F16, 19).to(DEV), randn((1, 2, 50, 128), BF, 20).to(DEV)
+    leaf = x.clone().requires_grad_()
+    (want,) = torch.autograd.grad(B.rope(leaf, t), leaf, w)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        leaf2 = x.clone().requires_grad_()
+        (got,) = torch.autograd.grad(B.rope(leaf2, t), leaf2, w)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got, want)
