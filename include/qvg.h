@@ -570,7 +570,8 @@ typedef struct qvg_page_step {
  * Rows i >= n_live[b], and rows that see no token, get a zero row and lse = -infinity.  What no row of a sequence sees may hold anything (also
  * what is no number): tokens behind kv_len, tokens between the first `sink` and the first row's window, whose pages may be
  * gone.  A page of a token that is seen, outside 0 .. pool_pages - 1, reads the nearest page of the pool.  All else must be
- * finite, and so must the scores, before and after they are scaled.
+ * finite, and so must the scores, before and after they are scaled: the lse of a row with a score that is no number, or
+ * infinite, is no number, and neither is the row if none of its scores is one or one is infinite (-infinity: a weight of 0).
  *   head_dim 64, 96, 128, 192 or 256; n_seqs times n_heads times blocks of 32 of a KV head's query rows at most 2^23
  *   out      may be q with q's strides; it overlaps no other input
  *   scratch  optional, 16-byte aligned: with qvg_attn_pages_scratch_bytes bytes the sequences' tokens are dealt to several workgroups

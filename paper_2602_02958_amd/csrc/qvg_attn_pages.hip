@@ -156,21 +156,23 @@ __device__ __forceinline__ RowAt row_at(const PageAttnArgs &a, int h, int64_t r)
     p.head = (int64_t)h * a.t.group + u; p.i = (int)r - u * a.t.n_new;
     return p;
 }
-// Store CH channels of a row from `ch` on: unnormalised sums o, the row's reference m and sum l of weights.
+// Store CH channels of a row from `ch` on: unnormalised sums o, the row's reference m and sum l of weights.  Where a score was no number l is
+// none, and so is the lse (a row that sees nothing has -infinity); the row itself says so where none of its scores was a number (its query
+// is none) or one was infinite, and is zero where some keys were none.
 template <class T, int CH>
 __device__ __forceinline__ void store_part(const PageAttnArgs &a, int b, int h, int64_t r, int live, int ch, const float *o, float m, float l) {
     const RowAt p = row_at(a, h, r);
-    const bool seen = p.i < live && l > 0.0f;
-    const float inv = seen ? 1.0f / l : 0.0f;
+    const bool seen = p.i < live && l > 0.0f, none = p.i < live && l != l;
+    const float inv = seen ? 1.0f / l : 0.0f, lost = none && !(m > kPgNoScore && m < INFINITY) ? l : 0.0f;
     uint32_t w[CH / 2];
 #pragma unroll
-    for (int e = 0; e < CH / 2; ++e) w[e] = seen ? T::pack(o[2 * e] * inv, o[2 * e + 1] * inv) : 0u;
+    for (int e = 0; e < CH / 2; ++e) w[e] = seen ? T::pack(o[2 * e] * inv, o[2 * e + 1] * inv) : T::pack(lost, lost);
     uint16_t *out = static_cast<uint16_t *>(a.t.out) + b * a.t.out_stride_seq + p.head * a.t.out_stride_head + p.i * a.t.out_stride_token + ch;
     if constexpr (CH == 8) *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
     if (a.t.lse && ch == 0)
         a.t.lse[((int64_t)b * a.c.n_heads * a.t.group + p.head) * a.t.n_new + p.i] =
-            seen ? (m * a.scale + (__builtin_log2f(l) - kPgUp)) * 0.6931471805599453f : -INFINITY;
+            seen ? (m * a.scale + (__builtin_log2f(l) - kPgUp)) * 0.6931471805599453f : (none ? l : -INFINITY);
 }
 
 // A lane's tokens of a tile are places in its page (paged), or rows anywhere in the pool, which lanes 0 .. 31 look up and leave in LDS.
