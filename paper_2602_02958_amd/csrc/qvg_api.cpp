@@ -7,8 +7,8 @@
 #include <new>
 
 #include "qvg.h"
+#include "qvg_attn_pages.hpp"
 #include "qvg_internal.hpp"
-#include "qvg_rows.hpp"
 #include "qvg_tree.hpp"
 
 using namespace qvg;

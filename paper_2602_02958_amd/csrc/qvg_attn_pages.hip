@@ -26,6 +26,7 @@ namespace qvg {
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4_t;
 
 constexpr int kPgThreads = 256, kPgWaves = kPgThreads / 64;
+static_assert(kPgLeast == kPgWaves, "a slot has a tile for each wavefront");
 constexpr float kPgNoScore = -3.402823466e38f;      // the running reference before any product
 // References are products q.k, before the scale: a weight is exp2((product - reference) x scale + kPgUp), whose difference is exact where it
 // matters, however large the products are.  A reference moves when a weight would pass 2^(kPgUp + kPgLag): they stay below 2^14,
@@ -33,7 +34,7 @@ constexpr float kPgNoScore = -3.402823466e38f;      // the running reference bef
 constexpr float kPgUp = 7.0f, kPgLag = 7.0f;
 // Binary16 ends at 2^-24, 2^-31 of a row's reference: many tokens that far below it are a part of the sum all the same (65536 tokens of
 // 2^-33 and values 2^16 times as large as the heavy token's).  So a tile whose weights are all below 2^-kPgThin of the reference enters
-// lifted by a power of two, with the row's sums lifted for as long (2^kPgMost of 2^58 at most): a weight is off by 2^-24 of the largest of
+// lifted by a power of two, with the row's sums lifted for as long (2^kPgMost of 2^60 at most): a weight is off by 2^-24 of the largest of
 // its tile at most, as an fp32 sum would be.  (Nothing to be measured: 12 heads over 748800 tokens 679 us, 680 with most tiles lifted, 677 in
 // bf16.)
 constexpr float kPgThin = 8.0f, kPgMost = 40.0f;
@@ -66,18 +67,9 @@ __device__ __forceinline__ PgLens lens_of(const PageAttnArgs &a, int b) {
     return {a.c.table_pages ? a.c.kv_len[b] : 0, a.t.n_live ? a.t.n_live[b] : a.t.n_new};
 }
 
-// How the slots of a divided call (a.slots of them, the same for every head and row block) are dealt to the sequences: a slot for every q
-// tiles or part of them, and one at least.  With n sequences and a.extra = slots - n the sum of ceil(T / q) is at most total / q + n, so that
-// q = total / extra suffices.  Where there are few sequences it is the smallest that does, or nearly: it lies between total / slots and
-// that, and is found in five halvings.  Where there are many it stays: the usual ones are taken whole, and those of more than q
-// tiles, fewer than `extra`, have 2 extra parts at most, which are all that leave partial results.
-// Every wavefront works that out for itself from the lengths, which only the device knows (n <= 256: a call of more sequences
-// is not divided).  Slots that are left over have nothing to do.
+// The slots of a divided call, dealt to the sequences as pg_share says.  Every wavefront works that out for itself from the lengths, which
+// only the device knows (n <= 256: a call of more sequences is not divided).  Slots that are left over have nothing to do.
 struct Slot { int b, part, parts, first; PgLens n; };                    // first: of the sequence's partial results; part >= parts: none
-__device__ __forceinline__ int parts_of(int total, int q) {
-    const int p = (int)(((uint32_t)total + (uint32_t)q - 1u) / (uint32_t)q);
-    return p < 1 ? 1 : p;
-}
 // Sums of lanes 0 .. i, and of all, between lanes of a row and then rows (no LDS, which five halvings of six exchanges would wait for)
 template <typename N>
 __device__ __forceinline__ N lanes_upto(N x) {
@@ -106,8 +98,8 @@ __device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot, DealPlace 
     Slot p{0, 0, 0, 0, {0, 0}};
     if (n == 1) {
         p.n = lens_of(a, 0);
-        const int total = pg_span_of<PAGED>(a, p.n).total, q = max(parts_of(total, a.slots), kPgWaves);
-        p.parts = parts_of(total, q);
+        const int total = pg_span_of<PAGED>(a, p.n).total, q = max(pg_parts(total, a.slots), kPgLeast);
+        p.parts = pg_parts(total, q);
         p.part = slot;
         return p;
     }
@@ -121,21 +113,20 @@ __device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot, DealPlace 
         total += (float)t;
     }
     total = lanes_sum(total);
-    // (rounded up, and down, by more than the sum is off; 2^26: more tiles than a sequence has)
-    int q = max((int)fminf(total * (1.0001f * __builtin_amdgcn_rcpf((float)a.extra)), 67108863.0f) + 1, kPgWaves);
-    int lo = n <= a.extra ? max((int)(total * (0.9999f * __builtin_amdgcn_rcpf((float)a.slots))), kPgWaves) : q;
+    const PgShare share = pg_share(total, __builtin_amdgcn_rcpf((float)a.extra), __builtin_amdgcn_rcpf((float)a.slots), n, a.extra);
+    int lo = share.lo, q = share.q;
 #pragma unroll 1
-    for (int h = 0; h < 5 && lo < q; ++h) {                              // uniform
+    for (int h = 0; h < kPgHalvings && lo < q; ++h) {                    // uniform
         const int mid = lo + (q - lo) / 2;
         int need = 0;
 #pragma unroll 1
-        for (int k = 0; k < n; k += 64) need += k + lane < n ? parts_of(keep.tiles[k + lane], mid) : 0;
+        for (int k = 0; k < n; k += 64) need += k + lane < n ? pg_parts(keep.tiles[k + lane], mid) : 0;
         if (lanes_sum(need) <= a.slots) q = mid; else lo = mid + 1;
     }
     int before = 0, divided = 0;                                         // slots, and partial results, of the sequences before
 #pragma unroll 1
     for (int k = 0; k < n; k += 64) {
-        const int i = k + lane, mine = i < n ? parts_of(keep.tiles[i], q) : 0, kept = mine > 1 ? mine : 0;
+        const int i = k + lane, mine = i < n ? pg_parts(keep.tiles[i], q) : 0, kept = mine > 1 ? mine : 0;
         const int upto = before + lanes_upto(mine), kept_upto = divided + lanes_upto(kept);
         const unsigned long long hit = __ballot(slot >= upto - mine && slot < upto);
         if (hit) {
@@ -153,9 +144,6 @@ __device__ __forceinline__ Slot deal(const PageAttnArgs &a, int slot, DealPlace 
     }
     return p;
 }
-// A part's partial result: [rows][D] sums, then the rows' references, then their sums of weights.
-static __host__ __device__ inline int64_t part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
-
 // Where a query row lies: head h * group + r / n_new, row r % n_new of the sequence.
 struct RowAt { int64_t head; int i; };
 __device__ __forceinline__ RowAt row_at(const PageAttnArgs &a, int h, int64_t r) {
@@ -545,47 +533,6 @@ static void launch_join(const PageAttnArgs &a, int64_t n, hipStream_t s) {
 }
 
 bool page_attn_dim(int d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
-
-PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
-    PagePlan p{16, 1, 0, 0, 0, 0, 0};
-    // Tiles end where pages do, so that a tile's page is uniform, unless that would leave many of them short.
-    p.paged = c.page_len % kPgTile == 0 || c.page_len >= 8 * kPgTile;
-    // tiles that a sequence's rows see, at most
-    int64_t tiles = p.paged ? (int64_t)c.table_pages * page_tiles((int)c.page_len) : page_tiles((int)(c.table_pages * c.page_len));
-    if (t.window > 0) {
-        const int64_t seen = (int64_t)t.window + t.n_new + t.sink, most = seen / kPgTile + 4 + (p.paged ? seen / c.page_len : 0);
-        if (most < tiles) tiles = most;
-    }
-    const int64_t rows = (int64_t)t.group * t.n_new;
-    p.rows = rows <= 16 ? 16 : 32;
-    p.row_blocks = (int)((rows + p.rows - 1) / p.rows);
-    const int64_t units = (int64_t)c.n_heads * p.row_blocks;             // of a sequence
-    if (c.n_seqs < 1 || c.n_seqs > 256 || rows < 1) return p;
-    // Two workgroups to a CU, which lengths that differ are dealt to best, or one where no two fit a CU, and for a sequence alone, whose
-    // parts are all alike (4 heads x 64 rows over 32768 tokens 27 -> 23 us, 256 channels 176 -> 168; a ragged batch of 16: 182 -> 176 us
-    // with two; three take up to 20 % longer, four up to 41 %); a tile to a wavefront at least.  With more sequences than that a call
-    // is divided only for those that are much longer than the others (extra).
-    // Not divided below 28 tiles, which cost less than the second launch (16 sequences of 500 tokens, 8 heads: 9.6 us, 13.4
-    // divided; 8 of 700: 10.8 and 13.0; but one of 1000: 12.6 and 8.2).
-    const int chip = c.n_seqs == 1 || c.head_dim > 192 || c.head_dim * p.rows > 16 * 256 ? 256 : 512;
-    if (tiles < 28 || (c.n_seqs == 1 && units > 128)) return p;          // (1024 rows of 8 heads over 8192: 79 us, 94 divided)
-    const int64_t full = (chip + units - 1) / units;
-    int64_t slots = chip / units;
-    if (slots >= 2 * (int64_t)c.n_seqs) {
-        const int64_t most = c.n_seqs * (tiles / kPgWaves);
-        if (slots > most) slots = most;
-        p.extra = (int)(slots - c.n_seqs);
-        p.kept = (int)slots;
-    } else {
-        if (tiles < 256 || units >= chip || c.n_seqs * c.n_heads * rows > (1 << 22)) return p;       // (128 of 2000 tokens: 178 us, 215 so)
-        slots = c.n_seqs + full;
-        p.extra = (int)full;
-        p.kept = (int)(2 * full < slots ? 2 * full : slots);
-    }
-    p.slots = (int)slots;
-    p.state_bytes = (size_t)(units * p.kept * part_floats(p.rows, c.head_dim)) * sizeof(float) + (size_t)c.n_seqs * sizeof(int2);
-    return p;
-}
 
 template <class T, int D>
 static void launch_dim(const PageAttnArgs &a, int blocks, hipStream_t s) {

@@ -59,7 +59,6 @@ struct PageAttnArgs {
     int2 *places;                                 // [n_seqs] a sequence's first partial result and its parts, for the joining launch
 };
 struct PagePlan { int rows, row_blocks, slots, extra, kept, paged; size_t state_bytes; };      // (as in PageAttnArgs)
-PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t);
 bool page_attn_dim(int d);
 hipError_t launch_attn_pages(const PageAttnArgs &a, hipStream_t s);
 
