@@ -504,25 +504,23 @@ void join_pages_kernel(PageAttnArgs a, int64_t n_rows) {
             o.x = o.x * g + x.x * f; o.y = o.y * g + x.y * f; o.z = o.z * g + x.z * f; o.w = o.w * g + x.w * f;
         }
     }
-    if constexpr (PER > 1) {
-        if (there) {
-            *reinterpret_cast<float4 *>(&sums[grp][c4 * 4]) = o;
-            if (c4 == 0) { weights[grp] = l; tops[grp] = m; }
-        }
-        __syncthreads();
-        if (!parts || grp != j * PER) return;
+    if (there) {
+        *reinterpret_cast<float4 *>(&sums[grp][c4 * 4]) = o;
+        if (c4 == 0) { weights[grp] = l; tops[grp] = m; }
+    }
+    __syncthreads();
+    if (!parts || grp != j * PER) return;
 #pragma unroll
-        for (int g = 0; g < PER; ++g) m = fmaxf(m, tops[grp + g]);
-        l = 0.0f;
-        o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int g = 0; g < PER; ++g) m = fmaxf(m, tops[grp + g]);
+    l = 0.0f;
+    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int g = 0; g < PER; ++g) {
-            const float4 x = *reinterpret_cast<const float4 *>(&sums[grp + g][c4 * 4]);
-            const float f = __builtin_amdgcn_exp2f((tops[grp + g] - m) * a.scale);
-            l += weights[grp + g] * f;
-            o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
-        }
-    } else if (!parts) return;
+    for (int g = 0; g < PER; ++g) {
+        const float4 x = *reinterpret_cast<const float4 *>(&sums[grp + g][c4 * 4]);
+        const float f = __builtin_amdgcn_exp2f((tops[grp + g] - m) * a.scale);
+        l += weights[grp + g] * f;
+        o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+    }
     const float v[4] = {o.x, o.y, o.z, o.w};
     store_part<T, 4>(a, b, h, r, a.t.n_live ? max(0, min(a.t.n_live[b], a.t.n_new)) : a.t.n_new, c4 * 4, v, m, l);
 }
@@ -545,7 +543,7 @@ static void launch_dim(const PageAttnArgs &a, int blocks, hipStream_t s) {
     if (a.slots) {
         const int64_t n = (int64_t)a.c.n_seqs * a.c.n_heads * a.t.group * a.t.n_new;
         // (many rows have few parts)
-        if (n > 512) launch_join<T, D, 1024 / D < 4 ? 1 : 2>(a, n, s);
+        if (n > 512) launch_join<T, D, 2>(a, n, s);
         else launch_join<T, D, 1024 / D>(a, n, s);
     }
 }
