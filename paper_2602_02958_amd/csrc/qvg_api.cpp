@@ -961,6 +961,10 @@ int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softma
         !rows_aligned(t->out, 2, t->out_stride_seq, t->out_stride_head, t->out_stride_token) || !aligned4(t->n_live) || !aligned4(t->lse) ||
         !aligned16(scratch))
         return QVG_ERR_ALIGN;
+    // (a workgroup reads its own rows of q before it writes them, and no others)
+    if (t->q == t->out && ((c->n_seqs > 1 && t->q_stride_seq != t->out_stride_seq) || ((c->n_heads > 1 || t->group > 1) && t->q_stride_head != t->out_stride_head) ||
+                           (t->n_new > 1 && t->q_stride_token != t->out_stride_token)))
+        return QVG_ERR_BAD_PARAM;
     const PagePlan plan = page_plan(*c, *t);
     PageAttnArgs a{};
     a.c = *c; a.t = *t; a.scale = scale;
