@@ -922,7 +922,7 @@ def _page_cache(k_pages, v_pages, page_table, kv_len, written=False) -> QvgPageC
         raise ValueError("page_table: need [B, M]")
     n, pages = table
     return QvgPageCache(TYPES[dtype], n, shape[0], shape[3], pages, 0, shape[2], shape[1], _counts(page_table, table, "page_table"),
-                        _counts(kv_len, (n,), "kv_len"), k_pages.data_ptr(), v_pages.data_ptr(), ks[0], ks[1], ks[2])
+                        _counts(kv_len, (n,), "kv_len"), k_pages.data_ptr(), v_pages.data_ptr(), ks[0], ks[1], ks[2] if shape[2] > 1 else 0)
 
 
 def append_pages(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new=None, k_rope=None, positions=None, half=False,
