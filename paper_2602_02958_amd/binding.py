@@ -779,6 +779,7 @@ def rope_table(n, frequencies, first=0, positions=None, axis=None, amplitude=1.0
         _check(out, dtype, "out")
         torch.autograd.graph.increment_version(out)                      # (a gradient of rope that has kept it is an error then)
     _here(frequencies, positions, out)
+    first = max(min(first, 1 << 31), -1)                                 # (ctypes keeps the low bits only)
     st = lib().qvg_rope_table(n, P, frequencies.data_ptr(), first, pos, A, ax, amplitude, TYPES[dtype], out.data_ptr(), _stream())
     if st != 0:
         raise QvgError(st, "qvg_rope_table")
@@ -995,7 +996,7 @@ def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True,
     else:
         o0, o1, o2, _ = _rows_of(out, "out", q.dtype, q.shape, True)
     lse = torch.empty(n, hq, m, dtype=torch.float32, device=device) if want_lse else None
-    window, sink = 0 if window is None else min(window, 0x7fffffff), min(sink, 0x7fffffff)
+    window, sink = 0 if window is None else min(window, 0x7fffffff), max(min(sink, 0x7fffffff), -1)      # (ctypes keeps the low bits only)
     if scratch is None:
         scratch = _scratch(_pages_scratch_bytes(n, H, d, group, m, pages, L, window, sink), device)
     elif scratch.dtype is not torch.uint8 or not scratch.is_contiguous():
