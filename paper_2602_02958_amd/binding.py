@@ -881,7 +881,7 @@ class _Turn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g):
         if g.stride(3) != 1 or g.data_ptr() % 16 or any(s * g.element_size() % 16 for s in g.stride()[:3]):
-            g = g.contiguous()
+            g = g.clone(memory_format=torch.contiguous_format)
         return rope(g, *ctx.saved_tensors, ctx.half, ctx.back), None, None, None, None, None
 
 

@@ -70,6 +70,10 @@ def test_shared_rows_and_gradients_without_strides():
     (got,) = torch.autograd.grad(B.rope(xd.expand(2, 6, 5, 64), t.to(DEV)), xd, g.to(DEV)[..., 1:])
     back, tol = turned(g[..., 1:], t[None, None], backward=True)
     within(got, back.sum(1, keepdim=True), tol.sum(1, keepdim=True) + 5 * 2.0 ** -24 * back.abs().sum(1, keepdim=True))
+    g = randn((1 + 2 * 5 * 64,), F32, 11)
+    (got,) = torch.autograd.grad(B.rope(xd, t.to(DEV)), xd, g.to(DEV)[1:].view(2, 1, 5, 64))
+    back, tol = turned(g[1:].view(2, 1, 5, 64), t[None, None], backward=True)
+    within(got, back, tol)
 
 
 def test_lengths_that_move_on_before_the_gradient_comes():
