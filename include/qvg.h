@@ -506,7 +506,7 @@ int qvg_rope_table(int64_t n_rows, int32_t n_pairs, const double *frequencies, i
  *                be x with x's strides, and overlaps it in no other way
  *   r            token i of sequence b stands at r->positions[b][i]; without positions at first[b] + i; without first at i
  *   first        [n_seqs] int32, device, or NULL
- * head_dim a multiple of 8 up to 512; n_seqs * n_tokens below 2^31.  Slower: half with n_pairs no multiple of 8.
+ * head_dim a multiple of 8 up to 512; n_seqs * n_tokens below 2^31.  Slower, three times and more: half with n_pairs no multiple of 8.
  */
 int qvg_rope(const qvg_rotary *r, int32_t type, int64_t n_seqs, int32_t n_heads, int64_t n_tokens, int32_t head_dim,
              const void *x, int64_t x_stride_seq, int64_t x_stride_head, int64_t x_stride_token, const int32_t *first, int32_t backward,
@@ -541,7 +541,7 @@ typedef struct qvg_page_cache {    /* a HOST structure; its pointers are device 
  *   len_out       [n_seqs] int32 or NULL: kv_len[b] + n_live[b], at most table_pages * page_len; may be kv_len
  * A token beyond the table, or whose page is outside 0 .. pool_pages - 1, is not written; nothing else of the pool is touched.
  * No two tokens may go to the same place (of a page that sequences share, or that a table names twice), and the pool must not overlap
- * k_new or v_new.  head_dim a multiple of 8 up to 512; n_seqs * n_new below 2^31.
+ * k_new or v_new.  head_dim a multiple of 8 up to 512 (qvg_attn_pages reads 64, 96, 128, 192 and 256); n_seqs * n_new below 2^31.
  */
 int qvg_append_pages(const qvg_page_cache *c, int64_t n_new, const void *k_new, const void *v_new, int64_t new_stride_seq,
                      int64_t new_stride_head, int64_t new_stride_token, const int32_t *n_live, const qvg_rotary *r, int32_t *len_out,

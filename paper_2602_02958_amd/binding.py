@@ -725,10 +725,11 @@ def copy_pages(cache: Encoded, src, dst, into: Encoded | None = None) -> Encoded
 def rope_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, trained=None, low=1.0, high=32.0, device="cuda"):
     """Frequencies of a rotary embedding of `rotary_dim` channels and the amplitude that goes with them: (float64 [rotary_dim / 2],
     float), base^(-2p / rotary_dim) radians a place.  For contexts `factor` times as long as those trained with:
-    scaling "linear": every frequency divided by factor (positions interpolated);
-    "base": the base raised to base * factor^(r / (r - 2)), r = rotary_dim: the slowest pair is divided by factor, the fastest one stays;
+    scaling "linear": every frequency divided by factor (positional interpolation, Chen et al. 2023);
+    "base": the base raised to base * factor^(r / (r - 2)), r = rotary_dim: the slowest pair is divided by factor, the fastest one stays
+    (known as NTK-aware scaling);
     "bands": by the number of turns a pair makes in `trained` places: from `high` on as it is, below `low` divided by factor, between
-    them mixed in proportion; amplitude 0.1 ln(factor) + 1, which both sides of a score are multiplied by."""
+    them mixed in proportion; amplitude 0.1 ln(factor) + 1, which both sides of a score are multiplied by (YaRN, Peng et al. 2023)."""
     if rotary_dim < 2 or rotary_dim % 2:
         raise ValueError("rotary_dim: need an even number of channels")
     if not (base > 0 and math.isfinite(base) and factor >= 1 and math.isfinite(factor)):
@@ -933,7 +934,7 @@ def append_pages(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new=None,
     sequences' pages, kv_len [B] int32: their tokens so far, n_new [B] int32: how many of the N are there (None: all).
     k_rope [n, P, 2]: K is turned on the way, by the row of its place in the sequence, or of positions [B, N] int32; half as in rope.
     Returns the new lengths [B] int32 (out_len, which may be kv_len, or a new tensor).  Tokens beyond the table, and those of pages
-    outside the pool, are left out."""
+    outside the pool, are left out.  Any d that is a multiple of 8 up to 512; attn_pages reads pages of 64, 96, 128, 192 and 256."""
     _all_here(k_new, v_new, k_pages, v_pages, page_table, kv_len, n_new, k_rope, positions, out_len)
     c = _page_cache(k_pages, v_pages, page_table, kv_len, True)
     ns = _two_rows(k_new, v_new, ("k_new", "v_new"), k_pages.dtype)
@@ -976,7 +977,7 @@ def attn_pages(q, k_pages, v_pages, page_table, kv_len, n_new=None, causal=True,
     the new tokens) -> out like q (and lse fp32 [B, H * group, N]); query head h reads KV head h // group.
     n_new [B] int32: how many of the N there are (None: all); row i of a sequence stands at place kv_len - n_new + i and sees the
     tokens up to its place (causal), or all kv_len, and with a window only the newest `window` of its place and the first `sink` tokens.
-    Rows behind n_new, and those that see nothing, are zero with lse -inf.
+    Rows behind n_new, and those that see nothing, are zero with lse -inf.  The result carries no gradient.
     scratch: uint8 tensor of attn_pages_scratch bytes for dividing the call over the chip; without one it is taken from torch's
     allocator (where that has no memory left the call runs undivided, which differs by the order of fp32 sums)."""
     _all_here(q, k_pages, v_pages, page_table, kv_len, n_new, out, scratch)

@@ -118,6 +118,8 @@ inline PagePlan page_plan(const qvg_page_cache &c, const qvg_page_step &t) {
     // divided; 8 of 700: 10.8 and 13.0; but one of 1000: 12.6 and 8.2).
     const int chip = c.n_seqs == 1 || c.head_dim > 192 || c.head_dim * p.rows > 16 * 256 ? 256 : 512;
     if (tiles < 28 || (c.n_seqs == 1 && units > 128)) return p;          // (1024 rows of 8 heads over 8192: 79 us, 94 divided)
+    // (The cut at 128 units is coarse: divided, 144 and 160 units over 8192 tokens take 63 and 70 us instead of 78, over 65536 443 and 468
+    // instead of 628 and 650; 240 units 89 instead of 78 to 80, and 606 and 670 instead of 609 and 639.)
     const int64_t full = (chip + units - 1) / units;
     int64_t slots = chip / units;
     if (slots >= 2 * (int64_t)c.n_seqs) {

@@ -10,8 +10,8 @@ namespace qvg {
 // A pair to a thread.  The angle is taken in quarter turns: place x frequency x 4 / 2 pi in 64 bits, less its nearest whole number (adding
 // 1.5 x 2^52 rounds to it, and leaves it in the sum's low bits), is half a quarter or less, which 32 bits hold to 2^-27 of a
 // turn.  Sine and cosine of that are Taylor's polynomials in 32 bits (their next terms are below 2^-29 at pi / 4), and the quarter says which
-// is which and its sign.  Memory bounds a large table of 32 bits: 748800 x 64 pairs and three axes, 392 MB, 66 us (5.9 TB/s); of 16 bits the
-// 35 instructions of a pair do, 51 us for 191 MB.
+// is which and its sign.  Memory bounds a large table of 32 bits: 748800 x 64 pairs and three axes, 392 MB, 70 us (5.6 TB/s); of 16 bits the
+// 35 instructions of a pair do, 49 us for 201 MB (replayed in a graph; the other figures of this file are launches of their own).
 __device__ __forceinline__ float2 cos_sin_of(double place, double quarters) {
     const double x = place * quarters, sum = x + 6755399441055744.0;
     const float r = (float)(x - (sum - 6755399441055744.0));
@@ -55,7 +55,8 @@ void rope_table_kernel(RopeTableArgs a, FastDiv by_pairs, int rows_per_block) {
         if constexpr (sizeof(TAB) == 4) v = two{__float_as_uint(cs.x), __float_as_uint(cs.y)};
         else v = pack_f16x2_rne(cs.x, cs.y);
         pair *row = to + (uint32_t)(j * rows_per_block * a.n_pairs);
-        // (a large table is read long after: past the caches it takes 66 us instead of 80, 383 MB)
+        // (past the caches a large table takes 66 us instead of 80, 392 MB, and what reads it next is no slower: 37440 places and then
+        // 12 x 4680 rows turned by some of them 11.5 us in a graph, 11.8 with the table written through the caches)
         if constexpr (ROWS > 1) __builtin_nontemporal_store(v, row);
         else *row = v;
     }
@@ -92,7 +93,7 @@ __device__ __forceinline__ Octet<T> load_octet(const typename T::raw *p) {
     for (size_t i = 0; i < sizeof(o.w) / 16; ++i) o.w[i] = reinterpret_cast<const uint4 *>(p)[i];
     return o;
 }
-// FAR: nobody reads them soon
+// FAR: past the caches' usual order of eviction
 template <class T, bool FAR>
 __device__ __forceinline__ void store_octet(typename T::raw *p, const Octet<T> &o) {
     typedef uint32_t words __attribute__((ext_vector_type(4)));
@@ -173,9 +174,14 @@ enum { kTurnNext, kTurnHalf, kTurnPair, kTurnNone };
 constexpr int kTurnHeads = 4;      // heads that a thread takes at once, where there are many rows: they share the table's row
 
 // A thread takes a piece of a token's rows in `HP` heads: it reads the table's row once for all of them, and all rows before it
-// writes any.  Memory bounds it, the rows both ways: 40 heads x 10800 rows of 128 bf16, 224 MB with the table, 40.7 us (5.5 TB/s); 12
-// heads x 4680 keys and values into pages, 59 MB, 11.6 us (5.1 TB/s; 14.2 with a head to a thread, written through the
-// caches); a token's 12 heads 2.4 us, a launch.
+// writes any.  Memory bounds it, the rows both ways: 40 heads x 10800 rows of 128 bf16, 224 MB with the table, 41 us (5.5 TB/s); 12
+// heads x 4680 keys and values into pages, 59 MB, 12.5 us (4.7 TB/s); a token's 12 heads 3.2 us, a launch.  Pages are written past the
+// caches: in a graph 9.7 us, 11.3 written through them, which attention that reads them next pays back, so that a step is as long either way
+// (append and attend: a chunk behind another, one row of each head 28.8 and 28.7 us, all rows 600 and 598; a token of 16 sequences over
+// 512 12.9 and 13.1; 64 new ones of each 33.9 to 34.3 and 34.0).
+// One pair to a thread and a head (kTurnPair), where the pairs' second halves start between 16-byte places: 12 x 4680 rows 17 us for 60
+// pairs and 23 for 29, 6.2 for 64; into pages 26, 34 and 7.9 (in a graph).  Elements of 2 bytes are loaded and stored one by one; octets
+// would have to be shifted between lanes.
 template <class T, typename TAB, int MODE, bool APPEND, int HP>
 __global__ __launch_bounds__(256)
 void turn_kernel(TurnArgs a, int per_block, int whole) {

@@ -5,7 +5,7 @@
 
 namespace qvg {
 
-// n / d for n below 2^31 as a multiplication: (mulhi(n, mul) + n) >> shift
+// n / d for n below 2^31 as a multiplication, (mulhi(n, mul) + n) >> shift: division by an invariant number after Granlund and Montgomery (1994)
 struct FastDiv { uint32_t d, mul, shift; };
 inline FastDiv fast_div(uint32_t d) {
     uint32_t s = 0;

@@ -72,10 +72,10 @@ def test_chunks(kv, live, H, g, m, d, L, dtype, causal, window, sink):
 
 
 def test_as_many_rows_as_a_call_takes():
-    """2^20 query rows of a KV head, 32768 blocks; of 3 heads."""
+    """2^20 query rows of a KV head, 32768 blocks; of 2 heads."""
     d, L = 64, 16
-    kp, vp = (rows_on_device((3, 3, L, d), BF, s) for s in (5, 6))
-    q = rows_on_device((1, 3 * 1024, 1024, d), BF, 7)
+    kp, vp = (rows_on_device((2, 3, L, d), BF, s) for s in (5, 6))
+    q = rows_on_device((1, 2 * 1024, 1024, d), BF, 7)
     table, kv = torch.tensor([[2, 0, 1]], dtype=torch.int32, device=DEV), torch.tensor([35], dtype=torch.int32, device=DEV)
     out, lse = B.attn_pages(q, kp, vp, table, kv, causal=False, want_lse=True)
     check(q, kp, vp, table, [35], [1024], out, lse, causal=False, block=1024)
