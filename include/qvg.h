@@ -578,9 +578,9 @@ typedef struct qvg_page_step {
  *            per KV head, by the sequences' lengths, and one more launch joins their partial results.  NULL or less: undivided, which
  *            differs by the order of fp32 sums.  Equal calls give equal bits; among others a sequence's result may differ by
  *            that order too.  Contents are scratch: nothing has to be initialised and nothing survives the call.
- * What is rounded: queries, keys and values enter the two contractions as they are, weights as two numbers of the type: off by
- * 2^-16 of themselves (bf16) or 2^-22, and in binary16 by no less than 2^-24 of the largest weight of their 32 tokens; scores, sums
- * and output are fp32 until the output is rounded.
+ * What is rounded: queries, keys and values enter the two contractions as they are, weights as two numbers of the type, off by at
+ * most 2^-16 of themselves (bf16), or the larger of 2^-22 of themselves and 2^-24 of the largest of their 32 tokens' (binary16);
+ * scores, sums and output are fp32 until the output is rounded.
  */
 int qvg_attn_pages(const qvg_page_cache *c, const qvg_page_step *t, float softmax_scale, void *scratch, size_t scratch_bytes, void *stream);
 

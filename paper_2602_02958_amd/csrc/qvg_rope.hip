@@ -11,7 +11,7 @@ namespace qvg {
 // 1.5 x 2^52 rounds to it, and leaves it in the sum's low bits), is half a quarter or less, which 32 bits hold to 2^-27 of a
 // turn.  Sine and cosine of that are Taylor's polynomials in 32 bits (their next terms are below 2^-29 at pi / 4), and the quarter says which
 // is which and its sign.  Memory bounds a large table of 32 bits: 748800 x 64 pairs and three axes, 392 MB, 70 us (5.6 TB/s); of 16 bits the
-// 35 instructions of a pair do, 49 us for 201 MB (replayed in a graph; the other figures of this file are launches of their own).
+// 35 instructions of a pair do, 49 us for 201 MB (replayed in a graph).
 __device__ __forceinline__ float2 cos_sin_of(double place, double quarters) {
     const double x = place * quarters, sum = x + 6755399441055744.0;
     const float r = (float)(x - (sum - 6755399441055744.0));
@@ -55,8 +55,8 @@ void rope_table_kernel(RopeTableArgs a, FastDiv by_pairs, int rows_per_block) {
         if constexpr (sizeof(TAB) == 4) v = two{__float_as_uint(cs.x), __float_as_uint(cs.y)};
         else v = pack_f16x2_rne(cs.x, cs.y);
         pair *row = to + (uint32_t)(j * rows_per_block * a.n_pairs);
-        // (past the caches a large table takes 66 us instead of 80, 392 MB, and what reads it next is no slower: 37440 places and then
-        // 12 x 4680 rows turned by some of them 11.5 us in a graph, 11.8 with the table written through the caches)
+        // (replayed in a graph a large table, 392 MB, takes 66 to 72 us past the caches, 80 through them, and what reads it next is no
+        // slower: 37440 places and then 12 x 4680 rows turned by some of them 11.5 and 11.8 us)
         if constexpr (ROWS > 1) __builtin_nontemporal_store(v, row);
         else *row = v;
     }
